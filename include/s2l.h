@@ -179,6 +179,103 @@ s2l_status s2l_kv_append(const s2l_kv_cache* cache, const s2l_batch* batch,
                          const void* k_new, const void* v_new, void* stream);
 
 /*
+ * Rotary positions with one or several axes (text; time, height and width of images and video): the
+ * first rot_dim dims of a head are rot_dim / 2 pairs, and pair i of the row at position x (on its
+ * axis) turns by the angle x * inv_freq[i]:
+ *   (a, b) -> scale * (a cos - b sin, b cos + a sin)
+ * in fp32 with a cos and sin of the exact product (in turns, by 64-bit arithmetic: far positions lose
+ * nothing), rounded once to bf16.  Dims from rot_dim on pass through unchanged.  Pair i is dims
+ * (i, i + rot_dim / 2), or (2 i, 2 i + 1) with S2L_ROPE_ADJACENT.  Not in the paper, whose models'
+ * layers rotate before they append.
+ */
+#define S2L_ROPE_MAX_AXES 4
+#define S2L_ROPE_ADJACENT 1
+typedef struct s2l_rope {
+  const float* inv_freq;    /* device [rot_dim / 2], radians a position                       */
+  const int32_t* positions; /* device [num_axes][pos_stride]: of every row of the batch, axis   */
+                            /* by axis; NULL (one axis only): row i of request r is at P_r + i  */
+  int64_t pos_stride;       /* elements from one axis to the next, >= T (unused with NULL)    */
+  int32_t rot_dim;          /* a multiple of 16, 16 .. 128                                    */
+  int32_t num_axes;         /* 1 .. S2L_ROPE_MAX_AXES                                         */
+  int32_t flags;            /* 0 or S2L_ROPE_ADJACENT                                         */
+  float scale;              /* factor on the rotated dims (1 for none), finite, > 0           */
+  uint8_t pair_axis[64];    /* axis of pair i, for i < rot_dim / 2; each < num_axes           */
+} s2l_rope;
+
+/*
+ * Rotate a step's queries and keys (as above) without appending: for layers that keep no pages, such
+ * as s2l_linear_attn's, one launch.
+ *   q: device bf16, row i of request r at element (cu_chunk[r] + i) * q_stride, its Hq heads of 128 one
+ *      after another; q_out likewise with q_out_stride.  k, k_out likewise; Hkv 0 and NULL for none.
+ *      An output may be its own input with the same stride; otherwise outputs overlap nothing.
+ *   Strides are in elements; of the outputs (and, beyond one row, of the inputs) at least heads * 128.
+ *      Rows from T on are not touched.  Any element alignment is taken; 16 bytes are fastest.
+ * Errors: EINVAL (nulls, negative or inconsistent arguments), ENOTSUP (rot_dim, axes), EHIP.
+ */
+s2l_status s2l_rope_qk(const s2l_batch* batch, const s2l_rope* rope, const void* q, int64_t q_stride,
+                       int32_t num_q_heads, void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride,
+                       int32_t num_kv_heads, void* k_out, int64_t k_out_stride, void* stream);
+
+/*
+ * s2l_kv_append of the rotated keys and of the values, and the rotated queries (Hq 0 and NULL for none),
+ * in one launch: pages and q_out are bit for bit what s2l_rope_qk followed by s2l_kv_append gives.
+ * Arguments as there; k and v are rows of Hkv heads of 128 with their own strides, so that the three
+ * may be views of one projected row.  A row's rotation goes by `rope`, its page and slot by P_r + i.
+ * Errors: as s2l_rope_qk and s2l_kv_append.
+ */
+s2l_status s2l_rope_kv_append(const s2l_kv_cache* cache, const s2l_batch* batch, const s2l_rope* rope,
+                              const void* q, int64_t q_stride, int32_t num_q_heads, void* q_out,
+                              int64_t q_out_stride, const void* k, int64_t k_stride, const void* v,
+                              int64_t v_stride, void* stream);
+
+/*
+ * Linear attention with a decay for each query head, for layers whose cache is a state of fixed size
+ * (not in the paper).  With g = h / G, l = exp(log_decay[h]), S the fp32 state [128 k][128 v] of
+ * request r and head h after its P_r cached tokens, and chunk rows i = 0 .. C_r - 1 in order:
+ *   S <- l S + k_i[g] v_i[g]^T        out_i[h] = scale * q_i[h] S        (bf16, RNE)
+ * Chunks of any split of a sequence give the same results up to rounding.
+ *   states   : device fp32 [num_slots][Hq][128][128]: request states in slots.
+ *   log_decay: device fp32 [Hq], ln of the decay, <= 0 (values above 0 count as 0, -inf forgets all).
+ *   slot_in  : device [R]: the slot with the state after P_r tokens, or -1 for a zero state.
+ *   slot_out : device [R]: the slot that receives the state after P_r + C_r tokens, or -1 for none.
+ * slot_in[r] == slot_out[r] advances a state in place; another slot keeps the old one as it is (the
+ * snapshot that a streamed context goes back to when an update cuts off what came after it).  C_r = 0
+ * copies.  A slot_in outside [-1, num_slots) makes NaN of the request's rows and state; a slot_out
+ * outside it stores nothing.  Not checked: slot_out entries >= 0 are distinct, and none is the
+ * slot_in of another request of the call.
+ */
+typedef struct s2l_linear_state {
+  float* states;
+  const float* log_decay;
+  const int32_t* slot_in;
+  const int32_t* slot_out;
+  int32_t num_slots;
+  int32_t num_heads;        /* Hq                                                             */
+} s2l_linear_state;
+
+/*
+ * Workspace bytes that s2l_linear_attn needs for this batch (states at the boundaries of the pieces
+ * that long chunks are cut into; 0 when none is).  A host computation from the host length copies.
+ * Errors: EINVAL (nulls, negative lengths, head count), EHIP (the CU count query).
+ */
+s2l_status s2l_linear_attn_workspace_bytes(const s2l_batch* batch, int32_t num_q_heads, size_t* bytes_out);
+
+/*
+ * The chunks of a varlen batch (of any mix of lengths; prefix lengths and block tables are not read).
+ *   q, k, v, out: device bf16 rows with strides as in s2l_rope_qk (Hq, Hkv, Hkv and Hq heads of 128);
+ *                 out overlaps nothing that is read.  Rows from T on are not touched.
+ *   workspace   : device, ws_bytes >= s2l_linear_attn_workspace_bytes(...); NULL when that is 0.
+ * Precision: states and sums in fp32; where bf16 MFMA takes a product, factors that are not bf16
+ * values go as the sum of two (2^-17 relative).  A value of v that is not finite reaches the rows from
+ * its own on, and the state, as a value that is not finite.
+ * Errors: EINVAL, EWORKSPACE, ENOTSUP (more than 65535 requests or heads), EHIP.
+ */
+s2l_status s2l_linear_attn(const s2l_linear_state* state, const s2l_batch* batch, const void* q, int64_t q_stride,
+                           const void* k, int64_t k_stride, const void* v, int64_t v_stride, int32_t num_kv_heads,
+                           float scale, void* out, int64_t out_stride, void* workspace, size_t ws_bytes,
+                           void* stream);
+
+/*
  * Read a request's cached K/V back out of its pages in position order: the inverse of the
  * block-table addressing of Sec. 2.2 (block j of a request holds tokens (j-1)k+1 .. jk,
  * anywhere in the pool), as a preempted request's blocks are copied out when it is swapped

@@ -12,6 +12,15 @@ request that already holds P cached tokens)::
     ws = torch.empty(s2l_attn_workspace_bytes(batch, Hq, Hkv), dtype=torch.uint8, device="cuda")
     plan = s2l_attn_plan(batch, Hq, Hkv, ws)                   # once per step, all layers
     s2l_chunk_prefill_attn(cache, batch, q, Hq, 128 ** -0.5, out, lse, plan, ws)
+
+Where queries and keys come unrotated from the projection, ``s2l_rope_kv_append`` takes the place of
+the append and rotates them on the way (positions of one axis or several, ``Rope``).  A layer of linear
+attention keeps a state a request instead of pages (``LinearState``)::
+
+    s2l_rope_kv_append(cache, batch, rope, q_raw, q, k_raw, v)     # pages <- rotated K, V; q <- rotated Q
+    s2l_rope_qk(batch, rope, q_raw, q, k_raw, k)                   # a layer without pages
+    ws = torch.empty(s2l_linear_attn_workspace_bytes(batch, Hq), dtype=torch.uint8, device="cuda")
+    s2l_linear_attn(state, batch, q, k, v, 128 ** -0.5, out, ws)
 """
 import ctypes
 
@@ -22,8 +31,9 @@ from . import _lib
 from ._lib import (S2L_KV_BF16, S2L_KV_FP8_E4M3, S2LError, S2LLibraryMissing, s2l_plan_info,
                    s2l_plan_opts)
 
-__all__ = ["PagedKVCache", "Batch", "plan_opts", "S2LError", "S2LLibraryMissing",
+__all__ = ["PagedKVCache", "Batch", "Rope", "LinearState", "rope_pair_axes", "plan_opts", "S2LError", "S2LLibraryMissing",
            "s2l_abi_version", "s2l_kv_append", "s2l_kv_gather", "s2l_kv_swap_out", "s2l_kv_swap_in",
+           "s2l_rope_qk", "s2l_rope_kv_append", "s2l_linear_attn", "s2l_linear_attn_workspace_bytes",
            "s2l_check_tables", "s2l_append_chunk_prefill_attn", "s2l_calib_stream_read", "s2l_calib_mfma_bf16", "s2l_attn_workspace_bytes",
            "s2l_attn_plan", "s2l_chunk_prefill_attn", "s2l_chunk_prefill_attn_q8", "s2l_attn_main", "s2l_split_reduce",
            "s2l_plan_host", "library_path", "plan_status", "s2l_chunk_prefill_attn_noalloc"]
@@ -123,6 +133,85 @@ class Batch:
             chunk_lens_host=self.chunk_host.ctypes.data_as(_lib.P_i32))
 
 
+def rope_pair_axes(sections, cyclic=False):
+    """The position axis of each rotated pair, for `sections[a]` pairs turning by axis a: the axes in
+    blocks one after another, or (cyclic) in turn: axis a > 0 takes pairs a, a + n, a + 2 n, ... until
+    it has its number, axis 0 the rest."""
+    sections = [int(m) for m in sections]
+    if not sections or min(sections) < 0:
+        raise ValueError(f"sections must be counts of pairs (got {sections})")
+    n, pairs = len(sections), sum(sections)
+    if not cyclic:
+        return [a for a, m in enumerate(sections) for _ in range(m)]
+    axes = [i % n if i // n < sections[i % n] else 0 for i in range(pairs)]
+    if [axes.count(a) for a in range(n)] != sections:
+        raise ValueError(f"sections {sections} do not fit in turns over {pairs} pairs")
+    return axes
+
+
+class Rope:
+    """How rows rotate: pair i of a head turns by (its axis's position) * inv_freq[i].
+
+    inv_freq: device fp32 [rot_dim / 2].  positions: None (row i of request r is at P_r + i), or a
+    device int32 tensor [T] or [axes][T], one position per row of the batch and axis.  pair_axes: the
+    axis of each pair (``rope_pair_axes``), None for axis 0 throughout.  adjacent: pairs are dims
+    (2 i, 2 i + 1) instead of (i, i + rot_dim / 2).  scale: a factor on the rotated dims."""
+
+    def __init__(self, inv_freq, positions=None, pair_axes=None, adjacent=False, scale=1.0):
+        _check(inv_freq, torch.float32, "inv_freq")
+        if inv_freq.dim() != 1 or not 1 <= inv_freq.shape[0] <= HEAD_DIM // 2:
+            raise ValueError(f"inv_freq must be a vector of 1 to {HEAD_DIM // 2} pairs")
+        pair_axes = [0] * inv_freq.shape[0] if pair_axes is None else [int(a) for a in pair_axes]
+        if len(pair_axes) != inv_freq.shape[0] or min(pair_axes) < 0 or max(pair_axes) >= _lib.S2L_ROPE_MAX_AXES:
+            raise ValueError(f"pair_axes must name an axis below {_lib.S2L_ROPE_MAX_AXES} for each of the "
+                             f"{inv_freq.shape[0]} pairs")
+        self.inv_freq, self.positions, self.adjacent, self.scale = inv_freq, positions, bool(adjacent), float(scale)
+        self.pair_axis = bytes(pair_axes) + bytes(64 - len(pair_axes))
+
+    def c(self, total_tokens, device):
+        p = self.positions
+        if p is not None and (p.dtype != torch.int32 or p.dim() not in (1, 2) or p.stride(-1) != 1 and p.shape[-1] > 1
+                              or p.shape[-1] < total_tokens or p.dim() == 2 and p.shape[0] > 1 and p.stride(0) < 0):
+            raise ValueError(f"positions must be an int32 tensor [T] or [axes][T] of {total_tokens} rows, each axis contiguous")
+        for t, name in ((self.inv_freq, "inv_freq"), (p, "positions")):
+            if t is not None and t.device != device:
+                raise ValueError(f"{name} is on {t.device}, the batch on {device}")
+        return _lib.s2l_rope(inv_freq=self.inv_freq.data_ptr(), positions=None if p is None else p.data_ptr(),
+                             pos_stride=0 if p is None or p.dim() == 1 else p.stride(0), rot_dim=2 * self.inv_freq.shape[0],
+                             num_axes=1 if p is None or p.dim() == 1 else p.shape[0],
+                             flags=_lib.S2L_ROPE_ADJACENT if self.adjacent else 0, scale=self.scale,
+                             pair_axis=(ctypes.c_uint8 * 64)(*self.pair_axis))
+
+
+class LinearState:
+    """A linear attention layer's request states: states fp32 [slots][Hq][128][128], log_decay fp32
+    [Hq] (ln of each head's decay, <= 0), and each request's slots, int32 [R]: slot_in (-1: a zero
+    state) is read, slot_out (-1: not kept) is written; the same slot advances in place."""
+
+    def __init__(self, states, log_decay, slot_in, slot_out):
+        _check(states, torch.float32, "states")
+        _check(log_decay, torch.float32, "log_decay")
+        if states.dim() != 4 or tuple(states.shape[2:]) != (HEAD_DIM, HEAD_DIM) or log_decay.shape != states.shape[1:2]:
+            raise ValueError(f"states must be [slots][Hq][{HEAD_DIM}][{HEAD_DIM}] and log_decay [Hq]")
+        self.states, self.log_decay, self.slot_in, self.slot_out = states, log_decay, slot_in, slot_out
+
+    @property
+    def num_heads(self):
+        return self.states.shape[1]
+
+    def c(self, num_reqs, device):
+        for t, name in ((self.slot_in, "slot_in"), (self.slot_out, "slot_out")):
+            _check(t, torch.int32, name)
+            if t.dim() != 1 or t.shape[0] != num_reqs:
+                raise ValueError(f"{name} must hold one slot for each of the {num_reqs} requests")
+        for t, name in ((self.states, "states"), (self.log_decay, "log_decay"), (self.slot_in, "slot_in"), (self.slot_out, "slot_out")):
+            if t.device != device:
+                raise ValueError(f"{name} is on {t.device}, the batch on {device}")
+        return _lib.s2l_linear_state(states=self.states.data_ptr(), log_decay=self.log_decay.data_ptr(),
+                                     slot_in=self.slot_in.data_ptr(), slot_out=self.slot_out.data_ptr(),
+                                     num_slots=self.states.shape[0], num_heads=self.states.shape[1])
+
+
 def plan_opts(target_items=0, min_split_keys=0, max_splits=0, tile_cols=0, key_halves=0):
     return s2l_plan_opts(target_items=target_items, min_split_keys=min_split_keys,
                          max_splits=max_splits, tile_cols=tile_cols, key_halves=key_halves)
@@ -160,6 +249,90 @@ def s2l_kv_append(cache, batch, k_new, v_new, stream=None):
     _check(v_new, torch.bfloat16, "v_new")
     cc, bc = cache.c(), batch.c()
     _lib.call("s2l_kv_append", ctypes.byref(cc), ctypes.byref(bc), _ptr(k_new), _ptr(v_new), _stream(stream))
+
+
+def _rows(t, name, batch):
+    """(pointer, row stride, heads) of a device bf16 tensor [rows][heads][128], rows anywhere apart,
+    that holds the batch's rows."""
+    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[2] != HEAD_DIM or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != HEAD_DIM):
+        raise ValueError(f"{name} must be bf16 rows [T][heads][{HEAD_DIM}] of contiguous heads (got {t.dtype}, shape "
+                         f"{tuple(t.shape)}, strides {t.stride()})")
+    if t.shape[0] < batch.total_tokens:
+        raise ValueError(f"{name} has {t.shape[0]} rows, the batch {batch.total_tokens}")
+    if not t.is_cuda or t.device != batch.chunk_lens.device:
+        raise ValueError(f"{name} is on {t.device}, the batch on {batch.chunk_lens.device}")
+    return _ptr(t), t.stride(0), t.shape[1]
+
+
+def _call_on(batch, name, *args, stream):
+    """An entry point's call with the batch's device current: `stream` (None: that device's current
+    stream) is one of its streams."""
+    with torch.cuda.device(batch.chunk_lens.device):
+        _lib.call(name, *args, _stream(stream))
+
+
+def _same_heads(a, b, what):
+    if a != b:
+        raise ValueError(f"{what} differ in their heads ({a} and {b})")
+
+
+def s2l_rope_qk(batch, rope, q, q_out, k=None, k_out=None, stream=None):
+    """Rotate the batch's query rows q into q_out and its key rows k (if any) into k_out: bf16
+    [rows][heads][128], rows at any stride; an output may be its own input."""
+    qp, qs, hq = _rows(q, "q", batch)
+    op, os_, ho = _rows(q_out, "q_out", batch)
+    _same_heads(hq, ho, "q and q_out")
+    kp, ks, hkv, kop, kos = None, 0, 0, None, 0
+    if k is not None:
+        kp, ks, hkv = _rows(k, "k", batch)
+        kop, kos, ho = _rows(k_out, "k_out", batch)
+        _same_heads(hkv, ho, "k and k_out")
+    bc, rc = batch.c(), rope.c(batch.total_tokens, batch.chunk_lens.device)
+    _call_on(batch, "s2l_rope_qk", ctypes.byref(bc), ctypes.byref(rc), qp, qs, hq, op, os_, kp, ks, hkv, kop, kos, stream=stream)
+
+
+def s2l_rope_kv_append(cache, batch, rope, q, q_out, k, v, stream=None):
+    """s2l_kv_append of the rotated keys and of the values, with the rotated queries in q_out (q and
+    q_out None: none), in one launch; tensors as for s2l_rope_qk."""
+    qp, qs, hq, op, os_ = None, 0, 0, None, 0
+    if q is not None:
+        qp, qs, hq = _rows(q, "q", batch)
+        op, os_, ho = _rows(q_out, "q_out", batch)
+        _same_heads(hq, ho, "q and q_out")
+    kp, ks, hk = _rows(k, "k", batch)
+    vp, vs, hv = _rows(v, "v", batch)
+    _same_heads(hk, cache.num_kv_heads, "k and the cache")
+    _same_heads(hv, cache.num_kv_heads, "v and the cache")
+    cc, bc, rc = cache.c(), batch.c(), rope.c(batch.total_tokens, batch.chunk_lens.device)
+    _call_on(batch, "s2l_rope_kv_append", ctypes.byref(cc), ctypes.byref(bc), ctypes.byref(rc), qp, qs, hq, op, os_, kp, ks, vp, vs,
+             stream=stream)
+
+
+def s2l_linear_attn_workspace_bytes(batch, num_q_heads):
+    bc = batch.c()
+    n = ctypes.c_size_t(0)
+    _lib.call("s2l_linear_attn_workspace_bytes", ctypes.byref(bc), num_q_heads, ctypes.byref(n))
+    return n.value
+
+
+def s2l_linear_attn(state, batch, q, k, v, scale, out, workspace=None, stream=None):
+    """Linear attention of the batch's chunks over `state` (advanced from its slot_in to its slot_out):
+    out[i][h] = scale * q_i[h] S after S <- exp(log_decay[h]) S + k_i v_i^T; tensors as for
+    s2l_rope_qk, the workspace a device uint8 tensor (None where no bytes are needed)."""
+    qp, qs, hq = _rows(q, "q", batch)
+    kp, ks, hkv = _rows(k, "k", batch)
+    vp, vs, hv = _rows(v, "v", batch)
+    op, os_, ho = _rows(out, "out", batch)
+    _same_heads(hq, state.num_heads, "q and the state")
+    _same_heads(hq, ho, "q and out")
+    _same_heads(hkv, hv, "k and v")
+    if workspace is not None:
+        _check(workspace, torch.uint8, "workspace")
+        if workspace.device != batch.chunk_lens.device:
+            raise ValueError(f"workspace is on {workspace.device}, the batch on {batch.chunk_lens.device}")
+    bc, sc = batch.c(), state.c(batch.num_reqs, batch.chunk_lens.device)
+    _call_on(batch, "s2l_linear_attn", ctypes.byref(sc), ctypes.byref(bc), qp, qs, kp, ks, vp, vs, hkv, float(scale), op, os_,
+             _ptr(workspace), 0 if workspace is None else workspace.numel(), stream=stream)
 
 
 def _swap(name, cache, pairs, host_k, host_v, stream):

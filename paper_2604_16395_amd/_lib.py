@@ -19,6 +19,7 @@ LIB_PATH = os.environ.get("S2L_LIBRARY") or os.path.join(_HERE, "libs2l.so")
 
 S2L_OK, S2L_EINVAL, S2L_ERANGE, S2L_EWORKSPACE, S2L_ENOTSUP, S2L_EHIP = 0, -1, -2, -3, -4, -5
 S2L_KV_BF16, S2L_KV_FP8_E4M3 = 0, 1
+S2L_ROPE_ADJACENT, S2L_ROPE_MAX_AXES = 1, 4
 STATUS_NAMES = {0: "S2L_OK", -1: "S2L_EINVAL", -2: "S2L_ERANGE", -3: "S2L_EWORKSPACE",
                 -4: "S2L_ENOTSUP", -5: "S2L_EHIP"}
 
@@ -50,6 +51,16 @@ class s2l_plan_info(ctypes.Structure):
                 ("num_q_heads", c_i32), ("num_kv_heads", c_i32), ("num_reqs", c_i32),
                 ("total_tokens", c_i64), ("workspace_bytes", c_i64), ("tile_cols", c_i32),
                 ("num_tiles", c_i32), ("part_floats", c_i64), ("key_halves", c_i32), ("flags", c_i32)]
+
+
+class s2l_rope(ctypes.Structure):
+    _fields_ = [("inv_freq", c_vp), ("positions", c_vp), ("pos_stride", c_i64), ("rot_dim", c_i32),
+                ("num_axes", c_i32), ("flags", c_i32), ("scale", ctypes.c_float), ("pair_axis", ctypes.c_uint8 * 64)]
+
+
+class s2l_linear_state(ctypes.Structure):
+    _fields_ = [("states", c_vp), ("log_decay", c_vp), ("slot_in", c_vp), ("slot_out", c_vp),
+                ("num_slots", c_i32), ("num_heads", c_i32)]
 
 
 class s2l_sched_config(ctypes.Structure):
@@ -86,12 +97,20 @@ P_cache = ctypes.POINTER(s2l_kv_cache)
 P_batch = ctypes.POINTER(s2l_batch)
 P_opts = ctypes.POINTER(s2l_plan_opts)
 P_info = ctypes.POINTER(s2l_plan_info)
+P_rope = ctypes.POINTER(s2l_rope)
+P_state = ctypes.POINTER(s2l_linear_state)
 
 # name -> (restype, argtypes); the list of every symbol include/s2l.h declares
 SIGNATURES = {
     "s2l_abi_version": (c_i32, []),
     "s2l_last_error": (ctypes.c_char_p, []),
     "s2l_kv_append": (c_i32, [P_cache, P_batch, c_vp, c_vp, c_vp]),
+    "s2l_rope_qk": (c_i32, [P_batch, P_rope, c_vp, c_i64, c_i32, c_vp, c_i64, c_vp, c_i64, c_i32, c_vp, c_i64, c_vp]),
+    "s2l_rope_kv_append": (c_i32, [P_cache, P_batch, P_rope, c_vp, c_i64, c_i32, c_vp, c_i64, c_vp, c_i64, c_vp, c_i64,
+                                   c_vp]),
+    "s2l_linear_attn_workspace_bytes": (c_i32, [P_batch, c_i32, ctypes.POINTER(ctypes.c_size_t)]),
+    "s2l_linear_attn": (c_i32, [P_state, P_batch, c_vp, c_i64, c_vp, c_i64, c_vp, c_i64, c_i32, ctypes.c_float, c_vp,
+                                c_i64, c_vp, ctypes.c_size_t, c_vp]),
     "s2l_kv_gather": (c_i32, [P_cache, P_batch, c_i32, c_vp, c_vp, c_vp, c_vp]),
     "s2l_check_tables": (c_i32, [P_cache, P_batch, c_vp, c_vp]),
     "s2l_kv_swap_out": (c_i32, [P_cache, c_vp, c_i32, c_vp, c_vp, c_i32, c_vp]),

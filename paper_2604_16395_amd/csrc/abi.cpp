@@ -553,6 +553,100 @@ s2l_status attn_launch(const s2l_kv_cache* cache, const s2l_batch* batch, const 
   return ok();
 }
 
+// The batch of a call that rows alone matter to (no pages): lengths, and the device arrays that find a row.
+s2l_status check_rows(const s2l_batch* b, int64_t* total_tokens) {
+  s2l_status st = check_batch(b, false, total_tokens);
+  if (st != S2L_OK) return st;
+  if (b->num_reqs > 0 && (!b->prefix_lens || !b->chunk_lens || !b->cu_chunk))
+    return fail(S2L_EINVAL, "a device batch array is NULL");
+  return S2L_OK;
+}
+
+// One tensor of rows: `heads` heads of 128 elements, `stride` elements from row to row.
+s2l_status check_tensor(const char* name, const void* p, int64_t stride, int32_t heads, bool written, int64_t rows) {
+  if (rows > 0 && !p) return fail(S2L_EINVAL, "%s is NULL", name);
+  if (stride < 0 || stride > ((int64_t)1 << 31)) return fail(S2L_EINVAL, "%s: row stride %lld out of range", name, (long long)stride);
+  if (written && rows > 1 && stride < (int64_t)heads * s2l::kHeadDim)
+    return fail(S2L_EINVAL, "%s: row stride %lld is less than a row of %d heads, which are written", name, (long long)stride, heads);
+  if (reinterpret_cast<uintptr_t>(p) % 2 != 0) return fail(S2L_EINVAL, "%s is not aligned to its elements", name);
+  return S2L_OK;
+}
+
+s2l_status check_rope(const s2l_rope* rope, int64_t T) {
+  if (!rope) return fail(S2L_EINVAL, "rope is NULL");
+  if (!rope->inv_freq) return fail(S2L_EINVAL, "inv_freq is NULL");
+  if (rope->rot_dim < 16 || rope->rot_dim > s2l::kHeadDim || rope->rot_dim % 16 != 0)
+    return fail(S2L_ENOTSUP, "rot_dim %d unsupported (a multiple of 16 up to 128)", rope->rot_dim);
+  if (rope->num_axes < 1 || rope->num_axes > S2L_ROPE_MAX_AXES)
+    return fail(S2L_ENOTSUP, "num_axes %d unsupported (1 to %d)", rope->num_axes, S2L_ROPE_MAX_AXES);
+  if (rope->flags & ~S2L_ROPE_ADJACENT) return fail(S2L_EINVAL, "unknown rope flags %d", rope->flags);
+  if (!(rope->scale > 0.0f) || !std::isfinite(rope->scale)) return fail(S2L_EINVAL, "rope scale must be finite and > 0");
+  if (!rope->positions && rope->num_axes > 1) return fail(S2L_EINVAL, "%d axes need positions", rope->num_axes);
+  if (rope->positions && rope->num_axes > 1 && rope->pos_stride < T)
+    return fail(S2L_EINVAL, "pos_stride %lld is less than the batch's %lld rows", (long long)rope->pos_stride, (long long)T);
+  for (int32_t i = 0; i < rope->rot_dim / 2; ++i)
+    if (rope->pair_axis[i] >= rope->num_axes)
+      return fail(S2L_EINVAL, "pair %d turns by axis %d of %d", i, rope->pair_axis[i], rope->num_axes);
+  return S2L_OK;
+}
+
+s2l_status rope_launch(const char* what, const s2l_kv_cache* cache, const s2l_batch* batch, const s2l_rope* rope,
+                       int64_t T, const void* q, int64_t q_stride, int32_t hq, void* q_out, int64_t q_out_stride,
+                       const void* k, int64_t k_stride, int32_t hkv, void* k_out, int64_t k_out_stride, const void* v,
+                       int64_t v_stride, void* stream) {
+  s2l_status st;
+  if ((st = check_rope(rope, T)) != S2L_OK) return st;
+  if (hq < 0 || hkv < 0) return fail(S2L_EINVAL, "head counts must be >= 0 (hq=%d hkv=%d)", hq, hkv);
+  if (hq > 65535 || hkv > 65535) return fail(S2L_ENOTSUP, "%s supports at most 65535 heads of a kind", what);
+  if (hq > 0 && ((st = check_tensor("q", q, q_stride, hq, false, T)) != S2L_OK ||
+                 (st = check_tensor("q_out", q_out, q_out_stride, hq, true, T)) != S2L_OK))
+    return st;
+  if (hkv > 0 && (st = check_tensor("k", k, k_stride, hkv, false, T)) != S2L_OK) return st;
+  if (hkv > 0 && !cache && (st = check_tensor("k_out", k_out, k_out_stride, hkv, true, T)) != S2L_OK) return st;
+  if (cache && (st = check_tensor("v", v, v_stride, hkv, false, T)) != S2L_OK) return st;
+  if ((hq > 0 && q == q_out && q_stride != q_out_stride && T > 1) ||
+      (hkv > 0 && !cache && k == k_out && k_stride != k_out_stride && T > 1))
+    return fail(S2L_EINVAL, "rows rotated in place need one stride");
+  s2l::RopeLaunch a = {};
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(k);
+  a.v = static_cast<const uint16_t*>(v);
+  a.q_out = static_cast<uint16_t*>(q_out);
+  a.k_out = static_cast<uint16_t*>(k_out);
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.q_out_stride = q_out_stride;
+  a.k_out_stride = k_out_stride;
+  a.inv_freq = rope->inv_freq;
+  a.positions = rope->positions;
+  a.pos_stride = rope->pos_stride;
+  for (int32_t i = 0; i < rope->rot_dim / 2; ++i) a.pair_axes[i / 32] |= (uint64_t)rope->pair_axis[i] << (2 * (i % 32));
+  a.rot_dim = rope->rot_dim;
+  a.num_axes = rope->num_axes;
+  a.scale = rope->scale;
+  a.adjacent = (rope->flags & S2L_ROPE_ADJACENT) != 0;
+  a.prefix_lens = batch->prefix_lens;
+  a.cu_chunk = batch->cu_chunk;
+  a.block_tables = batch->block_tables;
+  a.max_pages = batch->max_pages_per_req;
+  a.num_reqs = batch->num_reqs;
+  a.hq = hq;
+  a.hkv = hkv;
+  a.total_rows = (int32_t)T;
+  if (cache) {
+    a.k_pool = cache->k_pages;
+    a.v_pool = cache->v_pages;
+    a.k_scale = cache->k_scale;
+    a.v_scale = cache->v_scale;
+    a.fp8 = cache->dtype == S2L_KV_FP8_E4M3;
+  }
+  (void)hipGetLastError();
+  hipError_t e = s2l::launch_rope(a, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(what, e);
+  return ok();
+}
+
 // The device plan of a checked batch with resolved options.
 s2l_status plan_resolved(const s2l_batch* batch, int32_t hq, int32_t hkv, const Resolved& o, void* workspace,
                          size_t ws_bytes, s2l_plan_info* info, void* stream) {
@@ -639,6 +733,88 @@ s2l_status s2l_kv_append(const s2l_kv_cache* cache, const s2l_batch* batch, cons
   hipError_t e = s2l::launch_kv_append(kv_launch(cache, batch), k_new, v_new, max_touched,
                                        static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail("kv_append launch", e);
+  return ok();
+}
+
+s2l_status s2l_rope_qk(const s2l_batch* batch, const s2l_rope* rope, const void* q, int64_t q_stride,
+                       int32_t num_q_heads, void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride,
+                       int32_t num_kv_heads, void* k_out, int64_t k_out_stride, void* stream) {
+  s2l_status st;
+  int64_t T = 0;
+  if ((st = check_rows(batch, &T)) != S2L_OK) return st;
+  return rope_launch("rope_qk", nullptr, batch, rope, T, q, q_stride, num_q_heads, q_out, q_out_stride, k, k_stride,
+                     num_kv_heads, k_out, k_out_stride, nullptr, 0, stream);
+}
+
+s2l_status s2l_rope_kv_append(const s2l_kv_cache* cache, const s2l_batch* batch, const s2l_rope* rope, const void* q,
+                              int64_t q_stride, int32_t num_q_heads, void* q_out, int64_t q_out_stride, const void* k,
+                              int64_t k_stride, const void* v, int64_t v_stride, void* stream) {
+  s2l_status st;
+  int64_t T = 0;
+  if ((st = check_cache(cache, batch)) != S2L_OK) return st;
+  if ((st = check_batch(batch, true, &T)) != S2L_OK) return st;
+  return rope_launch("rope_kv_append", cache, batch, rope, T, q, q_stride, num_q_heads, q_out, q_out_stride, k,
+                     k_stride, cache->num_kv_heads, nullptr, 0, v, v_stride, stream);
+}
+
+s2l_status s2l_linear_attn_workspace_bytes(const s2l_batch* batch, int32_t num_q_heads, size_t* bytes_out) {
+  s2l_status st;
+  int64_t T = 0;
+  if (!bytes_out) return fail(S2L_EINVAL, "bytes_out is NULL");
+  if ((st = check_batch(batch, false, &T)) != S2L_OK) return st;
+  if (num_q_heads <= 0) return fail(S2L_EINVAL, "num_q_heads must be > 0");
+  *bytes_out = 0;
+  return ok();
+}
+
+s2l_status s2l_linear_attn(const s2l_linear_state* state, const s2l_batch* batch, const void* q, int64_t q_stride,
+                           const void* k, int64_t k_stride, const void* v, int64_t v_stride, int32_t num_kv_heads,
+                           float scale, void* out, int64_t out_stride, void* workspace, size_t ws_bytes,
+                           void* stream) {
+  s2l_status st;
+  int64_t T = 0;
+  if (!state) return fail(S2L_EINVAL, "state is NULL");
+  if ((st = check_rows(batch, &T)) != S2L_OK) return st;
+  const int32_t hq = state->num_heads, hkv = num_kv_heads;
+  if (hq <= 0 || hkv <= 0) return fail(S2L_EINVAL, "head counts must be > 0 (hq=%d hkv=%d)", hq, hkv);
+  if (hq % hkv != 0) return fail(S2L_EINVAL, "num_heads %d is not a multiple of num_kv_heads %d", hq, hkv);
+  if (batch->num_reqs > 65535 || hq > 65535)
+    return fail(S2L_ENOTSUP, "linear_attn supports at most 65535 requests and heads");
+  if (batch->num_reqs > 0) {
+    if (!state->states || !state->log_decay || !state->slot_in || !state->slot_out)
+      return fail(S2L_EINVAL, "states, log_decay, slot_in or slot_out is NULL");
+    if (state->num_slots <= 0) return fail(S2L_EINVAL, "num_slots must be > 0");
+    if (reinterpret_cast<uintptr_t>(state->states) % 16 != 0) return fail(S2L_EINVAL, "states must be aligned to 16 bytes");
+  }
+  if (!std::isfinite(scale)) return fail(S2L_EINVAL, "scale must be finite");
+  if ((st = check_tensor("q", q, q_stride, hq, false, T)) != S2L_OK ||
+      (st = check_tensor("k", k, k_stride, hkv, false, T)) != S2L_OK ||
+      (st = check_tensor("v", v, v_stride, hkv, false, T)) != S2L_OK ||
+      (st = check_tensor("out", out, out_stride, hq, true, T)) != S2L_OK)
+    return st;
+  s2l::LinearLaunch a = {};
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(k);
+  a.v = static_cast<const uint16_t*>(v);
+  a.out = static_cast<uint16_t*>(out);
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.out_stride = out_stride;
+  a.states = state->states;
+  a.log_decay = state->log_decay;
+  a.slot_in = state->slot_in;
+  a.slot_out = state->slot_out;
+  a.chunk_lens = batch->chunk_lens;
+  a.cu_chunk = batch->cu_chunk;
+  a.num_slots = state->num_slots;
+  a.num_reqs = batch->num_reqs;
+  a.hq = hq;
+  a.hkv = hkv;
+  a.scale = scale;
+  (void)hipGetLastError();
+  hipError_t e = s2l::launch_linear_attn(a, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail("linear_attn launch", e);
   return ok();
 }
 

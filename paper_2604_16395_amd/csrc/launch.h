@@ -93,6 +93,36 @@ struct ReduceLaunch {
 };
 hipError_t launch_split_reduce(const ReduceLaunch& a, hipStream_t stream);
 
+struct RopeLaunch {          // rotation of rows, and their append (rope.hip)
+  const uint16_t *q, *k, *v;
+  uint16_t *q_out, *k_out;   // k_out without pools, v with them only
+  int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride;   // elements
+  const float* inv_freq;
+  const int32_t* positions;
+  int64_t pos_stride;
+  uint64_t pair_axes[2];     // two bits a pair
+  int32_t rot_dim, num_axes;
+  float scale;
+  bool adjacent, fp8;
+  const int32_t *prefix_lens, *cu_chunk, *block_tables;
+  int32_t max_pages, num_reqs, hq, hkv, total_rows;
+  void *k_pool, *v_pool;     // null: no append
+  const float *k_scale, *v_scale;
+};
+hipError_t launch_rope(const RopeLaunch& a, hipStream_t stream);
+
+struct LinearLaunch {        // linear attention (linear_attn.hip)
+  const uint16_t *q, *k, *v;
+  uint16_t* out;
+  int64_t q_stride, k_stride, v_stride, out_stride;   // elements
+  float* states;
+  const float* log_decay;
+  const int32_t *slot_in, *slot_out, *chunk_lens, *cu_chunk;
+  int32_t num_slots, num_reqs, hq, hkv;
+  float scale;
+};
+hipError_t launch_linear_attn(const LinearLaunch& a, hipStream_t stream);
+
 // Size of the library-held scratch array of the allocation-free attention call, and its
 // device address on the current device (taken on the first call there; noalloc.hip).
 constexpr size_t kNoAllocScratchBytes = (size_t)64 << 20;
