@@ -265,8 +265,8 @@ s2l_status s2l_linear_attn_workspace_bytes(const s2l_batch* batch, int32_t num_q
  *   q, k, v, out: device bf16 rows with strides as in s2l_rope_qk (Hq, Hkv, Hkv and Hq heads of 128);
  *                 out overlaps nothing that is read.  Rows from T on are not touched.
  *   workspace   : device, ws_bytes >= s2l_linear_attn_workspace_bytes(...); NULL when that is 0.
- * Precision: states and sums in fp32; where bf16 MFMA takes a product, factors that are not bf16
- * values go as the sum of two (2^-17 relative).  A value of v that is not finite reaches the rows from
+ * Precision: states and sums in fp32; where the bf16 MFMA takes a product, factors that are not bf16
+ * values go as the sum of two of them (2^-16 relative) for outputs, of three for states.  A value of v that is not finite reaches the rows from
  * its own on, and the state, as a value that is not finite.
  * Errors: EINVAL, EWORKSPACE, ENOTSUP (more than 65535 requests or heads), EHIP.
  */

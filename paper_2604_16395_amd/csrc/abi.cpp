@@ -52,6 +52,15 @@ s2l_status hip_fail(const char* what, hipError_t e) {
   return fail(S2L_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
 
+s2l_status query_cus(int32_t* num_cus) {
+  int dev = 0, n = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e == hipSuccess) e = hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev);
+  if (e != hipSuccess) return hip_fail("querying the CU count", e);
+  *num_cus = n;
+  return S2L_OK;
+}
+
 struct Resolved {
   int32_t target_items, min_split_keys, max_splits, tile_cols, key_halves;
   int32_t whole_keys;       // a batch whose key ranges are all of at most so many keys is not split
@@ -258,11 +267,8 @@ s2l_status resolve_opts(const s2l_plan_opts* o, bool need_cus, int32_t num_cus, 
   r->key_halves = kh != 0 ? kh : (r->tile_cols == s2l::kMinTileCols ? 2 : 1);
   if (t == 0) {
     if (num_cus <= 0 && need_cus) {
-      int dev = 0, n = 0;
-      hipError_t e = hipGetDevice(&dev);
-      if (e == hipSuccess) e = hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev);
-      if (e != hipSuccess) return hip_fail("querying the CU count", e);
-      num_cus = n;
+      const s2l_status st = query_cus(&num_cus);
+      if (st != S2L_OK) return st;
     }
     if (num_cus <= 0) return fail(S2L_EINVAL, "num_cus must be > 0 when target_items is 0");
     t = s2l::items_per_cu(r->tile_cols, r->key_halves) * num_cus;
@@ -590,6 +596,34 @@ s2l_status check_rope(const s2l_rope* rope, int64_t T) {
   return S2L_OK;
 }
 
+// How linear attention cuts the batch: pieces that give each CU its two workgroups.
+s2l::LinearPlan linear_plan(const s2l_batch* b, int32_t hq, int32_t num_cus) {
+  s2l::LinearPlan p = {};
+  int64_t blocks = 0, longest = 0;
+  for (int32_t r = 0; r < b->num_reqs; ++r) {
+    const int32_t c = b->chunk_lens_host[r];
+    if (c <= s2l::kLinearShortTokens) continue;
+    blocks += s2l::ceil_div64(c, s2l::kLinearBlockTokens);
+    longest = std::max<int64_t>(longest, c);
+  }
+  const int64_t wanted = std::max<int64_t>(4, s2l::ceil_div64(blocks * hq, 2 * (int64_t)num_cus));
+  p.piece_tokens = (int32_t)(wanted * s2l::kLinearBlockTokens);
+  for (int32_t r = 0; r < b->num_reqs; ++r) {
+    const int32_t c = b->chunk_lens_host[r];
+    if (c <= s2l::kLinearShortTokens) {
+      ++p.short_reqs;
+      continue;
+    }
+    const int32_t n = (int32_t)s2l::ceil_div64(c, p.piece_tokens);
+    p.pieces += n;
+    if (n > 1) ++p.cut_reqs, p.ws_states += n;
+  }
+  return p;
+}
+size_t linear_bytes(const s2l::LinearPlan& p, int32_t hq) {
+  return (size_t)p.ws_states * hq * s2l::kHeadDim * s2l::kHeadDim * sizeof(float);
+}
+
 s2l_status rope_launch(const char* what, const s2l_kv_cache* cache, const s2l_batch* batch, const s2l_rope* rope,
                        int64_t T, const void* q, int64_t q_stride, int32_t hq, void* q_out, int64_t q_out_stride,
                        const void* k, int64_t k_stride, int32_t hkv, void* k_out, int64_t k_out_stride, const void* v,
@@ -763,7 +797,9 @@ s2l_status s2l_linear_attn_workspace_bytes(const s2l_batch* batch, int32_t num_q
   if (!bytes_out) return fail(S2L_EINVAL, "bytes_out is NULL");
   if ((st = check_batch(batch, false, &T)) != S2L_OK) return st;
   if (num_q_heads <= 0) return fail(S2L_EINVAL, "num_q_heads must be > 0");
-  *bytes_out = 0;
+  int32_t cus;
+  if ((st = query_cus(&cus)) != S2L_OK) return st;
+  *bytes_out = linear_bytes(linear_plan(batch, num_q_heads, cus), num_q_heads);
   return ok();
 }
 
@@ -792,7 +828,16 @@ s2l_status s2l_linear_attn(const s2l_linear_state* state, const s2l_batch* batch
       (st = check_tensor("v", v, v_stride, hkv, false, T)) != S2L_OK ||
       (st = check_tensor("out", out, out_stride, hq, true, T)) != S2L_OK)
     return st;
+  int32_t cus;
+  if ((st = query_cus(&cus)) != S2L_OK) return st;
+  const s2l::LinearPlan plan = linear_plan(batch, hq, cus);
+  if (const size_t need = linear_bytes(plan, hq); need > 0) {
+    if (!workspace) return fail(S2L_EWORKSPACE, "workspace is NULL");
+    if (ws_bytes < need) return fail(S2L_EWORKSPACE, "workspace %zu bytes < %zu needed", ws_bytes, need);
+    if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return fail(S2L_EINVAL, "workspace must be aligned to 16 bytes");
+  }
   s2l::LinearLaunch a = {};
+  a.ws = static_cast<float*>(workspace);
   a.q = static_cast<const uint16_t*>(q);
   a.k = static_cast<const uint16_t*>(k);
   a.v = static_cast<const uint16_t*>(v);
@@ -813,7 +858,7 @@ s2l_status s2l_linear_attn(const s2l_linear_state* state, const s2l_batch* batch
   a.hkv = hkv;
   a.scale = scale;
   (void)hipGetLastError();
-  hipError_t e = s2l::launch_linear_attn(a, static_cast<hipStream_t>(stream));
+  hipError_t e = s2l::launch_linear_attn(a, plan, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail("linear_attn launch", e);
   return ok();
 }

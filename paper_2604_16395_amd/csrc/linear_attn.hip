@@ -2,10 +2,26 @@
 //
 //   S <- l S + k_i v_i^T,   out_i = scale * q_i S      (S [128 k][128 v] in fp32, l = exp(log_decay))
 //
-// Recurrent form: a workgroup takes 32 columns of one (request, head) state.  Thread (kg, vq) keeps rows
-// 4 kg .. + 3 and columns 4 vq .. + 3 of them in registers over the request's tokens, so the state is
-// read and written once, whatever the chunk's length; a row's part of q S is summed over the eight row
-// groups of a wave by lane swaps and over the four waves through LDS, 16 tokens at a time.
+// Requests of up to kShortTokens new tokens take the recurrent form: a workgroup takes 32 columns of one
+// (request, head) state.  Thread (kg, vq) keeps rows 4 kg .. + 3 and columns 4 vq .. + 3 of them in
+// registers over the request's tokens, so the state is read and written once; a row's part of q S is
+// summed over the eight row groups of a wave by lane swaps and over the four waves through LDS.
+//
+// Longer chunks take the blocked form, 32 tokens at a time: with n of them valid (zero rows behind),
+//   out_i = scale (sum_{j <= i} l^(i-j) (q_i . k_j) v_j + l^(i+1) q_i S),
+//   S'    = l^n S + sum_j k_j (l^(n-1-j) v_j)^T,
+// all products on v_mfma_f32_32x32x16_bf16.  A workgroup of four waves takes one head of one piece of a
+// request; wave w owns columns 32 w .. + 31 of S (64 accumulators a lane) and of the output, and every
+// wave forms the block's 32 x 32 scores itself, so waves share nothing but the Q, K and V tiles.
+//   * Scores come out transposed (A = K rows, B = Q rows), so that each lane holds one query i and the
+//     keys j = 8 b + 4 half + a, the order in which the transposing LDS read (ds_read_b64_tr_b16) hands
+//     out V's and K's columns: P is an operand of the next product as it stands.
+//   * Accumulator row 16 s + 8 b + 4 half + a of a state tile holds key dim 16 s + 8 half + 4 b + a of it
+//     (the K columns are read in that order), so that S^T is an operand against Q's rows as they lie.
+//   * Factors that are no bf16 values are sums of bf16 terms: P and S (for the output, bf16 in the end)
+//     two, off by 2^-17; l^(n-1-j) v (for the state, fp32) three, exact to 2^-25.
+// A piece of a chunk needs the state before it.  Chunks that are cut take three launches: the pieces' own
+// states, each in its slot of the workspace; their running sum under the decay; then the blocks.
 #include "launch.h"
 #include "s2l_device.h"
 
@@ -13,27 +29,80 @@ namespace s2l {
 
 namespace {
 
-typedef u32x2 __attribute__((aligned(2))) u32x2_any;
+typedef u32x2 __attribute__((aligned(2))) u32x2_any;   // at any element's address (the hardware takes
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;   // unaligned vectors)
 constexpr int kState = 128 * 128;    // elements of one state
-constexpr int kSliceCols = 32;       // columns of a recurrent workgroup
-constexpr int kTokens = 16;          // tokens between two sums over the waves
 
 // ln of the decay: at most 0, and finite, so that 0 tokens of it are a factor 1 (-1e4 forgets all: 0 in fp32).
 __device__ inline double clean_log(float g) {
   return g > 0.f ? 0.0 : g < -1e4f ? -1e4 : (double)g;
 }
+// l^n, the exponent in 64 bits so that far tokens lose nothing but the last rounding.
+__device__ inline float power(double log2_decay, int n) { return __builtin_amdgcn_exp2f((float)(log2_decay * n)); }
+
+// Piece `seg` of request `req`: what a workgroup works on.
+struct Piece {
+  int32_t req, seg, len;        // len: the request's tokens
+  int32_t ws;                   // workspace index of the request's first piece
+};
+
+// Inclusive sum over the lanes of a wave.
+__device__ inline int32_t wave_scan(int32_t x) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int32_t y = __shfl_up(x, d, 64);
+    x += lane >= d ? y : 0;
+  }
+  return x;
+}
+
+// The idx-th of the batch's units, 64 requests at a time.  Units are the short requests (kShort), or the
+// pieces of the others: all, or (kInner) all but each cut request's last.
+enum Units { kShort, kPieces, kInner };
+template <Units kUnits>
+__device__ inline Piece find_unit(const LinearLaunch& a, int32_t idx) {
+  const int lane = threadIdx.x & 63;
+  int32_t ws = 0;
+  for (int32_t r0 = 0; r0 < a.num_reqs; r0 += 64) {
+    const int32_t len = r0 + lane < a.num_reqs ? a.chunk_lens[r0 + lane] : -1;
+    const int32_t pieces = len > kLinearShortTokens ? (len + a.piece_tokens - 1) / a.piece_tokens : 0;
+    const int32_t cut = pieces > 1 ? pieces : 0;
+    const int32_t mine = kUnits == kShort ? (len >= 0 && len <= kLinearShortTokens) : kUnits == kPieces ? pieces : cut ? cut - 1 : 0;
+    const int32_t sum = wave_scan(mine), ws_sum = kUnits == kShort ? 0 : wave_scan(cut);
+    const int32_t total = __builtin_amdgcn_readlane(sum, 63);
+    if (idx < total) {
+      const int32_t c = __popcll(__ballot(sum <= idx));
+      Piece p;
+      p.req = r0 + c;
+      p.len = __builtin_amdgcn_readlane(len, c);
+      p.seg = idx - (__builtin_amdgcn_readlane(sum, c) - __builtin_amdgcn_readlane(mine, c));
+      p.ws = ws + __builtin_amdgcn_readlane(ws_sum, c) - __builtin_amdgcn_readlane(cut, c);
+      return p;
+    }
+    idx -= total;
+    ws += __builtin_amdgcn_readlane(ws_sum, 63);
+  }
+  return Piece{-1, 0, 0, 0};   // the device lengths hold less than the host copies: nothing to do
+}
+
+// ---- recurrent form ----
+
+constexpr int kSliceCols = 32;       // columns of a recurrent workgroup
+static_assert(kLinearShortTokens <= 16, "partial sums of all tokens in LDS");
 
 __device__ inline f32x4 unpack4(const u32x2& x) { return f32x4{bf16lo(x[0]), bf16hi(x[0]), bf16lo(x[1]), bf16hi(x[1])}; }
-
 __device__ inline f32x4 load4(const uint16_t* p) {
   const u32x2 x = *reinterpret_cast<const u32x2_any*>(p);
   return unpack4(x);
 }
 
 __global__ __launch_bounds__(256) void linear_recurrent_kernel(LinearLaunch a) {
-  __shared__ float s_part[kTokens][4][kSliceCols];
-  const int r = blockIdx.z, h = blockIdx.y, col0 = (int)blockIdx.x * kSliceCols;
-  const int C = a.chunk_lens[r], si = a.slot_in[r], so = a.slot_out[r];
+  __shared__ float s_part[kLinearShortTokens][4][kSliceCols];
+  const Piece p = find_unit<kShort>(a, blockIdx.z);
+  if (p.req < 0) return;
+  const int r = p.req, h = blockIdx.y, col0 = (int)blockIdx.x * kSliceCols;
+  const int C = p.len, si = a.slot_in[r], so = a.slot_out[r];
   const int64_t row0 = a.cu_chunk[r];
   const int g = h / (a.hq / a.hkv);
   const int vq = threadIdx.x & 7, kg = threadIdx.x >> 3, wave = threadIdx.x >> 6;
@@ -48,49 +117,372 @@ __global__ __launch_bounds__(256) void linear_recurrent_kernel(LinearLaunch a) {
   }
   const float decay = (float)exp(clean_log(a.log_decay[h]));
 
-  for (int t0 = 0; t0 < C; t0 += kTokens) {
-    const int n = C - t0 < kTokens ? C - t0 : kTokens;
-    for (int t = 0; t < n; ++t) {
-      const int64_t row = row0 + t0 + t;
-      const f32x4 k = load4(a.k + row * a.k_stride + g * 128 + 4 * kg);
-      const f32x4 v = load4(a.v + row * a.v_stride + g * 128 + col0 + 4 * vq);
-      const f32x4 q = load4(a.q + row * a.q_stride + h * 128 + 4 * kg);
-      f32x4 o{};
+  for (int t = 0; t < C; ++t) {
+    const int64_t row = row0 + t;
+    const f32x4 k = load4(a.k + row * a.k_stride + g * 128 + 4 * kg);
+    const f32x4 v = load4(a.v + row * a.v_stride + g * 128 + col0 + 4 * vq);
+    const f32x4 q = load4(a.q + row * a.q_stride + h * 128 + 4 * kg);
+    f32x4 o{};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          s[j][c] = __builtin_fmaf(s[j][c], decay, k[j] * v[c]);
-          o[c] = __builtin_fmaf(q[j], s[j][c], o[c]);
-        }
-      }
+    for (int j = 0; j < 4; ++j) {
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        o[c] += __shfl_xor(o[c], 8, 64);
-        o[c] += __shfl_xor(o[c], 16, 64);
-        o[c] += __shfl_xor(o[c], 32, 64);
+        s[j][c] = __builtin_fmaf(s[j][c], decay, k[j] * v[c]);
+        o[c] = __builtin_fmaf(q[j], s[j][c], o[c]);
       }
-      if ((threadIdx.x & 63) < 8) *reinterpret_cast<f32x4*>(&s_part[t][wave][4 * vq]) = o;
     }
-    __syncthreads();
-    for (int u = threadIdx.x; u < n * kSliceCols; u += 256) {
-      const int t = u / kSliceCols, c = u % kSliceCols;
-      const float o = s_part[t][0][c] + s_part[t][1][c] + s_part[t][2][c] + s_part[t][3][c];
-      a.out[(row0 + t0 + t) * a.out_stride + h * 128 + col0 + c] = (uint16_t)pack_bf16x2(a.scale * o, 0.f);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      o[c] += __shfl_xor(o[c], 8, 64);
+      o[c] += __shfl_xor(o[c], 16, 64);
+      o[c] += __shfl_xor(o[c], 32, 64);
     }
-    __syncthreads();
+    if ((threadIdx.x & 63) < 8) *reinterpret_cast<f32x4*>(&s_part[t][wave][4 * vq]) = o;
   }
   if (so >= 0 && so < a.num_slots) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4*>(a.states + so * slot + at + j * 128) = s[j];
   }
+  __syncthreads();
+  for (int u = threadIdx.x; u < C * kSliceCols; u += 256) {
+    const int t = u / kSliceCols, c = u % kSliceCols;
+    const float o = s_part[t][0][c] + s_part[t][1][c] + s_part[t][2][c] + s_part[t][3][c];
+    a.out[(row0 + t) * a.out_stride + h * 128 + col0 + c] = (uint16_t)pack_bf16x2(a.scale * o, 0.f);
+  }
+}
+
+// ---- blocked form ----
+
+constexpr int kB = kLinearBlockTokens;
+static_assert(kB == 32, "a block is one MFMA tile of tokens");
+constexpr int kRow = 256;                // bytes of a row of a tile in LDS
+constexpr int kTile = kB * kRow;
+// Rows lie with their 16-byte chunks permuted, chunk c of row r at c ^ perm(r): 16 consecutive rows put one
+// chunk on 16 places (reads of one chunk of many rows), four consecutive rows put four chunks into four
+// different quarters (transposing reads of four rows by four chunks).
+__device__ inline int perm(int row) { return (row & 3) << 2 | ((row >> 2) & 3); }
+
+typedef short v4i16 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
+
+// Columns of 4 + 4 rows of a tile (the rows 8 apart), as an operand: addresses of the two reads.
+__device__ inline bf16x8 read_columns(const uint8_t* x, const uint8_t* y) {
+  const v4i16 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)x);
+  const v4i16 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)y);
+  const u32x2 a = __builtin_bit_cast(u32x2, u), b = __builtin_bit_cast(u32x2, v);
+  return __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
+}
+__device__ inline bf16x8 read_row(const uint8_t* p) { return *reinterpret_cast<const bf16x8*>(p); }
+
+__device__ inline f32x16 mfma(const bf16x8& a, const bf16x8& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+// x as a sum of kTerms bf16 vectors, each the rounding of what the ones before leave.
+template <int kTerms>
+struct Terms {
+  bf16x8 t[kTerms];
+};
+template <int kTerms>
+__device__ inline Terms<kTerms> split(float* x) {
+  Terms<kTerms> r;
+#pragma unroll
+  for (int i = 0; i < kTerms; ++i) {
+    u32x4 w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      w[j] = pack_bf16x2(x[2 * j], x[2 * j + 1]);
+      if (i + 1 < kTerms) {
+        x[2 * j] -= bf16lo(w[j]);
+        x[2 * j + 1] -= bf16hi(w[j]);
+      }
+    }
+    r.t[i] = __builtin_bit_cast(bf16x8, w);
+  }
+  return r;
+}
+
+// kOutputs: the blocks of all pieces, with outputs and, of a request's last piece, its state.
+// Otherwise the own states of all pieces but the last, and (piece 0) a copy of the request's state.
+template <bool kOutputs>
+__global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
+  constexpr int kTiles = kOutputs ? 3 : 2;   // K, V, Q
+  __shared__ __attribute__((aligned(16))) uint8_t s_tile[2][kTiles][kTile];
+  __shared__ int32_t s_bad[4][32];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int half = lane >> 5, n = lane & 31;
+  const int group = a.hq / a.hkv;
+  // workgroups of one key head's queries follow one another on one XCD, which then reads K and V once
+  const int unit = (int)(blockIdx.x / (8 * group)) * 8 + (int)(blockIdx.x % 8);
+  const int h0 = (int)(blockIdx.x / 8) % group;
+  if (unit >= a.num_units * a.hkv) return;
+  const int g = unit % a.hkv, h = g * group + h0;
+  const Piece p = find_unit<kOutputs ? kPieces : kInner>(a, unit / a.hkv);
+  if (p.req < 0) return;
+  const int pieces = (p.len + a.piece_tokens - 1) / a.piece_tokens;
+  const int first = p.seg * a.piece_tokens, len = min(a.piece_tokens, p.len - first);
+  const bool last = p.seg == pieces - 1;
+  if (pieces > 1 && p.ws + pieces > a.ws_states) return;   // as above: more than the host copies hold
+  const int64_t row0 = (int64_t)a.cu_chunk[p.req] + first;
+  const int si = a.slot_in[p.req], so = a.slot_out[p.req];
+  const int64_t slot = (int64_t)a.hq * kState;
+  float* const ws = a.ws + ((int64_t)p.ws + p.seg) * slot + (int64_t)h * kState;
+
+  // staging: this wave's rows 8 wave + 4 d + (lane / 16) of each tile, 16 bytes a lane
+  const int srow = 8 * wave + (lane >> 4), schunk = lane & 15;
+  const uint16_t* kp = a.k + (row0 + srow) * a.k_stride + g * 128 + 8 * schunk;
+  const uint16_t* vp = a.v + (row0 + srow) * a.v_stride + g * 128 + 8 * schunk;
+  const uint16_t* qp = kOutputs ? a.q + (row0 + srow) * a.q_stride + h * 128 + 8 * schunk : nullptr;
+  u32x4 st[kTiles][2];
+  auto load = [&](int t0) {    // the block at token t0; rows past the piece are zero
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+      const bool in = t0 + srow + 4 * d < len;
+      st[0][d] = in ? (u32x4)*reinterpret_cast<const u32x4_any*>(kp + (int64_t)(t0 + 4 * d) * a.k_stride) : u32x4{};
+      st[1][d] = in ? (u32x4)*reinterpret_cast<const u32x4_any*>(vp + (int64_t)(t0 + 4 * d) * a.v_stride) : u32x4{};
+      if constexpr (kOutputs)
+        st[2][d] = in ? (u32x4)*reinterpret_cast<const u32x4_any*>(qp + (int64_t)(t0 + 4 * d) * a.q_stride) : u32x4{};
+    }
+  };
+  auto store = [&](int buf) {
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+      const int row = srow + 4 * d, at = row * kRow + ((schunk ^ perm(row)) << 4);
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) *reinterpret_cast<u32x4*>(&s_tile[buf][t][at]) = st[t][d];
+    }
+  };
+  load(0);
+
+  // operand addresses within a tile
+  int rows[8];                // row n, dims 16 s + 8 half .. + 7
+#pragma unroll
+  for (int s = 0; s < 8; ++s) rows[s] = n * kRow + (((2 * s + half) ^ perm(n)) << 4);
+  const int j = lane & 15, b4 = (lane >> 4) & 1, trow = 4 * half + (j >> 2);
+  int kcol[4][2], vcol[2];    // [state tile][rows + 0, + 8]
+#pragma unroll
+  for (int y = 0; y < 2; ++y) {
+    const int row = trow + 8 * y;
+#pragma unroll
+    for (int m = 0; m < 4; ++m) kcol[m][y] = row * kRow + (((4 * m + 2 * b4 + (j & 1)) ^ perm(row)) << 4) + 8 * ((j >> 1) & 1);
+    vcol[y] = row * kRow + (((4 * wave + 2 * b4 + ((j >> 1) & 1)) ^ perm(row)) << 4) + 8 * (j & 1);
+  }
+
+  // state: register (m, i) is key dim 32 m + dim(i), column 32 wave + n
+  auto dim = [&](int i) { return 16 * (i >> 3) + 8 * half + 4 * ((i >> 2) & 1) + (i & 3); };
+  f32x16 S[4];
+  const float* from = !kOutputs ? (p.seg == 0 && si >= 0 && si < a.num_slots ? a.states + si * slot + (int64_t)h * kState : nullptr)
+                      : pieces > 1 ? ws
+                                   : (si >= 0 && si < a.num_slots ? a.states + si * slot + (int64_t)h * kState : nullptr);
+  const float none = (!kOutputs && p.seg > 0) || (kOutputs && pieces > 1) || si == -1 ? 0.f : __builtin_nanf("");
+#pragma unroll
+  for (int m = 0; m < 4; ++m)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) S[m][i] = from ? from[(32 * m + dim(i)) * 128 + 32 * wave + n] : none;
+  if (!kOutputs && p.seg == 0) {   // the state before piece 0 stays: the request may advance in place
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) ws[(32 * m + dim(i)) * 128 + 32 * wave + n] = S[m][i];
+  }
+
+  const double log_decay = clean_log(a.log_decay[h]), log2_decay = log_decay * 1.4426950408889634;
+  const double block_d = exp(log_decay * kB);
+  const float block_hi = (float)block_d, block_lo = (float)(block_d - (double)block_hi);
+  float within[16], fade[16];   // l^(i-j), 0 above the diagonal; l^(kB-1-j)
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int key = 16 * (i >> 3) + 8 * ((i >> 2) & 1) + 4 * half + (i & 3);
+    within[i] = n >= key ? power(log2_decay, n - key) : 0.f;
+    fade[i] = power(log2_decay, kB - 1 - key);
+  }
+  const float since = power(log2_decay, n + 1);
+
+  store(0);
+  if (kB < len) load(kB);
+  __syncthreads();
+  for (int t0 = 0, buf = 0; t0 < len; t0 += kB, buf ^= 1) {
+    const int valid = min(kB, len - t0);
+    const uint8_t* kt = s_tile[buf][0];
+    const uint8_t* vt = s_tile[buf][1];
+    const bf16x8 v0 = read_columns(vt + vcol[0], vt + vcol[1]);
+    const bf16x8 v1 = read_columns(vt + vcol[0] + 16 * kRow, vt + vcol[1] + 16 * kRow);
+    u32x4 vw[2] = {__builtin_bit_cast(u32x4, v0), __builtin_bit_cast(u32x4, v1)};
+
+    if constexpr (kOutputs) {
+      const uint8_t* qt = s_tile[buf][2];
+      f32x16 p16{}, o{};
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        const bf16x8 q = read_row(qt + rows[s]);
+        p16 = mfma(read_row(kt + rows[s]), q, p16);
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = S[s >> 1][8 * (s & 1) + i];
+        const Terms<2> st2 = split<2>(x);
+        o = mfma(st2.t[1], q, o);
+        o = mfma(st2.t[0], q, o);
+      }
+      // A value of v that is not finite is no matter of the rows before it: 0 in their sums, and NaN put
+      // into the rows from its own on.
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t w = vw[i >> 2][i & 3] & 0x7FFF7FFFu;
+        top = max(top, max(w & 0xFFFFu, w >> 16));
+      }
+      const bool bad = __ballot(top >= 0x7F80u) != 0;
+      if (bad) {
+        int at = kB;
+#pragma unroll
+        for (int i = 15; i >= 0; --i) {
+          const uint32_t w = vw[i >> 3][(i >> 1) & 3];
+          const uint32_t bits = i & 1 ? w >> 16 : w & 0xFFFFu;
+          if ((bits & 0x7F80u) == 0x7F80u) {
+            at = min(at, 16 * (i >> 3) + 8 * ((i >> 2) & 1) + 4 * half + (i & 3));
+            vw[i >> 3][(i >> 1) & 3] = w & (i & 1 ? 0x0000FFFFu : 0xFFFF0000u);
+          }
+        }
+        at = min(at, __shfl_xor(at, 32, 64));
+        if (half == 0) s_bad[wave][n] = at;
+        __builtin_amdgcn_wave_barrier();
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[i] *= since;
+#pragma unroll
+      for (int k2 = 0; k2 < 2; ++k2) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = within[8 * k2 + i] == 0.f ? 0.f : p16[8 * k2 + i] * within[8 * k2 + i];
+        const Terms<2> pt = split<2>(x);
+        const bf16x8 vv = __builtin_bit_cast(bf16x8, vw[k2]);
+        o = mfma(vv, pt.t[1], o);
+        o = mfma(vv, pt.t[0], o);
+      }
+      if (bad) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (n >= s_bad[wave][8 * (i >> 2) + 4 * half + (i & 3)]) o[i] = __builtin_nanf("");
+      }
+      // lane (n, half) holds columns 8 b + 4 half + a of row n: exchanged to eight in a row
+      uint16_t* dst = a.out + (row0 + t0 + n) * a.out_stride + h * 128 + 32 * wave + 8 * half;
+      if (n < valid) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const u32x2 x = swap_halves(pack_bf16x2(a.scale * o[8 * b], a.scale * o[8 * b + 1]),
+                                      pack_bf16x2(a.scale * o[8 * b + 4], a.scale * o[8 * b + 5]));
+          const u32x2 y = swap_halves(pack_bf16x2(a.scale * o[8 * b + 2], a.scale * o[8 * b + 3]),
+                                      pack_bf16x2(a.scale * o[8 * b + 6], a.scale * o[8 * b + 7]));
+          *reinterpret_cast<u32x4_any*>(dst + 16 * b) = u32x4{x[0], y[0], x[1], y[1]};
+        }
+      }
+    }
+
+    if (!kOutputs || t0 + kB < len || (last && so >= 0)) {   // of any use to what follows
+      float hi = block_hi, lo = block_lo;
+      if (valid < kB) {
+        const double d = exp(log_decay * valid);
+        hi = (float)d;
+        lo = (float)(d - (double)hi);
+      }
+#pragma unroll
+      for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) S[m][i] = __builtin_fmaf(S[m][i], hi, S[m][i] * lo);
+#pragma unroll
+      for (int k2 = 0; k2 < 2; ++k2) {
+        const u32x4 w = __builtin_bit_cast(u32x4, k2 ? v1 : v0);
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float f = fade[8 * k2 + i];
+          if (valid < kB) {
+            const int key = 16 * k2 + 8 * (i >> 2) + 4 * half + (i & 3);
+            f = power(log2_decay, max(valid - 1 - key, 0));
+          }
+          x[i] = (i & 1 ? bf16hi(w[i >> 1]) : bf16lo(w[i >> 1])) * f;
+        }
+        const Terms<3> vt3 = split<3>(x);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          const bf16x8 kk = read_columns(kt + kcol[m][0] + 16 * k2 * kRow, kt + kcol[m][1] + 16 * k2 * kRow);
+          S[m] = mfma(kk, vt3.t[2], S[m]);
+          S[m] = mfma(kk, vt3.t[1], S[m]);
+          S[m] = mfma(kk, vt3.t[0], S[m]);
+        }
+      }
+    }
+    if (t0 + kB < len) {
+      store(buf ^ 1);
+      if (t0 + 2 * kB < len) load(t0 + 2 * kB);
+    }
+    __syncthreads();
+  }
+
+  float* to = !kOutputs ? ws + slot : last && so >= 0 && so < a.num_slots ? a.states + so * slot + (int64_t)h * kState : nullptr;
+  if (to) {
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) to[(32 * m + dim(i)) * 128 + 32 * wave + n] = S[m][i];
+  }
+}
+
+// The states before the pieces of cut requests: workspace entry s + 1 of a request holds what piece s
+// alone makes of its tokens (piece 0: of the request's state too), and gets the sum with the entry before it, faded by
+// piece s.  A thread takes four elements of one head's states through all pieces.
+__global__ __launch_bounds__(256) void linear_carry_kernel(LinearLaunch a) {
+  const int h = blockIdx.y;
+  const int lane = threadIdx.x & 63;
+  // the blockIdx.z-th cut request
+  int32_t idx = blockIdx.z, ws = 0, pieces = 0;
+  for (int32_t r0 = 0; r0 < a.num_reqs; r0 += 64) {
+    const int32_t len = r0 + lane < a.num_reqs ? a.chunk_lens[r0 + lane] : -1;
+    const int32_t cut = len > kLinearShortTokens && len > a.piece_tokens ? (len + a.piece_tokens - 1) / a.piece_tokens : 0;
+    const uint64_t is = __ballot(cut > 0);
+    const int32_t total = __popcll(is), sum = wave_scan(cut);
+    if (idx < total) {
+      const uint64_t here = __ballot(cut > 0 && __popcll(is & (((uint64_t)1 << lane) - 1)) == idx);
+      const int32_t c = __builtin_ctzll(here);
+      pieces = __builtin_amdgcn_readlane(cut, c);
+      ws += __builtin_amdgcn_readlane(sum, c) - pieces;
+      break;
+    }
+    idx -= total;
+    ws += __builtin_amdgcn_readlane(sum, 63);
+  }
+  if (pieces == 0 || ws + pieces > a.ws_states) return;
+  const float fade = (float)exp(clean_log(a.log_decay[h]) * a.piece_tokens);
+  const int64_t slot = (int64_t)a.hq * kState;
+  f32x4* p = reinterpret_cast<f32x4*>(a.ws + ws * slot + (int64_t)h * kState) + blockIdx.x * 256 + threadIdx.x;
+  f32x4 sum = p[slot / 4];
+  for (int s = 2; s < pieces; ++s) {
+    f32x4 x = p[s * (slot / 4)];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __builtin_fmaf(sum[i], fade, x[i]);
+    p[s * (slot / 4)] = sum = x;
+  }
 }
 
 }  // namespace
 
-hipError_t launch_linear_attn(const LinearLaunch& a, hipStream_t stream) {
-  if (a.num_reqs == 0) return hipSuccess;
-  linear_recurrent_kernel<<<dim3(128 / kSliceCols, a.hq, a.num_reqs), 256, 0, stream>>>(a);
+hipError_t launch_linear_attn(const LinearLaunch& launch, const LinearPlan& plan, hipStream_t stream) {
+  LinearLaunch a = launch;
+  a.piece_tokens = plan.piece_tokens;
+  a.ws_states = plan.ws_states;
+  const int group = a.hq / a.hkv;
+  auto blocks = [&](int64_t units) { return dim3((uint32_t)((units * a.hkv + 7) / 8 * 8 * group)); };
+  if (plan.cut_reqs > 0) {
+    a.num_units = plan.ws_states - plan.cut_reqs;
+    linear_block_kernel<false><<<blocks(a.num_units), 256, 0, stream>>>(a);
+    linear_carry_kernel<<<dim3(kState / 1024, a.hq, plan.cut_reqs), 256, 0, stream>>>(a);
+  }
+  if (plan.pieces > 0) {
+    a.num_units = plan.pieces;
+    linear_block_kernel<true><<<blocks(a.num_units), 256, 0, stream>>>(a);
+  }
+  if (plan.short_reqs > 0)
+    linear_recurrent_kernel<<<dim3(128 / kSliceCols, a.hq, plan.short_reqs), 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
