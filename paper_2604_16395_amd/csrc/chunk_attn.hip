@@ -69,34 +69,14 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kOverflow = 18446744073709551616.0f;   // 2^64: largest probability kept
 
-// Raw buffer loads: a resource descriptor (base, size in bytes) in SGPRs plus a per-lane
-// byte offset.  Offsets at or past the size read as zero.
-constexpr int32_t kRsrcWord3 = 0x00020000;   // gfx9-family raw buffer: 32-bit dword format
 __device__ inline __amdgpu_buffer_rsrc_t make_rsrc(const void* base, int32_t bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, bytes, kRsrcWord3);
 }
 
-typedef __attribute__((address_space(3))) void lds_void;
 typedef short v4i16 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
 
 __device__ inline int clamp16(int x) { return x < 0 ? 0 : (x > 16 ? 16 : x); }
-
-// LDS-direct copy: 64 lanes x 16 bytes from a raw buffer (descriptor words in SGPRs) to the
-// 1 KiB of LDS at byte address `lds`, lane l's bytes at lds + 16 l.  Issued as inline
-// assembly so that the compiler does not treat every later LDS read as waiting on it; the
-// caller waits for the copy's vmcnt and synchronises before the destination is read.
-typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
-__device__ inline i32x4 sgpr_rsrc(const void* base, int32_t bytes) {
-  const uint64_t a = reinterpret_cast<uint64_t>(base);
-  return i32x4{(int32_t)__builtin_amdgcn_readfirstlane((uint32_t)a),
-               (int32_t)(__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32)) & 0xffff),
-               __builtin_amdgcn_readfirstlane(bytes), kRsrcWord3};
-}
-__device__ inline void lds_dma_b128(const i32x4& rs, uint32_t voff, uint32_t lds) {
-  __asm__ volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                   :: "s"(lds), "v"(voff), "s"(rs) : "m0");
-}
 
 // Wait until at most N vector-memory operations of this wave are outstanding (the older
 // ones, issued first, are then complete); lgkm and exp counters are not waited for.

@@ -202,12 +202,30 @@ __device__ inline Terms<kTerms> split(float* x) {
   return r;
 }
 
+// acc where both bf16 of w are finite (0 times them is 0), else NaN.  (By value: a bit cast of a vector's
+// element itself takes the vector's first.)
+__device__ inline float probe_bf16x2(uint32_t w, float acc) {
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), bf16x2{}, acc, false);
+}
+
+// The block's tile is there: at most kNewer vector-memory operations of this wave are younger than its
+// copies, and every wave has read what it wanted of the tile that is overwritten next.
+template <int kNewer>
+__device__ inline void tile_barrier() {
+  __asm__ volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kNewer) : "memory");
+}
+
 // kOutputs: the blocks of all pieces, with outputs and, of a request's last piece, its state.
 // Otherwise the own states of all pieces but the last, and (piece 0) a copy of the request's state.
-template <bool kOutputs>
+// kDirect: tiles are copied straight into LDS, kStages - 1 blocks ahead; rows at addresses or strides that
+// those copies do not take go through registers, one block ahead.
+template <bool kOutputs, bool kDirect>
 __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
-  constexpr int kTiles = kOutputs ? 3 : 2;   // K, V, Q
-  __shared__ __attribute__((aligned(16))) uint8_t s_tile[2][kTiles][kTile];
+  constexpr int kTiles = kOutputs ? 3 : 2;             // K, V, Q
+  constexpr int kStages = kDirect ? (kOutputs ? 3 : 4) : 2;
+  constexpr int kStage = kTiles * kTile, kRing = kStages * kStage;
+  constexpr int kCopies = 2 * kTiles, kStores = kOutputs ? 2 : 0;   // a wave's, for a block
+  __shared__ __attribute__((aligned(1024))) uint8_t s_ring[kRing];
   __shared__ int32_t s_bad[4][32];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5, n = lane & 31;
@@ -227,32 +245,59 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
   const int si = a.slot_in[p.req], so = a.slot_out[p.req];
   const int64_t slot = (int64_t)a.hq * kState;
   float* const ws = a.ws + ((int64_t)p.ws + p.seg) * slot + (int64_t)h * kState;
+  const int blocks = (len + kB - 1) / kB;
 
-  // staging: this wave's rows 8 wave + 4 d + (lane / 16) of each tile, 16 bytes a lane
-  const int srow = 8 * wave + (lane >> 4), schunk = lane & 15;
-  const uint16_t* kp = a.k + (row0 + srow) * a.k_stride + g * 128 + 8 * schunk;
-  const uint16_t* vp = a.v + (row0 + srow) * a.v_stride + g * 128 + 8 * schunk;
-  const uint16_t* qp = kOutputs ? a.q + (row0 + srow) * a.q_stride + h * 128 + 8 * schunk : nullptr;
+  // this wave's rows 8 wave + 4 d + (lane / 16) of each tile, 16 bytes a lane
+  const int srow = 8 * wave + (lane >> 4), place = lane & 15;
+  const uint16_t* src[3] = {a.k + row0 * a.k_stride + g * 128, a.v + row0 * a.v_stride + g * 128,
+                            kOutputs ? a.q + row0 * a.q_stride + h * 128 : nullptr};
+  const int64_t stride[3] = {a.k_stride, a.v_stride, a.q_stride};
+  const uint32_t ring0 = (uint32_t)(uintptr_t)(lds_void*)s_ring;
+  uint32_t off[kTiles][2];
   u32x4 st[kTiles][2];
-  auto load = [&](int t0) {    // the block at token t0; rows past the piece are zero
+  auto copy = [&](int block, int at) {      // straight into LDS; rows past the piece read as zero
+    const int rows = min(kB, len - block * kB);
 #pragma unroll
-    for (int d = 0; d < 2; ++d) {
-      const bool in = t0 + srow + 4 * d < len;
-      st[0][d] = in ? (u32x4)*reinterpret_cast<const u32x4_any*>(kp + (int64_t)(t0 + 4 * d) * a.k_stride) : u32x4{};
-      st[1][d] = in ? (u32x4)*reinterpret_cast<const u32x4_any*>(vp + (int64_t)(t0 + 4 * d) * a.v_stride) : u32x4{};
-      if constexpr (kOutputs)
-        st[2][d] = in ? (u32x4)*reinterpret_cast<const u32x4_any*>(qp + (int64_t)(t0 + 4 * d) * a.q_stride) : u32x4{};
+    for (int t = 0; t < kTiles; ++t) {
+      const i32x4 rs = sgpr_rsrc(src[t] + (int64_t)block * kB * stride[t], (rows - 1) * (int32_t)stride[t] * 2 + kRow);
+#pragma unroll
+      for (int d = 0; d < 2; ++d)
+        lds_dma_b128(rs, off[t][d], __builtin_amdgcn_readfirstlane(ring0 + at + t * kTile + (8 * wave + 4 * d) * kRow));
     }
   };
-  auto store = [&](int buf) {
+  auto load = [&](int block) {
 #pragma unroll
-    for (int d = 0; d < 2; ++d) {
-      const int row = srow + 4 * d, at = row * kRow + ((schunk ^ perm(row)) << 4);
+    for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t) *reinterpret_cast<u32x4*>(&s_tile[buf][t][at]) = st[t][d];
-    }
+      for (int d = 0; d < 2; ++d) {
+        const int64_t row = (int64_t)block * kB + srow + 4 * d;
+        st[t][d] = u32x4{};
+        if (row < len) st[t][d] = *reinterpret_cast<const u32x4_any*>(src[t] + row * stride[t] + 8 * place);
+      }
   };
-  load(0);
+  auto store = [&](int at) {
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int d = 0; d < 2; ++d) {
+        const int row = srow + 4 * d;
+        *reinterpret_cast<u32x4*>(s_ring + at + t * kTile + row * kRow + ((place ^ perm(row)) << 4)) = st[t][d];
+      }
+  };
+  if constexpr (kDirect) {
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int d = 0; d < 2; ++d) {
+        const int row = srow + 4 * d;
+        off[t][d] = (uint32_t)row * (uint32_t)stride[t] * 2 + ((place ^ perm(row)) << 4);
+      }
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s)
+      if (s < blocks) copy(s, s * kStage);
+  } else {
+    load(0);
+  }
 
   // operand addresses within a tile
   int rows[8];                // row n, dims 16 s + 8 half .. + 7
@@ -265,86 +310,99 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
     const int row = trow + 8 * y;
 #pragma unroll
     for (int m = 0; m < 4; ++m) kcol[m][y] = row * kRow + (((4 * m + 2 * b4 + (j & 1)) ^ perm(row)) << 4) + 8 * ((j >> 1) & 1);
-    vcol[y] = row * kRow + (((4 * wave + 2 * b4 + ((j >> 1) & 1)) ^ perm(row)) << 4) + 8 * (j & 1);
+    vcol[y] = kTile + row * kRow + (((4 * wave + 2 * b4 + ((j >> 1) & 1)) ^ perm(row)) << 4) + 8 * (j & 1);
   }
+
+  const double log_decay = clean_log(a.log_decay[h]), log2_decay = log_decay * 1.4426950408889634;
+  const double block_decay = exp(log_decay * kB);
+  const double inv_block = block_decay > 1e-30 ? 1.0 / block_decay : 0.0;
+  auto key_of = [&](int i) { return 16 * (i >> 3) + 8 * ((i >> 2) & 1) + 4 * half + (i & 3); };
+  float within[16], fade[16];   // scale l^(i-j); l^(kB-1-j)
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    if constexpr (kOutputs) within[i] = n >= key_of(i) ? a.scale * power(log2_decay, n - key_of(i)) : 0.f;
+    fade[i] = power(log2_decay, kB - 1 - key_of(i));
+  }
+  const float since = a.scale * power(log2_decay, n + 1);
 
   // state: register (m, i) is key dim 32 m + dim(i), column 32 wave + n
   auto dim = [&](int i) { return 16 * (i >> 3) + 8 * half + 4 * ((i >> 2) & 1) + (i & 3); };
   f32x16 S[4];
-  const float* from = !kOutputs ? (p.seg == 0 && si >= 0 && si < a.num_slots ? a.states + si * slot + (int64_t)h * kState : nullptr)
-                      : pieces > 1 ? ws
-                                   : (si >= 0 && si < a.num_slots ? a.states + si * slot + (int64_t)h * kState : nullptr);
-  const float none = (!kOutputs && p.seg > 0) || (kOutputs && pieces > 1) || si == -1 ? 0.f : __builtin_nanf("");
+  const bool own_state = kOutputs ? pieces == 1 : p.seg == 0;   // the request's, not the workspace's or none
+  const float* from = own_state ? (si >= 0 && si < a.num_slots ? a.states + si * slot + (int64_t)h * kState : nullptr)
+                      : kOutputs ? ws : nullptr;
+  const float none = !own_state || si == -1 ? 0.f : __builtin_nanf("");
 #pragma unroll
   for (int m = 0; m < 4; ++m)
 #pragma unroll
     for (int i = 0; i < 16; ++i) S[m][i] = from ? from[(32 * m + dim(i)) * 128 + 32 * wave + n] : none;
   if (!kOutputs && p.seg == 0) {   // the state before piece 0 stays: the request may advance in place
+    const float f = power(log2_decay, len);
 #pragma unroll
     for (int m = 0; m < 4; ++m)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) ws[(32 * m + dim(i)) * 128 + 32 * wave + n] = S[m][i];
+      for (int i = 0; i < 16; ++i) {
+        ws[(32 * m + dim(i)) * 128 + 32 * wave + n] = S[m][i];
+        S[m][i] *= f;
+      }
   }
 
-  const double log_decay = clean_log(a.log_decay[h]), log2_decay = log_decay * 1.4426950408889634;
-  const double block_d = exp(log_decay * kB);
-  const float block_hi = (float)block_d, block_lo = (float)(block_d - (double)block_hi);
-  float within[16], fade[16];   // l^(i-j), 0 above the diagonal; l^(kB-1-j)
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int key = 16 * (i >> 3) + 8 * ((i >> 2) & 1) + 4 * half + (i & 3);
-    within[i] = n >= key ? power(log2_decay, n - key) : 0.f;
-    fade[i] = power(log2_decay, kB - 1 - key);
+  if constexpr (!kDirect) {
+    store(0);
+    if (1 < blocks) load(1);
   }
-  const float since = power(log2_decay, n + 1);
-
-  store(0);
-  if (kB < len) load(kB);
-  __syncthreads();
-  for (int t0 = 0, buf = 0; t0 < len; t0 += kB, buf ^= 1) {
-    const int valid = min(kB, len - t0);
-    const uint8_t* kt = s_tile[buf][0];
-    const uint8_t* vt = s_tile[buf][1];
-    const bf16x8 v0 = read_columns(vt + vcol[0], vt + vcol[1]);
-    const bf16x8 v1 = read_columns(vt + vcol[0] + 16 * kRow, vt + vcol[1] + 16 * kRow);
-    u32x4 vw[2] = {__builtin_bit_cast(u32x4, v0), __builtin_bit_cast(u32x4, v1)};
+  double owed = 1.0;   // what the fp32 block factors so far left out
+  int at = 0;          // the block's stage
+  for (int b = 0; b < blocks; ++b) {
+    if constexpr (kDirect) {
+      if (b + kStages - 2 >= blocks) tile_barrier<0>();
+      else if (b < kStages - 1) tile_barrier<(kStages - 2) * kCopies>();
+      else tile_barrier<(kStages - 2) * kCopies + (kStages - 1) * kStores>();
+      // the stage before this one's is read out
+      if (b + kStages - 1 < blocks) copy(b + kStages - 1, at == 0 ? kRing - kStage : at - kStage);
+      __asm__ volatile("" ::: "memory");   // the block's stores are younger than the copies
+    } else {
+      __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+    const int valid = min(kB, len - b * kB);
+    const uint8_t* tile = s_ring + at;
+    const bf16x8 vc[2] = {read_columns(tile + vcol[0], tile + vcol[1]),
+                          read_columns(tile + vcol[0] + 16 * kRow, tile + vcol[1] + 16 * kRow)};
 
     if constexpr (kOutputs) {
-      const uint8_t* qt = s_tile[buf][2];
       f32x16 p16{}, o{};
 #pragma unroll
       for (int s = 0; s < 8; ++s) {
-        const bf16x8 q = read_row(qt + rows[s]);
-        p16 = mfma(read_row(kt + rows[s]), q, p16);
+        const bf16x8 q = read_row(tile + 2 * kTile + rows[s]);
+        p16 = mfma(read_row(tile + rows[s]), q, p16);
         float x[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = S[s >> 1][8 * (s & 1) + i];
-        const Terms<2> st2 = split<2>(x);
-        o = mfma(st2.t[1], q, o);
-        o = mfma(st2.t[0], q, o);
+        const Terms<2> sx = split<2>(x);
+        o = mfma(sx.t[1], q, o);
+        o = mfma(sx.t[0], q, o);
       }
       // A value of v that is not finite is no matter of the rows before it: 0 in their sums, and NaN put
-      // into the rows from its own on.
-      uint32_t top = 0;
+      // into the rows from its own on.  (0 times it is NaN, 0 times any other 0.)
+      u32x4 vw[2] = {__builtin_bit_cast(u32x4, vc[0]), __builtin_bit_cast(u32x4, vc[1])};
+      float probe = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t w = vw[i >> 2][i & 3] & 0x7FFF7FFFu;
-        top = max(top, max(w & 0xFFFFu, w >> 16));
-      }
-      const bool bad = __ballot(top >= 0x7F80u) != 0;
+      for (int i = 0; i < 8; ++i)
+        probe = probe_bf16x2(vw[i >> 2][i & 3], probe);
+      const bool bad = __ballot(probe != probe) != 0;
       if (bad) {
-        int at = kB;
+        int from_row = kB;
 #pragma unroll
         for (int i = 15; i >= 0; --i) {
           const uint32_t w = vw[i >> 3][(i >> 1) & 3];
           const uint32_t bits = i & 1 ? w >> 16 : w & 0xFFFFu;
           if ((bits & 0x7F80u) == 0x7F80u) {
-            at = min(at, 16 * (i >> 3) + 8 * ((i >> 2) & 1) + 4 * half + (i & 3));
+            from_row = min(from_row, key_of(i));
             vw[i >> 3][(i >> 1) & 3] = w & (i & 1 ? 0x0000FFFFu : 0xFFFF0000u);
           }
         }
-        at = min(at, __shfl_xor(at, 32, 64));
-        if (half == 0) s_bad[wave][n] = at;
+        from_row = min(from_row, __shfl_xor(from_row, 32, 64));
+        if (half == 0) s_bad[wave][n] = from_row;
         __builtin_amdgcn_wave_barrier();
       }
 #pragma unroll
@@ -353,7 +411,7 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
       for (int k2 = 0; k2 < 2; ++k2) {
         float x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = within[8 * k2 + i] == 0.f ? 0.f : p16[8 * k2 + i] * within[8 * k2 + i];
+        for (int i = 0; i < 8; ++i) x[i] = n >= key_of(8 * k2 + i) ? p16[8 * k2 + i] * within[8 * k2 + i] : 0.f;
         const Terms<2> pt = split<2>(x);
         const bf16x8 vv = __builtin_bit_cast(bf16x8, vw[k2]);
         o = mfma(vv, pt.t[1], o);
@@ -364,59 +422,67 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
         for (int i = 0; i < 16; ++i)
           if (n >= s_bad[wave][8 * (i >> 2) + 4 * half + (i & 3)]) o[i] = __builtin_nanf("");
       }
-      // lane (n, half) holds columns 8 b + 4 half + a of row n: exchanged to eight in a row
-      uint16_t* dst = a.out + (row0 + t0 + n) * a.out_stride + h * 128 + 32 * wave + 8 * half;
-      if (n < valid) {
+      // lane (n, half) holds columns 8 c + 4 half + 0 .. 3 of row n: exchanged to eight in a row
+      uint16_t* dst = a.out + (row0 + b * kB + n) * a.out_stride + h * 128 + 32 * wave + 8 * half;
+      u32x4 y[2];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const u32x2 x = swap_halves(pack_bf16x2(a.scale * o[8 * b], a.scale * o[8 * b + 1]),
-                                      pack_bf16x2(a.scale * o[8 * b + 4], a.scale * o[8 * b + 5]));
-          const u32x2 y = swap_halves(pack_bf16x2(a.scale * o[8 * b + 2], a.scale * o[8 * b + 3]),
-                                      pack_bf16x2(a.scale * o[8 * b + 6], a.scale * o[8 * b + 7]));
-          *reinterpret_cast<u32x4_any*>(dst + 16 * b) = u32x4{x[0], y[0], x[1], y[1]};
-        }
+      for (int c = 0; c < 2; ++c) {
+        const u32x2 u = swap_halves(pack_bf16x2(o[8 * c], o[8 * c + 1]), pack_bf16x2(o[8 * c + 4], o[8 * c + 5]));
+        const u32x2 w = swap_halves(pack_bf16x2(o[8 * c + 2], o[8 * c + 3]), pack_bf16x2(o[8 * c + 6], o[8 * c + 7]));
+        y[c] = u32x4{u[0], w[0], u[1], w[1]};
+      }
+      if (valid == kB) {       // kStores stores, which the next tile_barriers count on
+        *reinterpret_cast<u32x4_any*>(dst) = y[0];
+        *reinterpret_cast<u32x4_any*>(dst + 16) = y[1];
+      } else if (n < valid) {
+        *reinterpret_cast<u32x4_any*>(dst) = y[0];
+        *reinterpret_cast<u32x4_any*>(dst + 16) = y[1];
       }
     }
 
-    if (!kOutputs || t0 + kB < len || (last && so >= 0)) {   // of any use to what follows
-      float hi = block_hi, lo = block_lo;
-      if (valid < kB) {
-        const double d = exp(log_decay * valid);
-        hi = (float)d;
-        lo = (float)(d - (double)hi);
+    // The state.  With outputs it fades block by block (what the fp32 factor leaves out goes into the next);
+    // without, each block fades to the piece's end at once.
+    if (!kOutputs || b + 1 < blocks || (last && so >= 0)) {
+      if constexpr (kOutputs) {
+        const double f64 = (valid == kB ? block_decay : exp(log_decay * valid)) * owed;
+        const float f = (float)f64;
+        owed = 1.0 + (f64 - (double)f) * inv_block;
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) S[m][i] *= f;
       }
-#pragma unroll
-      for (int m = 0; m < 4; ++m)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) S[m][i] = __builtin_fmaf(S[m][i], hi, S[m][i] * lo);
+      const float to_end = kOutputs ? 1.f : power(log2_decay, len - (b + 1) * kB);
 #pragma unroll
       for (int k2 = 0; k2 < 2; ++k2) {
-        const u32x4 w = __builtin_bit_cast(u32x4, k2 ? v1 : v0);
+        const u32x4 w = __builtin_bit_cast(u32x4, vc[k2]);
         float x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          float f = fade[8 * k2 + i];
-          if (valid < kB) {
-            const int key = 16 * k2 + 8 * (i >> 2) + 4 * half + (i & 3);
-            f = power(log2_decay, max(valid - 1 - key, 0));
-          }
-          x[i] = (i & 1 ? bf16hi(w[i >> 1]) : bf16lo(w[i >> 1])) * f;
+        for (int i = 0; i < 8; ++i) x[i] = i & 1 ? bf16hi(w[i >> 1]) : bf16lo(w[i >> 1]);
+        if (!kOutputs || valid == kB) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] *= kOutputs ? fade[8 * k2 + i] : fade[8 * k2 + i] * to_end;
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] *= power(log2_decay, max(valid - 1 - key_of(8 * k2 + i), 0));
         }
-        const Terms<3> vt3 = split<3>(x);
+        const Terms<3> vx = split<3>(x);
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-          const bf16x8 kk = read_columns(kt + kcol[m][0] + 16 * k2 * kRow, kt + kcol[m][1] + 16 * k2 * kRow);
-          S[m] = mfma(kk, vt3.t[2], S[m]);
-          S[m] = mfma(kk, vt3.t[1], S[m]);
-          S[m] = mfma(kk, vt3.t[0], S[m]);
+          const bf16x8 kk = read_columns(tile + kcol[m][0] + 16 * k2 * kRow, tile + kcol[m][1] + 16 * k2 * kRow);
+          S[m] = mfma(kk, vx.t[2], S[m]);
+          S[m] = mfma(kk, vx.t[1], S[m]);
+          S[m] = mfma(kk, vx.t[0], S[m]);
         }
       }
     }
-    if (t0 + kB < len) {
-      store(buf ^ 1);
-      if (t0 + 2 * kB < len) load(t0 + 2 * kB);
+    at = at + kStage == kRing ? 0 : at + kStage;
+    if constexpr (!kDirect) {
+      if (b + 1 < blocks) {
+        store(at);
+        if (b + 2 < blocks) load(b + 2);
+      }
     }
-    __syncthreads();
   }
 
   float* to = !kOutputs ? ws + slot : last && so >= 0 && so < a.num_slots ? a.states + so * slot + (int64_t)h * kState : nullptr;
@@ -472,14 +538,21 @@ hipError_t launch_linear_attn(const LinearLaunch& launch, const LinearPlan& plan
   a.ws_states = plan.ws_states;
   const int group = a.hq / a.hkv;
   auto blocks = [&](int64_t units) { return dim3((uint32_t)((units * a.hkv + 7) / 8 * 8 * group)); };
+  // what a copy straight into LDS takes: 16-byte steps, a row's end before the next one's start, 32-bit offsets
+  auto direct = [](const uint16_t* p, int64_t stride) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0 && stride >= 128 && stride <= (1 << 24);
+  };
+  const bool kv = direct(a.k, a.k_stride) && direct(a.v, a.v_stride), qkv = kv && direct(a.q, a.q_stride);
   if (plan.cut_reqs > 0) {
     a.num_units = plan.ws_states - plan.cut_reqs;
-    linear_block_kernel<false><<<blocks(a.num_units), 256, 0, stream>>>(a);
+    if (kv) linear_block_kernel<false, true><<<blocks(a.num_units), 256, 0, stream>>>(a);
+    else linear_block_kernel<false, false><<<blocks(a.num_units), 256, 0, stream>>>(a);
     linear_carry_kernel<<<dim3(kState / 1024, a.hq, plan.cut_reqs), 256, 0, stream>>>(a);
   }
   if (plan.pieces > 0) {
     a.num_units = plan.pieces;
-    linear_block_kernel<true><<<blocks(a.num_units), 256, 0, stream>>>(a);
+    if (qkv) linear_block_kernel<true, true><<<blocks(a.num_units), 256, 0, stream>>>(a);
+    else linear_block_kernel<true, false><<<blocks(a.num_units), 256, 0, stream>>>(a);
   }
   if (plan.short_reqs > 0)
     linear_recurrent_kernel<<<dim3(128 / kSliceCols, a.hq, plan.short_reqs), 256, 0, stream>>>(a);

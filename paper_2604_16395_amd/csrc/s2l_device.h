@@ -97,6 +97,28 @@ __device__ inline u32x2 swap_halves(uint32_t a, uint32_t b) {
   return u32x2{r[0], r[1]};
 }
 
+// Raw buffer loads: a resource descriptor (base, size in bytes) in SGPRs plus a per-lane
+// byte offset.  Offsets at or past the size read as zero.
+constexpr int32_t kRsrcWord3 = 0x00020000;   // gfx9-family raw buffer: 32-bit dword format
+
+typedef __attribute__((address_space(3))) void lds_void;
+
+// LDS-direct copy: 64 lanes x 16 bytes from a raw buffer (descriptor words in SGPRs) to the
+// 1 KiB of LDS at byte address `lds`, lane l's bytes at lds + 16 l.  Issued as inline
+// assembly so that the compiler does not treat every later LDS read as waiting on it; the
+// caller waits for the copy's vmcnt and synchronises before the destination is read.
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+__device__ inline i32x4 sgpr_rsrc(const void* base, int32_t bytes) {
+  const uint64_t a = reinterpret_cast<uint64_t>(base);
+  return i32x4{(int32_t)__builtin_amdgcn_readfirstlane((uint32_t)a),
+               (int32_t)(__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32)) & 0xffff),
+               __builtin_amdgcn_readfirstlane(bytes), kRsrcWord3};
+}
+__device__ inline void lds_dma_b128(const i32x4& rs, uint32_t voff, uint32_t lds) {
+  __asm__ volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                   :: "s"(lds), "v"(voff), "s"(rs) : "m0");
+}
+
 // Outputs of a launch whose device plan did not fit the host's sizing (its status word is
 // not 0: the device length arrays disagree with the host copies, and nothing was planned).
 // Every workgroup writes NaN over its share of the `rows` output rows the host sized the
