@@ -178,6 +178,17 @@ __device__ inline f32x16 mfma(const bf16x8& a, const bf16x8& b, const f32x16& c)
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
+// (lo, hi) less the bf16 pair w: one v_dot2_f32_bf16 each instead of unpacking and subtracting.  Exact,
+// as w is their rounding.  (By value: a bit cast of a vector's element itself takes the vector's first.)
+// (-1, 0) is kept in a register: written as the inline constant -1.0 it came out as (0, -1).
+__device__ inline void take_off(uint32_t w, float& lo, float& hi) {
+  uint32_t first = 0x0000BF80u;
+  __asm__("" : "+s"(first));
+  const bf16x2 p = __builtin_bit_cast(bf16x2, w);
+  lo = __builtin_amdgcn_fdot2_f32_bf16(p, __builtin_bit_cast(bf16x2, first), lo, false);
+  hi = __builtin_amdgcn_fdot2_f32_bf16(p, __builtin_bit_cast(bf16x2, 0xBF800000u), hi, false);
+}
+
 // x as a sum of kTerms bf16 vectors, each the rounding of what the ones before leave.
 template <int kTerms>
 struct Terms {
@@ -192,18 +203,14 @@ __device__ inline Terms<kTerms> split(float* x) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       w[j] = pack_bf16x2(x[2 * j], x[2 * j + 1]);
-      if (i + 1 < kTerms) {
-        x[2 * j] -= bf16lo(w[j]);
-        x[2 * j + 1] -= bf16hi(w[j]);
-      }
+      if (i + 1 < kTerms) take_off(w[j], x[2 * j], x[2 * j + 1]);
     }
     r.t[i] = __builtin_bit_cast(bf16x8, w);
   }
   return r;
 }
 
-// acc where both bf16 of w are finite (0 times them is 0), else NaN.  (By value: a bit cast of a vector's
-// element itself takes the vector's first.)
+// acc where both bf16 of w are finite (0 times them is 0), else NaN.
 __device__ inline float probe_bf16x2(uint32_t w, float acc) {
   return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), bf16x2{}, acc, false);
 }
@@ -215,10 +222,17 @@ __device__ inline void tile_barrier() {
   __asm__ volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kNewer) : "memory");
 }
 
+// The lanes (n, half) whose query n sees key 16 (i / 8) + 8 (i / 4 % 2) + 4 half + i % 4 of its block.
+__device__ constexpr uint64_t causal_lanes(int i) {
+  const int key = 16 * (i >> 3) + 8 * ((i >> 2) & 1) + (i & 3);
+  return (uint64_t)(0xFFFFFFFFu << key) | (uint64_t)(0xFFFFFFFFu << (key + 4)) << 32;
+}
+
 // kOutputs: the blocks of all pieces, with outputs and, of a request's last piece, its state.
 // Otherwise the own states of all pieces but the last, and (piece 0) a copy of the request's state.
 // kDirect: tiles are copied straight into LDS, kStages - 1 blocks ahead; rows at addresses or strides that
 // those copies do not take go through registers, one block ahead.
+constexpr double kMostBehind = 60.0;
 template <bool kOutputs, bool kDirect>
 __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
   constexpr int kTiles = kOutputs ? 3 : 2;             // K, V, Q
@@ -235,8 +249,12 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
   const int h0 = (int)(blockIdx.x / 8) % group;
   if (unit >= a.num_units * a.hkv) return;
   const int g = unit % a.hkv, h = g * group + h0;
-  const Piece p = find_unit<kOutputs ? kPieces : kInner>(a, unit / a.hkv);
+  Piece p = find_unit<kOutputs ? kPieces : kInner>(a, unit / a.hkv);
   if (p.req < 0) return;
+  p.req = __builtin_amdgcn_readfirstlane(p.req);
+  p.seg = __builtin_amdgcn_readfirstlane(p.seg);
+  p.len = __builtin_amdgcn_readfirstlane(p.len);
+  p.ws = __builtin_amdgcn_readfirstlane(p.ws);
   const int pieces = (p.len + a.piece_tokens - 1) / a.piece_tokens;
   const int first = p.seg * a.piece_tokens, len = min(a.piece_tokens, p.len - first);
   const bool last = p.seg == pieces - 1;
@@ -314,8 +332,6 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
   }
 
   const double log_decay = clean_log(a.log_decay[h]), log2_decay = log_decay * 1.4426950408889634;
-  const double block_decay = exp(log_decay * kB);
-  const double inv_block = block_decay > 1e-30 ? 1.0 / block_decay : 0.0;
   auto key_of = [&](int i) { return 16 * (i >> 3) + 8 * ((i >> 2) & 1) + 4 * half + (i & 3); };
   float within[16], fade[16];   // scale l^(i-j); l^(kB-1-j)
 #pragma unroll
@@ -351,7 +367,7 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
     store(0);
     if (1 < blocks) load(1);
   }
-  double owed = 1.0;   // what the fp32 block factors so far left out
+  int behind = 0;      // tokens that S has yet to fade by: the state is l^behind S
   int at = 0;          // the block's stage
   for (int b = 0; b < blocks; ++b) {
     if constexpr (kDirect) {
@@ -382,6 +398,7 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
         o = mfma(sx.t[1], q, o);
         o = mfma(sx.t[0], q, o);
       }
+      const float reach = since * power(log2_decay, behind);
       // A value of v that is not finite is no matter of the rows before it: 0 in their sums, and NaN put
       // into the rows from its own on.  (0 times it is NaN, 0 times any other 0.)
       u32x4 vw[2] = {__builtin_bit_cast(u32x4, vc[0]), __builtin_bit_cast(u32x4, vc[1])};
@@ -406,12 +423,15 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
         __builtin_amdgcn_wave_barrier();
       }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[i] *= since;
+      for (int i = 0; i < 16; ++i) o[i] *= reach;
 #pragma unroll
       for (int k2 = 0; k2 < 2; ++k2) {
         float x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = n >= key_of(8 * k2 + i) ? p16[8 * k2 + i] * within[8 * k2 + i] : 0.f;
+        for (int i = 0; i < 8; ++i) {
+          const float y = p16[8 * k2 + i] * within[8 * k2 + i];
+          x[i] = __builtin_amdgcn_inverse_ballot_w64(causal_lanes(8 * k2 + i)) ? y : 0.f;
+        }
         const Terms<2> pt = split<2>(x);
         const bf16x8 vv = __builtin_bit_cast(bf16x8, vw[k2]);
         o = mfma(vv, pt.t[1], o);
@@ -440,19 +460,20 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
       }
     }
 
-    // The state.  With outputs it fades block by block (what the fp32 factor leaves out goes into the next);
-    // without, each block fades to the piece's end at once.
+    // The state.  Without outputs each block fades to the piece's end at once.  With them S fades only when it is
+    // behind by a factor of more than 2^kMostBehind (or at the end), and what joins it is blown up by that much.
     if (!kOutputs || b + 1 < blocks || (last && so >= 0)) {
-      if constexpr (kOutputs) {
-        const double f64 = (valid == kB ? block_decay : exp(log_decay * valid)) * owed;
-        const float f = (float)f64;
-        owed = 1.0 + (f64 - (double)f) * inv_block;
+      const int after = behind + valid;
+      const bool fades = kOutputs && (b + 1 == blocks || -log2_decay * after > kMostBehind);
+      if (fades) {
+        const float f = power(log2_decay, after);
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
           for (int i = 0; i < 16; ++i) S[m][i] *= f;
       }
-      const float to_end = kOutputs ? 1.f : power(log2_decay, len - (b + 1) * kB);
+      const float join = power(log2_decay, kOutputs ? (fades ? 0 : -after) : len - (b + 1) * kB);
+      behind = fades ? 0 : after;
 #pragma unroll
       for (int k2 = 0; k2 < 2; ++k2) {
         const u32x4 w = __builtin_bit_cast(u32x4, vc[k2]);
@@ -461,8 +482,8 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
         for (int i = 0; i < 8; ++i) x[i] = i & 1 ? bf16hi(w[i >> 1]) : bf16lo(w[i >> 1]);
         if (!kOutputs || valid == kB) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] *= kOutputs ? fade[8 * k2 + i] : fade[8 * k2 + i] * to_end;
-        } else {
+          for (int i = 0; i < 8; ++i) x[i] *= fade[8 * k2 + i] * join;
+        } else {   // the last block: it fades
 #pragma unroll
           for (int i = 0; i < 8; ++i) x[i] *= power(log2_decay, max(valid - 1 - key_of(8 * k2 + i), 0));
         }
