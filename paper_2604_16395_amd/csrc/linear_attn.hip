@@ -222,6 +222,17 @@ __device__ inline void tile_barrier() {
   __asm__ volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kNewer) : "memory");
 }
 
+// Order of a basic block for the scheduler: kMfma times an MFMA, LDS reads and VALU work to go beside it.
+template <int kMfma, int kValu, int kReads>
+__device__ inline void interleave() {
+#pragma unroll
+  for (int i = 0; i < kMfma; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, kValu, 0);
+  }
+}
+
 // The lanes (n, half) whose query n sees key 16 (i / 8) + 8 (i / 4 % 2) + 4 half + i % 4 of its block.
 __device__ constexpr uint64_t causal_lanes(int i) {
   const int key = 16 * (i >> 3) + 8 * ((i >> 2) & 1) + (i & 3);
@@ -273,8 +284,11 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
   const uint32_t ring0 = (uint32_t)(uintptr_t)(lds_void*)s_ring;
   uint32_t off[kTiles][2];
   u32x4 st[kTiles][2];
-  auto copy = [&](int block, int at) {      // straight into LDS; rows past the piece read as zero
-    const int rows = min(kB, len - block * kB);
+  // A piece's own state takes its blocks from the last to the first: the launch leaves the first ones in the
+  // memory-side cache, where the outputs' launch begins.
+  auto nth = [&](int b) { return kOutputs ? b : blocks - 1 - b; };
+  auto copy = [&](int b, int at) {      // straight into LDS; rows past the piece read as zero
+    const int block = nth(b), rows = min(kB, len - block * kB);
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
       const i32x4 rs = sgpr_rsrc(src[t] + (int64_t)block * kB * stride[t], (rows - 1) * (int32_t)stride[t] * 2 + kRow);
@@ -283,7 +297,8 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
         lds_dma_b128(rs, off[t][d], __builtin_amdgcn_readfirstlane(ring0 + at + t * kTile + (8 * wave + 4 * d) * kRow));
     }
   };
-  auto load = [&](int block) {
+  auto load = [&](int b) {
+    const int block = nth(b);
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
@@ -317,17 +332,14 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
     load(0);
   }
 
-  // operand addresses within a tile
-  int rows[8];                // row n, dims 16 s + 8 half .. + 7
-#pragma unroll
-  for (int s = 0; s < 8; ++s) rows[s] = n * kRow + (((2 * s + half) ^ perm(n)) << 4);
+  // operand addresses within a stage; chunk bits are apart from the rest, so other chunks are an exclusive or away
+  const int rows = n * kRow + ((half ^ perm(n)) << 4);   // row n, dims 16 s + 8 half .. + 7: ^ s << 5
   const int j = lane & 15, b4 = (lane >> 4) & 1, trow = 4 * half + (j >> 2);
-  int kcol[4][2], vcol[2];    // [state tile][rows + 0, + 8]
+  int kcol[2], vcol[2];       // rows + 0, + 8; state tile m: ^ m << 6
 #pragma unroll
   for (int y = 0; y < 2; ++y) {
     const int row = trow + 8 * y;
-#pragma unroll
-    for (int m = 0; m < 4; ++m) kcol[m][y] = row * kRow + (((4 * m + 2 * b4 + (j & 1)) ^ perm(row)) << 4) + 8 * ((j >> 1) & 1);
+    kcol[y] = row * kRow + (((2 * b4 + (j & 1)) ^ perm(row)) << 4) + 8 * ((j >> 1) & 1);
     vcol[y] = kTile + row * kRow + (((4 * wave + 2 * b4 + ((j >> 1) & 1)) ^ perm(row)) << 4) + 8 * (j & 1);
   }
 
@@ -380,33 +392,30 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
     } else {
       __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
-    const int valid = min(kB, len - b * kB);
-    const uint8_t* tile = s_ring + at;
-    const bf16x8 vc[2] = {read_columns(tile + vcol[0], tile + vcol[1]),
-                          read_columns(tile + vcol[0] + 16 * kRow, tile + vcol[1] + 16 * kRow)};
+    const int valid = kOutputs ? min(kB, len - b * kB) : kB;
+    const uint8_t* const tile = s_ring;
+    const bf16x8 vc[2] = {read_columns(tile + at + vcol[0], tile + at + vcol[1]),
+                          read_columns(tile + at + vcol[0] + 16 * kRow, tile + at + vcol[1] + 16 * kRow)};
+    u32x4 vw[2] = {__builtin_bit_cast(u32x4, vc[0]), __builtin_bit_cast(u32x4, vc[1])};
 
+    // What joins the state.  Without outputs each block fades to the piece's end at once.  With them S fades only
+    // when it is behind by a factor of more than 2^kMostBehind (or at the end), and what joins it is blown up
+    // by as much.
+    const int after = behind + valid;
+    const bool fades = kOutputs && (b + 1 == blocks || -log2_decay * after > kMostBehind);
+    const float join = power(log2_decay, kOutputs ? (fades ? 0 : -after) : len - (nth(b) + 1) * kB);
+    if (kOutputs && valid < kB) {   // the last block
+#pragma unroll
+      for (int i = 0; i < 16; ++i) fade[i] = power(log2_decay, max(valid - 1 - key_of(i), 0));
+    }
+    bool bad = false;
     if constexpr (kOutputs) {
-      f32x16 p16{}, o{};
-#pragma unroll
-      for (int s = 0; s < 8; ++s) {
-        const bf16x8 q = read_row(tile + 2 * kTile + rows[s]);
-        p16 = mfma(read_row(tile + rows[s]), q, p16);
-        float x[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = S[s >> 1][8 * (s & 1) + i];
-        const Terms<2> sx = split<2>(x);
-        o = mfma(sx.t[1], q, o);
-        o = mfma(sx.t[0], q, o);
-      }
-      const float reach = since * power(log2_decay, behind);
       // A value of v that is not finite is no matter of the rows before it: 0 in their sums, and NaN put
       // into the rows from its own on.  (0 times it is NaN, 0 times any other 0.)
-      u32x4 vw[2] = {__builtin_bit_cast(u32x4, vc[0]), __builtin_bit_cast(u32x4, vc[1])};
       float probe = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        probe = probe_bf16x2(vw[i >> 2][i & 3], probe);
-      const bool bad = __ballot(probe != probe) != 0;
+      for (int i = 0; i < 8; ++i) probe = probe_bf16x2(vw[i >> 2][i & 3], probe);
+      bad = __ballot(probe != probe) != 0;
       if (bad) {
         int from_row = kB;
 #pragma unroll
@@ -422,6 +431,52 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
         if (half == 0) s_bad[wave][n] = from_row;
         __builtin_amdgcn_wave_barrier();
       }
+    }
+
+    Terms<3> vx[2];
+#pragma unroll
+    for (int k2 = 0; k2 < 2; ++k2) {
+      const u32x4 w = __builtin_bit_cast(u32x4, vc[k2]);
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = (i & 1 ? bf16hi(w[i >> 1]) : bf16lo(w[i >> 1])) * (fade[8 * k2 + i] * join);
+      vx[k2] = split<3>(x);
+    }
+
+    f32x16 p16{}, o{};
+    if constexpr (kOutputs) {
+      const int row = at + rows;
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        const bf16x8 q = read_row(tile + 2 * kTile + (row ^ s << 5));
+        p16 = mfma(read_row(tile + (row ^ s << 5)), q, p16);
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = S[s >> 1][8 * (s & 1) + i];
+        const Terms<2> sx = split<2>(x);
+        o = mfma(sx.t[1], q, o);
+        o = mfma(sx.t[0], q, o);
+      }
+      interleave<24, 9, 1>();
+    }
+    if (fades) {
+      const float f = power(log2_decay, after);
+#pragma unroll
+      for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) S[m][i] *= f;
+    }
+#pragma unroll
+    for (int k2 = 0; k2 < 2; ++k2)
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const bf16x8 kk = read_columns(tile + ((at + kcol[0]) ^ m << 6) + 16 * k2 * kRow, tile + ((at + kcol[1]) ^ m << 6) + 16 * k2 * kRow);
+        S[m] = mfma(kk, vx[k2].t[2], S[m]);
+        S[m] = mfma(kk, vx[k2].t[1], S[m]);
+        S[m] = mfma(kk, vx[k2].t[0], S[m]);
+      }
+    if constexpr (kOutputs) {
+      const float reach = since * power(log2_decay, behind);
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[i] *= reach;
 #pragma unroll
@@ -437,6 +492,7 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
         o = mfma(vv, pt.t[1], o);
         o = mfma(vv, pt.t[0], o);
       }
+      interleave<28, 4, 1>();
       if (bad) {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
@@ -459,44 +515,7 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
         *reinterpret_cast<u32x4_any*>(dst + 16) = y[1];
       }
     }
-
-    // The state.  Without outputs each block fades to the piece's end at once.  With them S fades only when it is
-    // behind by a factor of more than 2^kMostBehind (or at the end), and what joins it is blown up by that much.
-    if (!kOutputs || b + 1 < blocks || (last && so >= 0)) {
-      const int after = behind + valid;
-      const bool fades = kOutputs && (b + 1 == blocks || -log2_decay * after > kMostBehind);
-      if (fades) {
-        const float f = power(log2_decay, after);
-#pragma unroll
-        for (int m = 0; m < 4; ++m)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) S[m][i] *= f;
-      }
-      const float join = power(log2_decay, kOutputs ? (fades ? 0 : -after) : len - (b + 1) * kB);
-      behind = fades ? 0 : after;
-#pragma unroll
-      for (int k2 = 0; k2 < 2; ++k2) {
-        const u32x4 w = __builtin_bit_cast(u32x4, vc[k2]);
-        float x[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = i & 1 ? bf16hi(w[i >> 1]) : bf16lo(w[i >> 1]);
-        if (!kOutputs || valid == kB) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] *= fade[8 * k2 + i] * join;
-        } else {   // the last block: it fades
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] *= power(log2_decay, max(valid - 1 - key_of(8 * k2 + i), 0));
-        }
-        const Terms<3> vx = split<3>(x);
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-          const bf16x8 kk = read_columns(tile + kcol[m][0] + 16 * k2 * kRow, tile + kcol[m][1] + 16 * k2 * kRow);
-          S[m] = mfma(kk, vx.t[2], S[m]);
-          S[m] = mfma(kk, vx.t[1], S[m]);
-          S[m] = mfma(kk, vx.t[0], S[m]);
-        }
-      }
-    }
+    behind = fades ? 0 : after;
     at = at + kStage == kRing ? 0 : at + kStage;
     if constexpr (!kDirect) {
       if (b + 1 < blocks) {
