@@ -616,7 +616,7 @@ s2l::LinearPlan linear_plan(const s2l_batch* b, int32_t hq, int32_t num_cus) {
     }
     const int32_t n = (int32_t)s2l::ceil_div64(c, p.piece_tokens);
     p.pieces += n;
-    if (n > 1) ++p.cut_reqs, p.ws_states += n;
+    if (n > 1) ++p.cut_reqs, p.ws_states += n + 1;
   }
   return p;
 }

@@ -120,7 +120,7 @@ struct LinearLaunch {        // linear attention (linear_attn.hip)
   const int32_t *slot_in, *slot_out, *chunk_lens, *cu_chunk;
   int32_t num_slots, num_reqs, hq, hkv;
   float scale;
-  float* ws;                 // [ws_states][hq][128][128]: states before the pieces of cut requests
+  float* ws;                 // [ws_states][hq][128][128]: states around the pieces of cut requests
   int32_t piece_tokens, ws_states, num_units;   // from the plan, per launch
 };
 // Requests of at most kLinearShortTokens new tokens are advanced token by token, the others in blocks.
@@ -128,7 +128,7 @@ constexpr int32_t kLinearShortTokens = 16, kLinearBlockTokens = 32;
 struct LinearPlan {          // how the batch is cut, from the host lengths
   int32_t piece_tokens;      // longer requests are cut into pieces of so many tokens (a multiple of a block)
   int32_t pieces;            // of all requests that are not short
-  int32_t cut_reqs, ws_states;   // requests of more than one piece, and their pieces
+  int32_t cut_reqs, ws_states;   // requests of more than one piece; one state before, between and after them
   int32_t short_reqs;
 };
 hipError_t launch_linear_attn(const LinearLaunch& a, const LinearPlan& plan, hipStream_t stream);

@@ -58,8 +58,8 @@ __device__ inline int32_t wave_scan(int32_t x) {
 }
 
 // The idx-th of the batch's units, 64 requests at a time.  Units are the short requests (kShort), or the
-// pieces of the others: all, or (kInner) all but each cut request's last.
-enum Units { kShort, kPieces, kInner };
+// pieces of the others: of all, or (kCutPieces) of those that are cut.
+enum Units { kShort, kPieces, kCutPieces };
 template <Units kUnits>
 __device__ inline Piece find_unit(const LinearLaunch& a, int32_t idx) {
   const int lane = threadIdx.x & 63;
@@ -67,9 +67,9 @@ __device__ inline Piece find_unit(const LinearLaunch& a, int32_t idx) {
   for (int32_t r0 = 0; r0 < a.num_reqs; r0 += 64) {
     const int32_t len = r0 + lane < a.num_reqs ? a.chunk_lens[r0 + lane] : -1;
     const int32_t pieces = len > kLinearShortTokens ? (len + a.piece_tokens - 1) / a.piece_tokens : 0;
-    const int32_t cut = pieces > 1 ? pieces : 0;
-    const int32_t mine = kUnits == kShort ? (len >= 0 && len <= kLinearShortTokens) : kUnits == kPieces ? pieces : cut ? cut - 1 : 0;
-    const int32_t sum = wave_scan(mine), ws_sum = kUnits == kShort ? 0 : wave_scan(cut);
+    const int32_t cut = pieces > 1 ? pieces : 0, entries = cut ? cut + 1 : 0;   // workspace entries
+    const int32_t mine = kUnits == kShort ? (len >= 0 && len <= kLinearShortTokens) : kUnits == kPieces ? pieces : cut;
+    const int32_t sum = wave_scan(mine), ws_sum = kUnits == kShort ? 0 : wave_scan(entries);
     const int32_t total = __builtin_amdgcn_readlane(sum, 63);
     if (idx < total) {
       const int32_t c = __popcll(__ballot(sum <= idx));
@@ -77,7 +77,7 @@ __device__ inline Piece find_unit(const LinearLaunch& a, int32_t idx) {
       p.req = r0 + c;
       p.len = __builtin_amdgcn_readlane(len, c);
       p.seg = idx - (__builtin_amdgcn_readlane(sum, c) - __builtin_amdgcn_readlane(mine, c));
-      p.ws = ws + __builtin_amdgcn_readlane(ws_sum, c) - __builtin_amdgcn_readlane(cut, c);
+      p.ws = ws + __builtin_amdgcn_readlane(ws_sum, c) - __builtin_amdgcn_readlane(entries, c);
       return p;
     }
     idx -= total;
@@ -203,7 +203,7 @@ __device__ inline Terms<kTerms> split(float* x) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       w[j] = pack_bf16x2(x[2 * j], x[2 * j + 1]);
-      if (i + 1 < kTerms) take_off(w[j], x[2 * j], x[2 * j + 1]);
+      take_off(w[j], x[2 * j], x[2 * j + 1]);   // unused after the last: gone
     }
     r.t[i] = __builtin_bit_cast(bf16x8, w);
   }
@@ -221,29 +221,16 @@ template <int kNewer>
 __device__ inline void tile_barrier() {
   __asm__ volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kNewer) : "memory");
 }
+// What the workgroup's waves wrote to LDS is there.
+__device__ inline void lds_barrier() { __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// Order of a basic block for the scheduler: kMfma times an MFMA, LDS reads and VALU work to go beside it.
-template <int kMfma, int kValu, int kReads>
-__device__ inline void interleave() {
-#pragma unroll
-  for (int i = 0; i < kMfma; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(0x002, kValu, 0);
-  }
-}
-
-// The lanes (n, half) whose query n sees key 16 (i / 8) + 8 (i / 4 % 2) + 4 half + i % 4 of its block.
-__device__ constexpr uint64_t causal_lanes(int i) {
-  const int key = 16 * (i >> 3) + 8 * ((i >> 2) & 1) + (i & 3);
-  return (uint64_t)(0xFFFFFFFFu << key) | (uint64_t)(0xFFFFFFFFu << (key + 4)) << 32;
-}
-
-// kOutputs: the blocks of all pieces, with outputs and, of a request's last piece, its state.
-// Otherwise the own states of all pieces but the last, and (piece 0) a copy of the request's state.
+// kOutputs: the blocks of all pieces, with outputs; of requests that are not cut, the state after them too.
+// Otherwise what each piece of a cut request alone makes of its tokens (piece 0: of the request's state
+// too), and a copy of the request's state.
 // kDirect: tiles are copied straight into LDS, kStages - 1 blocks ahead; rows at addresses or strides that
 // those copies do not take go through registers, one block ahead.
 constexpr double kMostBehind = 60.0;
+constexpr int kScoreRow = 80;            // bytes of a query's row of scores: 32 bf16 and a pad off the same banks
 template <bool kOutputs, bool kDirect>
 __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
   constexpr int kTiles = kOutputs ? 3 : 2;             // K, V, Q
@@ -251,6 +238,7 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
   constexpr int kStage = kTiles * kTile, kRing = kStages * kStage;
   constexpr int kCopies = 2 * kTiles, kStores = kOutputs ? 2 : 0;   // a wave's, for a block
   __shared__ __attribute__((aligned(1024))) uint8_t s_ring[kRing];
+  __shared__ __attribute__((aligned(16))) uint8_t s_score[2][kOutputs ? kB * kScoreRow : 16];   // two terms
   __shared__ int32_t s_bad[4][32];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5, n = lane & 31;
@@ -260,16 +248,16 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
   const int h0 = (int)(blockIdx.x / 8) % group;
   if (unit >= a.num_units * a.hkv) return;
   const int g = unit % a.hkv, h = g * group + h0;
-  Piece p = find_unit<kOutputs ? kPieces : kInner>(a, unit / a.hkv);
+  Piece p = find_unit<kOutputs ? kPieces : kCutPieces>(a, unit / a.hkv);
   if (p.req < 0) return;
   p.req = __builtin_amdgcn_readfirstlane(p.req);
   p.seg = __builtin_amdgcn_readfirstlane(p.seg);
   p.len = __builtin_amdgcn_readfirstlane(p.len);
   p.ws = __builtin_amdgcn_readfirstlane(p.ws);
   const int pieces = (p.len + a.piece_tokens - 1) / a.piece_tokens;
+  const bool cut = pieces > 1;
   const int first = p.seg * a.piece_tokens, len = min(a.piece_tokens, p.len - first);
-  const bool last = p.seg == pieces - 1;
-  if (pieces > 1 && p.ws + pieces > a.ws_states) return;   // as above: more than the host copies hold
+  if (cut && p.ws + pieces >= a.ws_states) return;   // as above: more than the host copies hold
   const int64_t row0 = (int64_t)a.cu_chunk[p.req] + first;
   const int si = a.slot_in[p.req], so = a.slot_out[p.req];
   const int64_t slot = (int64_t)a.hq * kState;
@@ -332,31 +320,37 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
     load(0);
   }
 
-  // operand addresses within a stage; chunk bits are apart from the rest, so other chunks are an exclusive or away
+  // Operand addresses within a stage; chunk bits are apart from the rest, so other chunks are an exclusive or away.
   const int rows = n * kRow + ((half ^ perm(n)) << 4);   // row n, dims 16 s + 8 half .. + 7: ^ s << 5
-  const int j = lane & 15, b4 = (lane >> 4) & 1, trow = 4 * half + (j >> 2);
-  int kcol[2], vcol[2];       // rows + 0, + 8; state tile m: ^ m << 6
+  const int j = lane & 15, b4 = (lane >> 4) & 1, trow = 8 * half + (j >> 2);
+  int kcol[2], vcol[2];       // rows + 0, + 4 of 8 half; state tile m: ^ m << 6
 #pragma unroll
   for (int y = 0; y < 2; ++y) {
-    const int row = trow + 8 * y;
+    const int row = trow + 4 * y;
     kcol[y] = row * kRow + (((2 * b4 + (j & 1)) ^ perm(row)) << 4) + 8 * ((j >> 1) & 1);
     vcol[y] = kTile + row * kRow + (((4 * wave + 2 * b4 + ((j >> 1) & 1)) ^ perm(row)) << 4) + 8 * (j & 1);
   }
+  // scores: this wave's 16 queries by 16 keys, lane (j, quarter) dims 32 s + 8 quarter .. + 7 of row j: ^ s << 6;
+  // the results are keys key0 .. + 3 of query0
+  const int quarter = lane >> 4, query0 = 16 * (wave >> 1) + j, key0 = 16 * (wave & 1) + 4 * quarter;
+  const int krow = (16 * (wave & 1) + j) * kRow + ((quarter ^ perm(j)) << 4);
+  const int qrow = 2 * kTile + query0 * kRow + ((quarter ^ perm(j)) << 4);
 
   const double log_decay = clean_log(a.log_decay[h]), log2_decay = log_decay * 1.4426950408889634;
-  auto key_of = [&](int i) { return 16 * (i >> 3) + 8 * ((i >> 2) & 1) + 4 * half + (i & 3); };
-  float within[16], fade[16];   // scale l^(i-j); l^(kB-1-j)
+  auto key_of = [&](int i) { return 16 * (i >> 3) + 8 * half + (i & 7); };   // of a column operand's element
+  float within[4], fade[16];   // scale l^(query - key), 0 for later keys; l^(kB-1-key)
+  if constexpr (kOutputs) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    if constexpr (kOutputs) within[i] = n >= key_of(i) ? a.scale * power(log2_decay, n - key_of(i)) : 0.f;
-    fade[i] = power(log2_decay, kB - 1 - key_of(i));
+    for (int i = 0; i < 4; ++i) within[i] = query0 >= key0 + i ? a.scale * power(log2_decay, query0 - key0 - i) : 0.f;
   }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) fade[i] = power(log2_decay, kB - 1 - key_of(i));
   const float since = a.scale * power(log2_decay, n + 1);
 
   // state: register (m, i) is key dim 32 m + dim(i), column 32 wave + n
   auto dim = [&](int i) { return 16 * (i >> 3) + 8 * half + 4 * ((i >> 2) & 1) + (i & 3); };
   f32x16 S[4];
-  const bool own_state = kOutputs ? pieces == 1 : p.seg == 0;   // the request's, not the workspace's or none
+  const bool own_state = kOutputs ? !cut : p.seg == 0;   // the request's, not the workspace's or none
   const float* from = own_state ? (si >= 0 && si < a.num_slots ? a.states + si * slot + (int64_t)h * kState : nullptr)
                       : kOutputs ? ws : nullptr;
   const float none = !own_state || si == -1 ? 0.f : __builtin_nanf("");
@@ -390,9 +384,9 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
       if (b + kStages - 1 < blocks) copy(b + kStages - 1, at == 0 ? kRing - kStage : at - kStage);
       __asm__ volatile("" ::: "memory");   // the block's stores are younger than the copies
     } else {
-      __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      lds_barrier();
     }
-    const int valid = kOutputs ? min(kB, len - b * kB) : kB;
+    const int valid = min(kB, len - nth(b) * kB);
     const uint8_t* const tile = s_ring;
     const bf16x8 vc[2] = {read_columns(tile + at + vcol[0], tile + at + vcol[1]),
                           read_columns(tile + at + vcol[0] + 16 * kRow, tile + at + vcol[1] + 16 * kRow)};
@@ -403,11 +397,16 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
     // by as much.
     const int after = behind + valid;
     const bool fades = kOutputs && (b + 1 == blocks || -log2_decay * after > kMostBehind);
-    const float join = power(log2_decay, kOutputs ? (fades ? 0 : -after) : len - (nth(b) + 1) * kB);
-    if (kOutputs && valid < kB) {   // the last block
+    float f[16];
+    if (valid == kB) {
+      const float join = power(log2_decay, kOutputs ? (fades ? 0 : -after) : len - (nth(b) + 1) * kB);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) fade[i] = power(log2_decay, max(valid - 1 - key_of(i), 0));
+      for (int i = 0; i < 16; ++i) f[i] = fade[i] * join;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) f[i] = power(log2_decay, max(valid - 1 - key_of(i), 0));
     }
+
     bool bad = false;
     if constexpr (kOutputs) {
       // A value of v that is not finite is no matter of the rows before it: 0 in their sums, and NaN put
@@ -431,68 +430,77 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
         if (half == 0) s_bad[wave][n] = from_row;
         __builtin_amdgcn_wave_barrier();
       }
+
+      // this wave's quarter of the scores
+      f32x4 sc{};
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(read_row(tile + ((at + krow) ^ s << 6)), read_row(tile + ((at + qrow) ^ s << 6)), sc, 0, 0, 0);
+      float y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = query0 >= key0 + i ? sc[i] * within[i] : 0.f;
+      uint8_t* const to = s_score[0] + query0 * kScoreRow + key0 * 2;
+      const uint32_t w0 = pack_bf16x2(y[0], y[1]), w1 = pack_bf16x2(y[2], y[3]);
+      *reinterpret_cast<u32x2*>(to) = u32x2{w0, w1};
+      take_off(w0, y[0], y[1]);
+      take_off(w1, y[2], y[3]);
+      *reinterpret_cast<u32x2*>(to + kB * kScoreRow) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
     }
 
-    Terms<3> vx[2];
+    constexpr int kTerms = kOutputs ? 2 : 3;   // for outputs, in bf16 in the end, two will do
+    float x[2][8];
+    Terms<kTerms> vx[2];
 #pragma unroll
     for (int k2 = 0; k2 < 2; ++k2) {
       const u32x4 w = __builtin_bit_cast(u32x4, vc[k2]);
-      float x[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = (i & 1 ? bf16hi(w[i >> 1]) : bf16lo(w[i >> 1])) * (fade[8 * k2 + i] * join);
-      vx[k2] = split<3>(x);
+      for (int i = 0; i < 8; ++i) x[k2][i] = (i & 1 ? bf16hi(w[i >> 1]) : bf16lo(w[i >> 1])) * f[8 * k2 + i];
+      vx[k2] = split<kTerms>(x[k2]);
     }
-
-    f32x16 p16{}, o{};
+    f32x16 o{};
     if constexpr (kOutputs) {
       const int row = at + rows;
 #pragma unroll
       for (int s = 0; s < 8; ++s) {
         const bf16x8 q = read_row(tile + 2 * kTile + (row ^ s << 5));
-        p16 = mfma(read_row(tile + (row ^ s << 5)), q, p16);
-        float x[8];
+        float z[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = S[s >> 1][8 * (s & 1) + i];
-        const Terms<2> sx = split<2>(x);
+        for (int i = 0; i < 8; ++i) z[i] = S[s >> 1][8 * (s & 1) + i];
+        const Terms<2> sx = split<2>(z);
         o = mfma(sx.t[1], q, o);
         o = mfma(sx.t[0], q, o);
       }
-      interleave<24, 9, 1>();
-    }
-    if (fades) {
-      const float f = power(log2_decay, after);
+      if (fades) {
+        const float by = power(log2_decay, after);
 #pragma unroll
-      for (int m = 0; m < 4; ++m)
+        for (int m = 0; m < 4; ++m)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) S[m][i] *= f;
-    }
-#pragma unroll
-    for (int k2 = 0; k2 < 2; ++k2)
-#pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        const bf16x8 kk = read_columns(tile + ((at + kcol[0]) ^ m << 6) + 16 * k2 * kRow, tile + ((at + kcol[1]) ^ m << 6) + 16 * k2 * kRow);
-        S[m] = mfma(kk, vx[k2].t[2], S[m]);
-        S[m] = mfma(kk, vx[k2].t[1], S[m]);
-        S[m] = mfma(kk, vx[k2].t[0], S[m]);
+          for (int i = 0; i < 16; ++i) S[m][i] *= by;
       }
+      lds_barrier();   // all quarters of the scores
+    }
+    auto join_state = [&](const bf16x8* terms0, const bf16x8* terms1, int count) {
+#pragma unroll
+      for (int k2 = 0; k2 < 2; ++k2)
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          const bf16x8 kk = read_columns(tile + ((at + kcol[0]) ^ m << 6) + 16 * k2 * kRow, tile + ((at + kcol[1]) ^ m << 6) + 16 * k2 * kRow);
+#pragma unroll
+          for (int i = count - 1; i >= 0; --i) S[m] = mfma(kk, (k2 ? terms1 : terms0)[i], S[m]);
+        }
+    };
+    join_state(vx[0].t, vx[1].t, kTerms);
     if constexpr (kOutputs) {
       const float reach = since * power(log2_decay, behind);
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[i] *= reach;
 #pragma unroll
       for (int k2 = 0; k2 < 2; ++k2) {
-        float x[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float y = p16[8 * k2 + i] * within[8 * k2 + i];
-          x[i] = __builtin_amdgcn_inverse_ballot_w64(causal_lanes(8 * k2 + i)) ? y : 0.f;
-        }
-        const Terms<2> pt = split<2>(x);
+        const uint8_t* sr = s_score[0] + n * kScoreRow + 32 * k2 + 16 * half;
         const bf16x8 vv = __builtin_bit_cast(bf16x8, vw[k2]);
-        o = mfma(vv, pt.t[1], o);
-        o = mfma(vv, pt.t[0], o);
+        o = mfma(vv, read_row(sr + kB * kScoreRow), o);
+        o = mfma(vv, read_row(sr), o);
       }
-      interleave<28, 4, 1>();
       if (bad) {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
@@ -514,6 +522,10 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
         *reinterpret_cast<u32x4_any*>(dst) = y[0];
         *reinterpret_cast<u32x4_any*>(dst + 16) = y[1];
       }
+      if (!cut) {              // this state is what the call returns: the third term too
+        Terms<1> rest[2] = {split<1>(x[0]), split<1>(x[1])};
+        join_state(rest[0].t, rest[1].t, 1);
+      }
     }
     behind = fades ? 0 : after;
     at = at + kStage == kRing ? 0 : at + kStage;
@@ -525,7 +537,7 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
     }
   }
 
-  float* to = !kOutputs ? ws + slot : last && so >= 0 && so < a.num_slots ? a.states + so * slot + (int64_t)h * kState : nullptr;
+  float* to = !kOutputs ? ws + slot : !cut && so >= 0 && so < a.num_slots ? a.states + so * slot + (int64_t)h * kState : nullptr;
   if (to) {
 #pragma unroll
     for (int m = 0; m < 4; ++m)
@@ -534,40 +546,48 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
   }
 }
 
-// The states before the pieces of cut requests: workspace entry s + 1 of a request holds what piece s
-// alone makes of its tokens (piece 0: of the request's state too), and gets the sum with the entry before it, faded by
-// piece s.  A thread takes four elements of one head's states through all pieces.
+// The states between the pieces of cut requests: workspace entry s + 1 of a request holds what piece s
+// alone makes of its tokens (piece 0: of the request's state too), and gets the sum with the entry before it, faded
+// by piece s; the last one goes to the request's slot.  A thread takes four elements of one head's
+// states through all pieces.
 __global__ __launch_bounds__(256) void linear_carry_kernel(LinearLaunch a) {
   const int h = blockIdx.y;
   const int lane = threadIdx.x & 63;
   // the blockIdx.z-th cut request
-  int32_t idx = blockIdx.z, ws = 0, pieces = 0;
+  int32_t idx = blockIdx.z, ws = 0, pieces = 0, req = 0, len = 0;
   for (int32_t r0 = 0; r0 < a.num_reqs; r0 += 64) {
-    const int32_t len = r0 + lane < a.num_reqs ? a.chunk_lens[r0 + lane] : -1;
-    const int32_t cut = len > kLinearShortTokens && len > a.piece_tokens ? (len + a.piece_tokens - 1) / a.piece_tokens : 0;
+    const int32_t l = r0 + lane < a.num_reqs ? a.chunk_lens[r0 + lane] : -1;
+    const int32_t cut = l > kLinearShortTokens && l > a.piece_tokens ? (l + a.piece_tokens - 1) / a.piece_tokens : 0;
+    const int32_t entries = cut ? cut + 1 : 0;
     const uint64_t is = __ballot(cut > 0);
-    const int32_t total = __popcll(is), sum = wave_scan(cut);
+    const int32_t total = __popcll(is), sum = wave_scan(entries);
     if (idx < total) {
       const uint64_t here = __ballot(cut > 0 && __popcll(is & (((uint64_t)1 << lane) - 1)) == idx);
       const int32_t c = __builtin_ctzll(here);
       pieces = __builtin_amdgcn_readlane(cut, c);
-      ws += __builtin_amdgcn_readlane(sum, c) - pieces;
+      len = __builtin_amdgcn_readlane(l, c);
+      ws += __builtin_amdgcn_readlane(sum, c) - pieces - 1;
+      req = r0 + c;
       break;
     }
     idx -= total;
     ws += __builtin_amdgcn_readlane(sum, 63);
   }
-  if (pieces == 0 || ws + pieces > a.ws_states) return;
-  const float fade = (float)exp(clean_log(a.log_decay[h]) * a.piece_tokens);
-  const int64_t slot = (int64_t)a.hq * kState;
-  f32x4* p = reinterpret_cast<f32x4*>(a.ws + ws * slot + (int64_t)h * kState) + blockIdx.x * 256 + threadIdx.x;
+  if (pieces == 0 || ws + pieces >= a.ws_states) return;
+  const double log_decay = clean_log(a.log_decay[h]);
+  const float fade = (float)exp(log_decay * a.piece_tokens), fade_last = (float)exp(log_decay * (len - (pieces - 1) * a.piece_tokens));
+  const int so = a.slot_out[req];
+  const int64_t slot = (int64_t)a.hq * kState, at = (int64_t)h * kState / 4 + blockIdx.x * 256 + threadIdx.x;
+  f32x4* p = reinterpret_cast<f32x4*>(a.ws + ws * slot) + at;
   f32x4 sum = p[slot / 4];
-  for (int s = 2; s < pieces; ++s) {
+  for (int s = 2; s <= pieces; ++s) {
     f32x4 x = p[s * (slot / 4)];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = __builtin_fmaf(sum[i], fade, x[i]);
-    p[s * (slot / 4)] = sum = x;
+    for (int i = 0; i < 4; ++i) x[i] = __builtin_fmaf(sum[i], s < pieces ? fade : fade_last, x[i]);
+    if (s < pieces) p[s * (slot / 4)] = x;
+    sum = x;
   }
+  if (so >= 0 && so < a.num_slots) reinterpret_cast<f32x4*>(a.states + so * slot)[at] = sum;
 }
 
 }  // namespace
@@ -584,7 +604,7 @@ hipError_t launch_linear_attn(const LinearLaunch& launch, const LinearPlan& plan
   };
   const bool kv = direct(a.k, a.k_stride) && direct(a.v, a.v_stride), qkv = kv && direct(a.q, a.q_stride);
   if (plan.cut_reqs > 0) {
-    a.num_units = plan.ws_states - plan.cut_reqs;
+    a.num_units = plan.ws_states - plan.cut_reqs;   // their pieces
     if (kv) linear_block_kernel<false, true><<<blocks(a.num_units), 256, 0, stream>>>(a);
     else linear_block_kernel<false, false><<<blocks(a.num_units), 256, 0, stream>>>(a);
     linear_carry_kernel<<<dim3(kState / 1024, a.hq, plan.cut_reqs), 256, 0, stream>>>(a);
