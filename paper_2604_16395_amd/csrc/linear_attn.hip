@@ -44,20 +44,22 @@ __device__ inline float power(double log2_decay, int n) { return __builtin_amdgc
 struct Piece {
   int32_t req, seg, len;        // len: the request's tokens
   int32_t ws;                   // workspace index of the request's first piece
+  int32_t row, slot_in, slot_out;   // of the request
 };
 
-// Inclusive sum over the lanes of a wave.
+// Inclusive sum over the lanes of a wave: within rows of 16 lanes, then across them (lanes that a step gives
+// nothing add 0).
 __device__ inline int32_t wave_scan(int32_t x) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int32_t y = __shfl_up(x, d, 64);
-    x += lane >= d ? y : 0;
-  }
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);   // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);   // row_bcast:15 into rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);   // row_bcast:31 into rows 2 and 3
   return x;
 }
 
-// The idx-th of the batch's units, 64 requests at a time.  Units are the short requests (kShort), or the
+// The idx-th of the batch's units, 64 requests at a time, all that is known of them in one round of loads.  Units are the short requests (kShort), or the
 // pieces of the others: of all, or (kCutPieces) of those that are cut.
 enum Units { kShort, kPieces, kCutPieces };
 template <Units kUnits>
@@ -65,7 +67,9 @@ __device__ inline Piece find_unit(const LinearLaunch& a, int32_t idx) {
   const int lane = threadIdx.x & 63;
   int32_t ws = 0;
   for (int32_t r0 = 0; r0 < a.num_reqs; r0 += 64) {
-    const int32_t len = r0 + lane < a.num_reqs ? a.chunk_lens[r0 + lane] : -1;
+    const int32_t r = r0 + lane < a.num_reqs ? r0 + lane : r0;
+    const int32_t row = a.cu_chunk[r], slot_in = a.slot_in[r], slot_out = a.slot_out[r], l = a.chunk_lens[r];
+    const int32_t len = r0 + lane < a.num_reqs ? l : -1;
     const int32_t pieces = len > kLinearShortTokens ? (len + a.piece_tokens - 1) / a.piece_tokens : 0;
     const int32_t cut = pieces > 1 ? pieces : 0, entries = cut ? cut + 1 : 0;   // workspace entries
     const int32_t mine = kUnits == kShort ? (len >= 0 && len <= kLinearShortTokens) : kUnits == kPieces ? pieces : cut;
@@ -78,12 +82,15 @@ __device__ inline Piece find_unit(const LinearLaunch& a, int32_t idx) {
       p.len = __builtin_amdgcn_readlane(len, c);
       p.seg = idx - (__builtin_amdgcn_readlane(sum, c) - __builtin_amdgcn_readlane(mine, c));
       p.ws = ws + __builtin_amdgcn_readlane(ws_sum, c) - __builtin_amdgcn_readlane(entries, c);
+      p.row = __builtin_amdgcn_readlane(row, c);
+      p.slot_in = __builtin_amdgcn_readlane(slot_in, c);
+      p.slot_out = __builtin_amdgcn_readlane(slot_out, c);
       return p;
     }
     idx -= total;
     ws += __builtin_amdgcn_readlane(ws_sum, 63);
   }
-  return Piece{-1, 0, 0, 0};   // the device lengths hold less than the host copies: nothing to do
+  return Piece{-1, 0, 0, 0, 0, 0, 0};   // the device lengths hold less than the host copies: nothing to do
 }
 
 // ---- recurrent form ----
@@ -101,9 +108,9 @@ __global__ __launch_bounds__(256) void linear_recurrent_kernel(LinearLaunch a) {
   __shared__ float s_part[kLinearShortTokens][4][kSliceCols];
   const Piece p = find_unit<kShort>(a, blockIdx.z);
   if (p.req < 0) return;
-  const int r = p.req, h = blockIdx.y, col0 = (int)blockIdx.x * kSliceCols;
-  const int C = p.len, si = a.slot_in[r], so = a.slot_out[r];
-  const int64_t row0 = a.cu_chunk[r];
+  const int h = blockIdx.y, col0 = (int)blockIdx.x * kSliceCols;
+  const int C = p.len, si = p.slot_in, so = p.slot_out;
+  const int64_t row0 = p.row;
   const int g = h / (a.hq / a.hkv);
   const int vq = threadIdx.x & 7, kg = threadIdx.x >> 3, wave = threadIdx.x >> 6;
   const int64_t at = (int64_t)h * kState + (4 * kg) * 128 + col0 + 4 * vq;   // within a slot
@@ -250,16 +257,16 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
   const int g = unit % a.hkv, h = g * group + h0;
   Piece p = find_unit<kOutputs ? kPieces : kCutPieces>(a, unit / a.hkv);
   if (p.req < 0) return;
-  p.req = __builtin_amdgcn_readfirstlane(p.req);
   p.seg = __builtin_amdgcn_readfirstlane(p.seg);
   p.len = __builtin_amdgcn_readfirstlane(p.len);
   p.ws = __builtin_amdgcn_readfirstlane(p.ws);
+  p.row = __builtin_amdgcn_readfirstlane(p.row);
   const int pieces = (p.len + a.piece_tokens - 1) / a.piece_tokens;
   const bool cut = pieces > 1;
   const int first = p.seg * a.piece_tokens, len = min(a.piece_tokens, p.len - first);
   if (cut && p.ws + pieces >= a.ws_states) return;   // as above: more than the host copies hold
-  const int64_t row0 = (int64_t)a.cu_chunk[p.req] + first;
-  const int si = a.slot_in[p.req], so = a.slot_out[p.req];
+  const int64_t row0 = (int64_t)p.row + first;
+  const int si = __builtin_amdgcn_readfirstlane(p.slot_in), so = __builtin_amdgcn_readfirstlane(p.slot_out);
   const int64_t slot = (int64_t)a.hq * kState;
   float* const ws = a.ws + ((int64_t)p.ws + p.seg) * slot + (int64_t)h * kState;
   const int blocks = (len + kB - 1) / kB;
@@ -580,12 +587,19 @@ __global__ __launch_bounds__(256) void linear_carry_kernel(LinearLaunch a) {
   const int64_t slot = (int64_t)a.hq * kState, at = (int64_t)h * kState / 4 + blockIdx.x * 256 + threadIdx.x;
   f32x4* p = reinterpret_cast<f32x4*>(a.ws + ws * slot) + at;
   f32x4 sum = p[slot / 4];
-  for (int s = 2; s <= pieces; ++s) {
-    f32x4 x = p[s * (slot / 4)];
+  constexpr int kAhead = 8;   // loads do not wait for one another
+  for (int s0 = 2; s0 <= pieces; s0 += kAhead) {
+    f32x4 x[kAhead];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = __builtin_fmaf(sum[i], s < pieces ? fade : fade_last, x[i]);
-    if (s < pieces) p[s * (slot / 4)] = x;
-    sum = x;
+    for (int i = 0; i < kAhead; ++i)
+      if (s0 + i <= pieces) x[i] = p[(s0 + i) * (slot / 4)];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (s0 + i > pieces) break;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) sum[c] = __builtin_fmaf(sum[c], s0 + i < pieces ? fade : fade_last, x[i][c]);
+      if (s0 + i < pieces) p[(s0 + i) * (slot / 4)] = sum;
+    }
   }
   if (so >= 0 && so < a.num_slots) reinterpret_cast<f32x4*>(a.states + so * slot)[at] = sum;
 }
