@@ -237,16 +237,15 @@ __device__ inline void lds_barrier() { __asm__ volatile("s_waitcnt lgkmcnt(0)\n\
 // kDirect: tiles are copied straight into LDS, kStages - 1 blocks ahead; rows at addresses or strides that
 // those copies do not take go through registers, one block ahead.
 constexpr double kMostBehind = 60.0;
-constexpr int kScoreRow = 80;            // bytes of a query's row of scores: 32 bf16 and a pad off the same banks
+constexpr int kScores = kB * 2 * kB;     // bytes of a block's scores in one term: rows of a query's 32 bf16
 template <bool kOutputs, bool kDirect>
 __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
   constexpr int kTiles = kOutputs ? 3 : 2;             // K, V, Q
-  constexpr int kStages = kDirect ? (kOutputs ? 3 : 4) : 2;
+  constexpr int kStages = kOutputs ? 3 : kDirect ? 4 : 2;
   constexpr int kStage = kTiles * kTile, kRing = kStages * kStage;
-  constexpr int kCopies = 2 * kTiles, kStores = kOutputs ? 2 : 0;   // a wave's, for a block
+  constexpr int kCopies = 2 * kTiles, kStores = 2;   // a wave's, for a block
   __shared__ __attribute__((aligned(1024))) uint8_t s_ring[kRing];
-  __shared__ __attribute__((aligned(16))) uint8_t s_score[2][kOutputs ? kB * kScoreRow : 16];   // two terms
-  __shared__ int32_t s_bad[4][32];
+  __shared__ __attribute__((aligned(1024))) uint8_t s_score[kOutputs ? 4 * kScores : 16];   // two blocks' two terms
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5, n = lane & 31;
   const int group = a.hq / a.hkv;
@@ -338,10 +337,15 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
     vcol[y] = kTile + row * kRow + (((4 * wave + 2 * b4 + ((j >> 1) & 1)) ^ perm(row)) << 4) + 8 * (j & 1);
   }
   // scores: this wave's 16 queries by 16 keys, lane (j, quarter) dims 32 s + 8 quarter .. + 7 of row j: ^ s << 6;
-  // the results are keys key0 .. + 3 of query0
+  // the results are keys key0 .. + 3 of query0.  A query's row lies with its 16-byte chunks permuted by query / 4, so
+  // that 16 queries put one chunk on all banks.
   const int quarter = lane >> 4, query0 = 16 * (wave >> 1) + j, key0 = 16 * (wave & 1) + 4 * quarter;
   const int krow = (16 * (wave & 1) + j) * kRow + ((quarter ^ perm(j)) << 4);
   const int qrow = 2 * kTile + query0 * kRow + ((quarter ^ perm(j)) << 4);
+  const int score_to = query0 * 2 * kB + (((key0 >> 3) ^ ((query0 >> 2) & 3)) << 4) + 8 * (quarter & 1);
+  int score_from[2];          // keys 16 k2 + 8 half .. + 7 of query n
+#pragma unroll
+  for (int k2 = 0; k2 < 2; ++k2) score_from[k2] = n * 2 * kB + (((2 * k2 + half) ^ ((n >> 2) & 3)) << 4);
 
   const double log_decay = clean_log(a.log_decay[h]), log2_decay = log_decay * 1.4426950408889634;
   auto key_of = [&](int i) { return 16 * (i >> 3) + 8 * half + (i & 7); };   // of a column operand's element
@@ -379,19 +383,50 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
   if constexpr (!kDirect) {
     store(0);
     if (1 < blocks) load(1);
+    if (kOutputs && 1 < blocks) {
+      store(kStage);
+      if (2 < blocks) load(2);
+    }
+  }
+  // This wave's quarter of a block's scores, in two terms.
+  auto scores = [&](int stage, int parity) {
+    f32x4 sc{};
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(read_row(s_ring + ((stage + krow) ^ s << 6)), read_row(s_ring + ((stage + qrow) ^ s << 6)), sc, 0, 0, 0);
+    float y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = query0 >= key0 + i ? sc[i] * within[i] : 0.f;
+    uint8_t* const to = s_score + 2 * kScores * parity + score_to;
+    const uint32_t w0 = pack_bf16x2(y[0], y[1]), w1 = pack_bf16x2(y[2], y[3]);
+    *reinterpret_cast<u32x2*>(to) = u32x2{w0, w1};
+    take_off(w0, y[0], y[1]);
+    take_off(w1, y[2], y[3]);
+    *reinterpret_cast<u32x2*>(to + kScores) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+  };
+  if constexpr (kOutputs) {
+    if (kDirect && blocks > 1) tile_barrier<kCopies>();
+    else if (kDirect) tile_barrier<0>();
+    else lds_barrier();
+    scores(0, 0);
   }
   int behind = 0;      // tokens that S has yet to fade by: the state is l^behind S
   int at = 0;          // the block's stage
   for (int b = 0; b < blocks; ++b) {
-    if constexpr (kDirect) {
+    // With outputs the next block's tile has to be there too, for its scores.
+    if constexpr (!kDirect) lds_barrier();
+    else if constexpr (kOutputs) {
+      if (b == 0) tile_barrier<0>();
+      else if (b + 1 < blocks) tile_barrier<kStores>();
+      else lds_barrier();
+    } else {
       if (b + kStages - 2 >= blocks) tile_barrier<0>();
-      else if (b < kStages - 1) tile_barrier<(kStages - 2) * kCopies>();
-      else tile_barrier<(kStages - 2) * kCopies + (kStages - 1) * kStores>();
+      else tile_barrier<(kStages - 2) * kCopies>();
+    }
+    if constexpr (kDirect) {
       // the stage before this one's is read out
       if (b + kStages - 1 < blocks) copy(b + kStages - 1, at == 0 ? kRing - kStage : at - kStage);
       __asm__ volatile("" ::: "memory");   // the block's stores are younger than the copies
-    } else {
-      lds_barrier();
     }
     const int valid = min(kB, len - nth(b) * kB);
     const uint8_t* const tile = s_ring;
@@ -415,6 +450,7 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
     }
 
     bool bad = false;
+    int bad_row = kB;    // the first such row of column n
     if constexpr (kOutputs) {
       // A value of v that is not finite is no matter of the rows before it: 0 in their sums, and NaN put
       // into the rows from its own on.  (0 times it is NaN, 0 times any other 0.)
@@ -433,25 +469,10 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
             vw[i >> 3][(i >> 1) & 3] = w & (i & 1 ? 0x0000FFFFu : 0xFFFF0000u);
           }
         }
-        from_row = min(from_row, __shfl_xor(from_row, 32, 64));
-        if (half == 0) s_bad[wave][n] = from_row;
-        __builtin_amdgcn_wave_barrier();
+        bad_row = min(from_row, __shfl_xor(from_row, 32, 64));
       }
-
-      // this wave's quarter of the scores
-      f32x4 sc{};
-#pragma unroll
-      for (int s = 0; s < 4; ++s)
-        sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(read_row(tile + ((at + krow) ^ s << 6)), read_row(tile + ((at + qrow) ^ s << 6)), sc, 0, 0, 0);
-      float y[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = query0 >= key0 + i ? sc[i] * within[i] : 0.f;
-      uint8_t* const to = s_score[0] + query0 * kScoreRow + key0 * 2;
-      const uint32_t w0 = pack_bf16x2(y[0], y[1]), w1 = pack_bf16x2(y[2], y[3]);
-      *reinterpret_cast<u32x2*>(to) = u32x2{w0, w1};
-      take_off(w0, y[0], y[1]);
-      take_off(w1, y[2], y[3]);
-      *reinterpret_cast<u32x2*>(to + kB * kScoreRow) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+      // the next block's scores (of a block that there is not: of what lies there, and not used)
+      scores(at + kStage == kRing ? 0 : at + kStage, (b + 1) & 1);
     }
 
     constexpr int kTerms = kOutputs ? 2 : 3;   // for outputs, in bf16 in the end, two will do
@@ -484,7 +505,6 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) S[m][i] *= by;
       }
-      lds_barrier();   // all quarters of the scores
     }
     auto join_state = [&](const bf16x8* terms0, const bf16x8* terms1, int count) {
 #pragma unroll
@@ -503,15 +523,15 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
       for (int i = 0; i < 16; ++i) o[i] *= reach;
 #pragma unroll
       for (int k2 = 0; k2 < 2; ++k2) {
-        const uint8_t* sr = s_score[0] + n * kScoreRow + 32 * k2 + 16 * half;
+        const uint8_t* sr = s_score + 2 * kScores * (b & 1) + score_from[k2];
         const bf16x8 vv = __builtin_bit_cast(bf16x8, vw[k2]);
-        o = mfma(vv, read_row(sr + kB * kScoreRow), o);
+        o = mfma(vv, read_row(sr + kScores), o);
         o = mfma(vv, read_row(sr), o);
       }
       if (bad) {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (n >= s_bad[wave][8 * (i >> 2) + 4 * half + (i & 3)]) o[i] = __builtin_nanf("");
+          if (n >= __shfl(bad_row, 8 * (i >> 2) + 4 * half + (i & 3), 64)) o[i] = __builtin_nanf("");
       }
       // lane (n, half) holds columns 8 c + 4 half + 0 .. 3 of row n: exchanged to eight in a row
       uint16_t* dst = a.out + (row0 + b * kB + n) * a.out_stride + h * 128 + 32 * wave + 8 * half;
@@ -537,9 +557,10 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
     behind = fades ? 0 : after;
     at = at + kStage == kRing ? 0 : at + kStage;
     if constexpr (!kDirect) {
-      if (b + 1 < blocks) {
-        store(at);
-        if (b + 2 < blocks) load(b + 2);
+      constexpr int kAhead = kOutputs ? 2 : 1;
+      if (b + kAhead < blocks) {
+        store(kOutputs ? (at + kStage == kRing ? 0 : at + kStage) : at);
+        if (b + kAhead + 1 < blocks) load(b + kAhead + 1);
       }
     }
   }
