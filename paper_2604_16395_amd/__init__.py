@@ -237,7 +237,8 @@ def _load_native():
         # a torch without GPU support lacks the last two: no current stream, so the ctypes path
         device, raw_stream = (getattr(torch._C, n, None) for n in ("_cuda_getDevice", "_cuda_getCurrentRawStream"))
         _native = _lib.binding((torch.Tensor, PagedKVCache, Batch, s2l_plan_opts, s2l_plan_info, torch.cuda.Stream,
-                                torch.bfloat16, torch.float32, torch.uint8, torch.cuda.is_initialized, device, raw_stream))
+                                torch.bfloat16, torch.float32, torch.uint8, torch.cuda.is_initialized, device, raw_stream,
+                                Rope, LinearState, torch.int32))
     return _native
 
 
@@ -279,6 +280,9 @@ def _same_heads(a, b, what):
 def s2l_rope_qk(batch, rope, q, q_out, k=None, k_out=None, stream=None):
     """Rotate the batch's query rows q into q_out and its key rows k (if any) into k_out: bf16
     [rows][heads][128], rows at any stride; an output may be its own input."""
+    st = (_native or _load_native()).rope_qk(batch, rope, q, q_out, k, k_out, stream)
+    if st is not None:
+        return _lib.failed("s2l_rope_qk", st) if st else None
     qp, qs, hq = _rows(q, "q", batch)
     op, os_, ho = _rows(q_out, "q_out", batch)
     _same_heads(hq, ho, "q and q_out")
@@ -294,6 +298,9 @@ def s2l_rope_qk(batch, rope, q, q_out, k=None, k_out=None, stream=None):
 def s2l_rope_kv_append(cache, batch, rope, q, q_out, k, v, stream=None):
     """s2l_kv_append of the rotated keys and of the values, with the rotated queries in q_out (q and
     q_out None: none), in one launch; tensors as for s2l_rope_qk."""
+    st = (_native or _load_native()).rope_append(cache, batch, rope, q, q_out, k, v, stream)
+    if st is not None:
+        return _lib.failed("s2l_rope_kv_append", st) if st else None
     qp, qs, hq, op, os_ = None, 0, 0, None, 0
     if q is not None:
         qp, qs, hq = _rows(q, "q", batch)
@@ -319,6 +326,9 @@ def s2l_linear_attn(state, batch, q, k, v, scale, out, workspace=None, stream=No
     """Linear attention of the batch's chunks over `state` (advanced from its slot_in to its slot_out):
     out[i][h] = scale * q_i[h] S after S <- exp(log_decay[h]) S + k_i v_i^T; tensors as for
     s2l_rope_qk, the workspace a device uint8 tensor (None where no bytes are needed)."""
+    st = (_native or _load_native()).linear(state, batch, q, k, v, scale, out, workspace, stream)
+    if st is not None:
+        return _lib.failed("s2l_linear_attn", st) if st else None
     qp, qs, hq = _rows(q, "q", batch)
     kp, ks, hkv = _rows(k, "k", batch)
     vp, vs, hv = _rows(v, "v", batch)

@@ -196,7 +196,7 @@ class _NoBinding:
     def _refuse(*_):
         return None
 
-    append = plan = attn = fused = reduce = _refuse
+    append = plan = attn = fused = reduce = rope_qk = rope_append = linear = _refuse
 
 
 def binding(objects):
@@ -217,6 +217,6 @@ def binding(objects):
                       "build it with `python -m paper_2604_16395_amd.build`", RuntimeWarning, stacklevel=3)
         return _NoBinding
     names = ("s2l_kv_append", "s2l_attn_plan", "s2l_chunk_prefill_attn", "s2l_chunk_prefill_attn_q8", "s2l_attn_main",
-             "s2l_append_chunk_prefill_attn", "s2l_split_reduce")
+             "s2l_append_chunk_prefill_attn", "s2l_split_reduce", "s2l_rope_qk", "s2l_rope_kv_append", "s2l_linear_attn")
     _binding.setup(objects, tuple(ctypes.cast(getattr(handle, n), c_vp).value for n in names))
     return _binding

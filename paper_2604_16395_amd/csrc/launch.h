@@ -121,12 +121,13 @@ struct LinearLaunch {        // linear attention (linear_attn.hip)
   int32_t num_slots, num_reqs, hq, hkv;
   float scale;
   float* ws;                 // [ws_states][hq][128][128]: states around the pieces of cut requests
-  int32_t piece_tokens, ws_states, num_units;   // from the plan, per launch
+  int32_t piece_tokens, unit_tokens, ws_states, num_units;   // from the plan, per launch
 };
 // Requests of at most kLinearShortTokens new tokens are advanced token by token, the others in blocks.
 constexpr int32_t kLinearShortTokens = 16, kLinearBlockTokens = 32;
 struct LinearPlan {          // how the batch is cut, from the host lengths
   int32_t piece_tokens;      // longer requests are cut into pieces of so many tokens (a multiple of a block)
+  int32_t unit_tokens;       // the longest piece's
   int32_t pieces;            // of all requests that are not short
   int32_t cut_reqs, ws_states;   // requests of more than one piece; one state before, between and after them
   int32_t short_reqs;

@@ -59,36 +59,54 @@ __device__ inline int32_t wave_scan(int32_t x) {
   return x;
 }
 
-// The idx-th of the batch's units, 64 requests at a time, all that is known of them in one round of loads.  Units are the short requests (kShort), or the
-// pieces of the others: of all, or (kCutPieces) of those that are cut.
+// The idx-th of the batch's units, 64 requests at a time, all that is known of them in one round of loads.  Units
+// are the short requests (kShort), or the pieces of the others: of all, or (kCutPieces) of those that are cut.
+// Pieces come longest first (by eighths of the longest): the longest then have a CU of their own while there
+// are fewer than CUs, and do not begin last (11 requests of 17 to 2048 tokens, 32 heads: 199 us in the batch's
+// order, 141 in this).
 enum Units { kShort, kPieces, kCutPieces };
 template <Units kUnits>
 __device__ inline Piece find_unit(const LinearLaunch& a, int32_t idx) {
   const int lane = threadIdx.x & 63;
   int32_t ws = 0;
   for (int32_t r0 = 0; r0 < a.num_reqs; r0 += 64) {
-    const int32_t r = r0 + lane < a.num_reqs ? r0 + lane : r0;
+    const int32_t count = a.num_reqs - r0 < 64 ? a.num_reqs - r0 : 64;
+    const int32_t r = r0 + (lane < count ? lane : 0);
     const int32_t row = a.cu_chunk[r], slot_in = a.slot_in[r], slot_out = a.slot_out[r], l = a.chunk_lens[r];
-    const int32_t len = r0 + lane < a.num_reqs ? l : -1;
+    const int32_t len = lane < count ? l : -1;
     const int32_t pieces = len > kLinearShortTokens ? (len + a.piece_tokens - 1) / a.piece_tokens : 0;
     const int32_t cut = pieces > 1 ? pieces : 0, entries = cut ? cut + 1 : 0;   // workspace entries
     const int32_t mine = kUnits == kShort ? (len >= 0 && len <= kLinearShortTokens) : kUnits == kPieces ? pieces : cut;
-    const int32_t sum = wave_scan(mine), ws_sum = kUnits == kShort ? 0 : wave_scan(entries);
-    const int32_t total = __builtin_amdgcn_readlane(sum, 63);
-    if (idx < total) {
-      const int32_t c = __popcll(__ballot(sum <= idx));
+    int32_t before = 0, ws_before = 0;   // units that come before this lane's request's, and entries
+    if constexpr (kUnits == kShort) {
+      before = wave_scan(mine) - mine;
+    } else {
+      ws_before = wave_scan(entries) - entries;
+      const int32_t size = len < a.piece_tokens ? len : a.piece_tokens;
+      const int32_t eighth = min(7, (int32_t)((float)size * (8.f / (float)a.unit_tokens)));
+      int32_t base = 0;
+#pragma unroll
+      for (int32_t c = 7; c >= 0; --c) {
+        const int32_t sum = wave_scan(eighth == c ? mine : 0);
+        if (eighth == c) before = base + sum - mine;
+        base += __builtin_amdgcn_readlane(sum, 63);
+      }
+    }
+    const uint64_t here = __ballot(idx >= before && idx < before + mine);
+    if (here != 0) {
+      const int32_t c = __builtin_ctzll(here);
       Piece p;
       p.req = r0 + c;
       p.len = __builtin_amdgcn_readlane(len, c);
-      p.seg = idx - (__builtin_amdgcn_readlane(sum, c) - __builtin_amdgcn_readlane(mine, c));
-      p.ws = ws + __builtin_amdgcn_readlane(ws_sum, c) - __builtin_amdgcn_readlane(entries, c);
+      p.seg = idx - __builtin_amdgcn_readlane(before, c);
+      p.ws = ws + __builtin_amdgcn_readlane(ws_before, c);
       p.row = __builtin_amdgcn_readlane(row, c);
       p.slot_in = __builtin_amdgcn_readlane(slot_in, c);
       p.slot_out = __builtin_amdgcn_readlane(slot_out, c);
       return p;
     }
-    idx -= total;
-    ws += __builtin_amdgcn_readlane(ws_sum, 63);
+    idx -= __builtin_amdgcn_readlane(wave_scan(mine), 63);
+    ws += __builtin_amdgcn_readlane(wave_scan(entries), 63);
   }
   return Piece{-1, 0, 0, 0, 0, 0, 0};   // the device lengths hold less than the host copies: nothing to do
 }
@@ -631,6 +649,7 @@ hipError_t launch_linear_attn(const LinearLaunch& launch, const LinearPlan& plan
   LinearLaunch a = launch;
   a.piece_tokens = plan.piece_tokens;
   a.ws_states = plan.ws_states;
+  a.unit_tokens = plan.unit_tokens;
   const int group = a.hq / a.hkv;
   auto blocks = [&](int64_t units) { return dim3((uint32_t)((units * a.hkv + 7) / 8 * 8 * group)); };
   // what a copy straight into LDS takes: 16-byte steps, a row's end before the next one's start, 32-bit offsets

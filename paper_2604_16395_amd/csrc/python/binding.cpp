@@ -1,4 +1,4 @@
-// Argument marshalling of the per-step calls (append, plan, attention, merge) for the Python
+// Argument marshalling of the per-step calls (append, plan, attention, merge, rotation, linear attention) for the Python
 // package, through the CPython API: a step of small sizes is bound by what the host does between
 // its launches, and building the argument structs through ctypes took 9 of the 14 us of a call.
 // Every pointer, length and stream is read from the objects on each call; nothing is kept.
@@ -9,6 +9,8 @@
 // that this module follows the library that the package loaded.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+
+#include <cstring>
 
 #include "s2l.h"
 
@@ -22,12 +24,17 @@ struct Entry {
   s2l_status (*fused)(const s2l_kv_cache*, const s2l_batch*, const void*, const void*, const void*, int32_t, float,
                       void*, float*, const s2l_plan_info*, void*, size_t, int32_t*, void*);
   s2l_status (*reduce)(const s2l_batch*, int32_t, void*, float*, const s2l_plan_info*, const void*, size_t, void*);
+  decltype(&s2l_rope_qk) rope_qk;
+  decltype(&s2l_rope_kv_append) rope_append;
+  decltype(&s2l_linear_attn) linear;
 } lib;
 
-PyObject *tensor_type, *cache_type, *batch_type, *opts_type, *info_type, *stream_type, *bf16, *f32, *u8, *is_initialized, *get_device, *get_stream;
+PyObject *tensor_type, *cache_type, *batch_type, *opts_type, *info_type, *stream_type, *bf16, *f32, *u8, *is_initialized, *get_device, *get_stream,
+    *rope_type, *state_type, *i32;
 PyObject *s_dtype, *s_data_ptr, *s_is_contiguous, *s_shape, *s_numel, *s_k_pages, *s_v_pages, *s_k_scale, *s_v_scale,
     *s_fp8, *s_prefix_host, *s_chunk_host, *s_tables_host, *s_prefix_lens, *s_chunk_lens, *s_cu_chunk, *s_block_tables,
-    *s_cuda_stream;
+    *s_cuda_stream, *s_stride, *s_get_device, *s_inv_freq, *s_positions, *s_pair_axis, *s_adjacent, *s_scale, *s_states, *s_log_decay,
+    *s_slot_in, *s_slot_out;
 
 // Owned reference, released at the end of the scope.
 struct Ref {
@@ -178,6 +185,101 @@ bool int_arg(PyObject* o, int32_t* v) {
   return true;
 }
 
+// The current device's index; none before the GPU is in use.
+bool current_device(long* dev) {
+  const Ref ready(PyObject_CallNoArgs(is_initialized));
+  if (!ready || ready.o != Py_True) return false;
+  const Ref d(PyObject_CallNoArgs(get_device));
+  if (!d) return false;
+  *dev = PyLong_AsLong(d.o);
+  return !PyErr_Occurred();
+}
+bool on_device(PyObject* t, long dev) {
+  const Ref d(PyObject_CallMethodNoArgs(t, s_get_device));
+  return d && PyLong_AsLong(d.o) == dev && !PyErr_Occurred();
+}
+
+// Shape and strides, in elements, of a tensor of `ndim` dimensions.
+bool layout(PyObject* t, int ndim, int64_t* shape, int64_t* stride) {
+  const Ref sh(PyObject_GetAttr(t, s_shape)), st(PyObject_CallMethodNoArgs(t, s_stride));
+  if (!sh || !st || !PyTuple_Check(sh.o) || !PyTuple_Check(st.o) || PyTuple_GET_SIZE(sh.o) != ndim || PyTuple_GET_SIZE(st.o) != ndim)
+    return false;
+  for (int i = 0; i < ndim; ++i) {
+    shape[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(sh.o, i));
+    stride[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(st.o, i));
+  }
+  return !PyErr_Occurred();
+}
+
+// A device tensor of rows [>= tokens][heads][128], each row's heads contiguous.
+struct Rows {
+  void* p = nullptr;
+  int64_t stride = 0;
+  int32_t heads = 0;
+  bool take(PyObject* t, int64_t tokens, long dev) {
+    int64_t n[3], s[3];
+    if ((PyObject*)Py_TYPE(t) != tensor_type) return false;
+    const Ref d(PyObject_GetAttr(t, s_dtype));
+    if (!d || d.o != bf16 || !layout(t, 3, n, s) || n[0] < tokens || n[1] > INT32_MAX || n[2] != S2L_HEAD_DIM || s[2] != 1 ||
+        (n[1] > 1 && s[1] != S2L_HEAD_DIM) || !on_device(t, dev) || !data_ptr(t, &p))
+      return false;
+    stride = s[0];
+    heads = (int32_t)n[1];
+    return true;
+  }
+};
+
+int64_t total_tokens(const s2l_batch& b) {
+  int64_t n = 0;
+  for (int32_t r = 0; r < b.num_reqs; ++r) n += b.chunk_lens_host[r] > 0 ? b.chunk_lens_host[r] : 0;
+  return n;
+}
+
+// The batch, on the current device.
+bool batch_on_device(PyObject* o, BatchArg* batch, int64_t* tokens, long* dev) {
+  if (!current_device(dev) || !batch->take(o)) return false;
+  const Ref c(PyObject_GetAttr(o, s_chunk_lens));
+  *tokens = total_tokens(batch->c);
+  return c && on_device(c.o, *dev);
+}
+
+// An attribute that is a contiguous device tensor of `dtype`; its element count.
+bool attr_tensor(PyObject* o, PyObject* name, PyObject* dtype, long dev, void** p, size_t* n) {
+  const Ref t(PyObject_GetAttr(o, name));
+  return t && tensor(t.o, dtype, p) && numel(t.o, n) && on_device(t.o, dev);
+}
+
+bool rope_arg(PyObject* o, int64_t tokens, long dev, s2l_rope* r) {
+  if ((PyObject*)Py_TYPE(o) != rope_type) return false;
+  *r = s2l_rope{};
+  void* f;
+  size_t pairs;
+  if (!attr_tensor(o, s_inv_freq, f32, dev, &f, &pairs) || pairs > 64) return false;
+  r->inv_freq = static_cast<const float*>(f);
+  r->rot_dim = 2 * (int32_t)pairs;
+  r->num_axes = 1;
+  const Ref pos(PyObject_GetAttr(o, s_positions)), axis(PyObject_GetAttr(o, s_pair_axis)), adj(PyObject_GetAttr(o, s_adjacent)),
+      scale(PyObject_GetAttr(o, s_scale));
+  if (!pos || !axis || !adj || !scale || !PyBytes_CheckExact(axis.o) || PyBytes_GET_SIZE(axis.o) != sizeof r->pair_axis ||
+      !PyFloat_CheckExact(scale.o) || (adj.o != Py_True && adj.o != Py_False))
+    return false;
+  std::memcpy(r->pair_axis, PyBytes_AS_STRING(axis.o), sizeof r->pair_axis);
+  r->flags = adj.o == Py_True ? S2L_ROPE_ADJACENT : 0;
+  r->scale = (float)PyFloat_AS_DOUBLE(scale.o);
+  if (pos.o == Py_None) return true;
+  if ((PyObject*)Py_TYPE(pos.o) != tensor_type) return false;
+  const Ref d(PyObject_GetAttr(pos.o, s_dtype));
+  int64_t n[2] = {1, 0}, s[2] = {0, 1};
+  void* p;
+  if (!d || d.o != i32 || (!layout(pos.o, 2, n, s) && !layout(pos.o, 1, n + 1, s + 1)) || n[0] < 1 || n[0] > S2L_ROPE_MAX_AXES || n[1] < tokens || s[1] != 1 || s[0] < 0 ||
+      !on_device(pos.o, dev) || !data_ptr(pos.o, &p))
+    return false;
+  r->positions = static_cast<const int32_t*>(p);
+  r->pos_stride = s[0];
+  r->num_axes = (int32_t)n[0];
+  return true;
+}
+
 PyObject* general() {   // not the plain form: whatever was raised on the way does not count
   PyErr_Clear();
   Py_RETURN_NONE;
@@ -270,18 +372,82 @@ PyObject* reduce(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return call([&] { return lib.reduce(&batch.c, hq, out, static_cast<float*>(lse), info.p, ws, bytes, stream); });
 }
 
+// (batch, rope, q, q_out, k, k_out, stream)
+PyObject* rope_qk(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  BatchArg batch;
+  s2l_rope rope;
+  Rows q, q_out, k, k_out;
+  int64_t tokens;
+  long dev;
+  void* stream;
+  if (n != 7 || !batch_on_device(a[0], &batch, &tokens, &dev) || !rope_arg(a[1], tokens, dev, &rope) || !q.take(a[2], tokens, dev) ||
+      !q_out.take(a[3], tokens, dev) || q.heads != q_out.heads || !stream_arg(a[6], &stream))
+    return general();
+  if (a[4] != Py_None && (!k.take(a[4], tokens, dev) || !k_out.take(a[5], tokens, dev) || k.heads != k_out.heads)) return general();
+  return call([&] {
+    return lib.rope_qk(&batch.c, &rope, q.p, q.stride, q.heads, q_out.p, q_out.stride, k.p, k.stride, k.heads, k_out.p, k_out.stride,
+                       stream);
+  });
+}
+
+// (cache, batch, rope, q, q_out, k, v, stream)
+PyObject* rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  s2l_kv_cache cache;
+  BatchArg batch;
+  s2l_rope rope;
+  Rows q, q_out, k, v;
+  int64_t tokens;
+  long dev;
+  void* stream;
+  if (n != 8 || !cache_arg(a[0], &cache) || !batch_on_device(a[1], &batch, &tokens, &dev) || !rope_arg(a[2], tokens, dev, &rope) ||
+      !k.take(a[5], tokens, dev) || !v.take(a[6], tokens, dev) || k.heads != cache.num_kv_heads || v.heads != k.heads ||
+      !stream_arg(a[7], &stream))
+    return general();
+  if (a[3] != Py_None && (!q.take(a[3], tokens, dev) || !q_out.take(a[4], tokens, dev) || q.heads != q_out.heads)) return general();
+  return call([&] {
+    return lib.rope_append(&cache, &batch.c, &rope, q.p, q.stride, q.heads, q_out.p, q_out.stride, k.p, k.stride, v.p, v.stride, stream);
+  });
+}
+
+// (state, batch, q, k, v, scale, out, workspace, stream)
+PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  BatchArg batch;
+  Rows q, k, v, out;
+  int64_t tokens, shape[4], stride[4];
+  long dev;
+  size_t in_slots, out_slots, decays, elements, bytes = 0;
+  void *in, *slots, *states, *decay, *ws = nullptr, *st;
+  if (n != 9 || (PyObject*)Py_TYPE(a[0]) != state_type || !batch_on_device(a[1], &batch, &tokens, &dev) || !q.take(a[2], tokens, dev) ||
+      !k.take(a[3], tokens, dev) || !v.take(a[4], tokens, dev) || !PyFloat_CheckExact(a[5]) || !out.take(a[6], tokens, dev) ||
+      k.heads != v.heads || q.heads != out.heads || !stream_arg(a[8], &st) ||
+      !attr_tensor(a[0], s_slot_in, i32, dev, &in, &in_slots) || !attr_tensor(a[0], s_slot_out, i32, dev, &slots, &out_slots) ||
+      !attr_tensor(a[0], s_log_decay, f32, dev, &decay, &decays) || !attr_tensor(a[0], s_states, f32, dev, &states, &elements))
+    return general();
+  if (a[7] != Py_None && (!tensor(a[7], u8, &ws) || !numel(a[7], &bytes) || !on_device(a[7], dev))) return general();
+  const Ref all(PyObject_GetAttr(a[0], s_states));
+  if (!all || !layout(all.o, 4, shape, stride) || shape[0] > INT32_MAX || shape[1] != q.heads || decays != (size_t)q.heads ||
+      shape[2] != S2L_HEAD_DIM || shape[3] != S2L_HEAD_DIM || in_slots != (size_t)batch.c.num_reqs || out_slots != in_slots)
+    return general();
+  const s2l_linear_state state = {static_cast<float*>(states), static_cast<const float*>(decay), static_cast<const int32_t*>(in),
+                                  static_cast<const int32_t*>(slots), (int32_t)shape[0], q.heads};
+  const float scale = (float)PyFloat_AS_DOUBLE(a[5]);
+  return call([&] {
+    return lib.linear(&state, &batch.c, q.p, q.stride, k.p, k.stride, v.p, v.stride, k.heads, scale, out.p, out.stride, ws, bytes, st);
+  });
+}
+
 // (types and dtypes and torch functions as a tuple, entry point addresses as a tuple)
 PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  void* f[7];
+  void* f[10];
   PyObject** o[] = {&tensor_type, &cache_type, &batch_type, &opts_type, &info_type, &stream_type,
-                    &bf16, &f32, &u8, &is_initialized, &get_device, &get_stream};
-  if (n != 2 || !PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) != 12 || !PyTuple_Check(a[1]) || PyTuple_GET_SIZE(a[1]) != 7) {
+                    &bf16, &f32, &u8, &is_initialized, &get_device, &get_stream, &rope_type, &state_type, &i32};
+  if (n != 2 || !PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) != 15 || !PyTuple_Check(a[1]) || PyTuple_GET_SIZE(a[1]) != 10) {
     PyErr_SetString(PyExc_TypeError, "setup(objects, addresses)");
     return nullptr;
   }
-  for (int i = 0; i < 7; ++i)
+  for (int i = 0; i < 10; ++i)
     if (!to_ptr(PyTuple_GET_ITEM(a[1], i), &f[i])) return nullptr;
-  for (int i = 0; i < 12; ++i) {
+  for (int i = 0; i < 15; ++i) {
     Py_INCREF(PyTuple_GET_ITEM(a[0], i));
     Py_XSETREF(*o[i], PyTuple_GET_ITEM(a[0], i));
   }
@@ -290,11 +456,15 @@ PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
   for (int i = 0; i < 3; ++i) lib.attn[i] = reinterpret_cast<decltype(lib.attn[0])>(f[2 + i]);
   lib.fused = reinterpret_cast<decltype(lib.fused)>(f[5]);
   lib.reduce = reinterpret_cast<decltype(lib.reduce)>(f[6]);
+  lib.rope_qk = reinterpret_cast<decltype(lib.rope_qk)>(f[7]);
+  lib.rope_append = reinterpret_cast<decltype(lib.rope_append)>(f[8]);
+  lib.linear = reinterpret_cast<decltype(lib.linear)>(f[9]);
   Py_RETURN_NONE;
 }
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {FAST(setup), FAST(append), FAST(plan), FAST(attn), FAST(fused), FAST(reduce), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {FAST(setup), FAST(append), FAST(plan), FAST(attn), FAST(fused), FAST(reduce), FAST(rope_qk),
+                         FAST(rope_append), FAST(linear), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Argument marshalling of the per-step calls.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 
@@ -308,7 +478,10 @@ PyMODINIT_FUNC PyInit__binding(void) {
                {&s_numel, "numel"}, {&s_k_pages, "k_pages"}, {&s_v_pages, "v_pages"}, {&s_k_scale, "k_scale"},
                {&s_v_scale, "v_scale"}, {&s_fp8, "fp8"}, {&s_prefix_host, "prefix_host"}, {&s_chunk_host, "chunk_host"},
                {&s_tables_host, "tables_host"}, {&s_prefix_lens, "prefix_lens"}, {&s_chunk_lens, "chunk_lens"},
-               {&s_cu_chunk, "cu_chunk"}, {&s_block_tables, "block_tables"}, {&s_cuda_stream, "cuda_stream"}};
+               {&s_cu_chunk, "cu_chunk"}, {&s_block_tables, "block_tables"}, {&s_cuda_stream, "cuda_stream"},
+               {&s_stride, "stride"}, {&s_get_device, "get_device"}, {&s_inv_freq, "inv_freq"}, {&s_positions, "positions"},
+               {&s_pair_axis, "pair_axis"}, {&s_adjacent, "adjacent"}, {&s_scale, "scale"}, {&s_states, "states"},
+               {&s_log_decay, "log_decay"}, {&s_slot_in, "slot_in"}, {&s_slot_out, "slot_out"}};
   for (const auto& n : names)
     if (!(*n.o = PyUnicode_InternFromString(n.s))) return nullptr;
   return PyModule_Create(&module);

@@ -239,3 +239,46 @@ def test_graph_replays_and_streams():
             g.replay()
         torch.cuda.synchronize()
         assert all(same(a, b) for a, b in zip((q_out, cache.k_pages, cache.v_pages), ref))
+
+
+def test_plain_calls_are_marshalled_natively(monkeypatch):
+    """None of these calls needs the ctypes path (about 15 us more); positions of one axis in either form."""
+    gen = torch.Generator(device=DEV).manual_seed(10)
+    P, C, hq, hkv = [3, 40], [5, 1], 4, 2
+    T = sum(C)
+    batch = s2l.Batch(P, C, np.arange(8, dtype=np.int32).reshape(2, 4))
+    cache = s2l.PagedKVCache(*(torch.zeros((8, hkv, 16, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2)))
+    qkv = rows(gen, T, hq + 2 * hkv)
+    q, k, v = qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:]
+    pos = torch.randint(0, 99, (3, T), generator=gen, device=DEV, dtype=torch.int32)
+    inv = torch.from_numpy(freqs(64)).to(DEV)
+    ropes = [s2l.Rope(inv), s2l.Rope(inv, pos[0]), s2l.Rope(inv, pos[:1]), s2l.Rope(inv, pos, s2l.rope_pair_axes((24, 20, 20)), True, 0.5)]
+
+    def both(rope):
+        q_out, k_out, q2 = (torch.zeros((T, n, 128), dtype=torch.bfloat16, device=DEV) for n in (hq, hkv, hq))
+        s2l.s2l_rope_qk(batch, rope, q, q_out, k, k_out)
+        s2l.s2l_rope_kv_append(cache, batch, rope, q, q2, k, v)
+        torch.cuda.synchronize()
+        assert same(q_out, q2)
+        return [q_out, k_out, cache.k_pages.clone()]
+
+    states = torch.randn((3, hq, 128, 128), generator=gen, device=DEV)
+    slots = torch.tensor([0, 1], dtype=torch.int32, device=DEV)
+
+    def linear():
+        s = states.clone()
+        out = torch.zeros((T, hq, 128), dtype=torch.bfloat16, device=DEV)
+        s2l.s2l_linear_attn(s2l.LinearState(s, -torch.ones(hq, device=DEV), slots, slots), batch, q, k, v, 0.1, out, None)
+        torch.cuda.synchronize()
+        return [out, s]
+
+    native = s2l._load_native()
+    with monkeypatch.context() as m:   # the general path
+        m.setattr(s2l, "_native", s2l._lib._NoBinding)
+        ref = [both(r) for r in ropes] + [linear()]
+    assert s2l._native is native
+    with monkeypatch.context() as m:
+        m.setattr(s2l._lib, "call", None)
+        got = [both(r) for r in ropes] + [linear()]
+    assert all(same(a, b) for x, y in zip(ref, got) for a, b in zip(x, y))
+    assert same(got[1][0], got[2][0]) and not same(got[0][0], got[1][0])
