@@ -117,10 +117,6 @@ constexpr int kSliceCols = 32;       // columns of a recurrent workgroup
 static_assert(kLinearShortTokens <= 16, "partial sums of all tokens in LDS");
 
 __device__ inline f32x4 unpack4(const u32x2& x) { return f32x4{bf16lo(x[0]), bf16hi(x[0]), bf16lo(x[1]), bf16hi(x[1])}; }
-__device__ inline f32x4 load4(const uint16_t* p) {
-  const u32x2 x = *reinterpret_cast<const u32x2_any*>(p);
-  return unpack4(x);
-}
 
 __global__ __launch_bounds__(256) void linear_recurrent_kernel(LinearLaunch a) {
   __shared__ float s_part[kLinearShortTokens][4][kSliceCols];
@@ -140,13 +136,23 @@ __global__ __launch_bounds__(256) void linear_recurrent_kernel(LinearLaunch a) {
     if (si >= 0 && si < a.num_slots) s[j] = *reinterpret_cast<const f32x4*>(a.states + si * slot + at + j * 128);
     else s[j] = f32x4{} + (si == -1 ? 0.f : __builtin_nanf(""));
   }
+  // a token's rows are loaded while the one before is worked on
+  const uint16_t* kp = a.k + row0 * a.k_stride + g * 128 + 4 * kg;
+  const uint16_t* vp = a.v + row0 * a.v_stride + g * 128 + col0 + 4 * vq;
+  const uint16_t* qp = a.q + row0 * a.q_stride + h * 128 + 4 * kg;
+  u32x2 kn{}, vn{}, qn{};
+  auto next = [&](int t) {
+    if (t >= C) return;
+    kn = *reinterpret_cast<const u32x2_any*>(kp + t * a.k_stride);
+    vn = *reinterpret_cast<const u32x2_any*>(vp + t * a.v_stride);
+    qn = *reinterpret_cast<const u32x2_any*>(qp + t * a.q_stride);
+  };
+  next(0);
   const float decay = (float)exp(clean_log(a.log_decay[h]));
 
   for (int t = 0; t < C; ++t) {
-    const int64_t row = row0 + t;
-    const f32x4 k = load4(a.k + row * a.k_stride + g * 128 + 4 * kg);
-    const f32x4 v = load4(a.v + row * a.v_stride + g * 128 + col0 + 4 * vq);
-    const f32x4 q = load4(a.q + row * a.q_stride + h * 128 + 4 * kg);
+    const f32x4 k = unpack4(kn), v = unpack4(vn), q = unpack4(qn);
+    next(t + 1);
     f32x4 o{};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -158,9 +164,8 @@ __global__ __launch_bounds__(256) void linear_recurrent_kernel(LinearLaunch a) {
     }
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      o[c] += __shfl_xor(o[c], 8, 64);
-      o[c] += __shfl_xor(o[c], 16, 64);
-      o[c] += __shfl_xor(o[c], 32, 64);
+      o[c] += u2f(__builtin_amdgcn_update_dpp(0, f2u(o[c]), 0x128, 0xF, 0xF, false));   // row_ror:8
+      o[c] = sum_of_four(o[c]);
     }
     if ((threadIdx.x & 63) < 8) *reinterpret_cast<f32x4*>(&s_part[t][wave][4 * vq]) = o;
   }

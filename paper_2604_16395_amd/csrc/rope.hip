@@ -5,10 +5,13 @@
 // position * (inv_freq / 2 pi), and only its distance from the nearest whole turn is rounded to
 // fp32 (2^-26 of a turn), for the hardware's sine and cosine, which take turns.
 //
-// A wave takes one row (token) and 8 kHeads of its heads (a workgroup four rows); lane l holds unit l % 8 of head l / 8, the
-// 16 elements of 8 pairs in two 16-byte chunks, so that a lane's 8 sines and cosines serve all its
-// heads and rows of a head are read and written whole.  Units past the rotated dims, and V's, are
-// copied.  Nothing is shared between waves: no LDS, no barrier.
+// A wave takes one row (token) and 8 kHeads of its heads (a workgroup four rows; workgroups of the same rows
+// follow one another); lane l holds unit l % 8 of head l / 8, the 16 elements of 8 pairs in two 16-byte
+// chunks, so that a lane's 8 sines and cosines serve all its heads and rows of a head are read and
+// written whole.  Units past the rotated dims, and V's, are copied.  Nothing is shared between waves: no LDS, no barrier.
+// Bound by the memory for many rows: 35104 rows of 32 + 8 + 8 heads, 863 MB, 158 us, 5.5 TB/s (168 with one head a
+// lane; 217 with one head a lane and the groups of a row far apart); by the chain of loads for few: one row 3.1 us, 512
+// rows 4.5 us (4.8 with two heads a lane).
 #include "launch.h"
 #include "s2l.h"
 #include "s2l_device.h"
@@ -65,11 +68,13 @@ template <bool kAdjacent, bool kAppend, bool kFp8, int kHeads>
 __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a) {
   const int lane = threadIdx.x & 63, unit = lane & 7;
   const int heads = a.hq + a.hkv * (kAppend ? 2 : 1);
-  const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t groups = (heads + 8 * kHeads - 1) / (8 * kHeads);
+  const int first = (int)(blockIdx.x % groups) * 8 * kHeads;   // the wave's first head
+  const int64_t row = (int64_t)(blockIdx.x / groups) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (row >= a.total_rows) return;
-  const int head0 = (int)blockIdx.y * 8 * kHeads + (lane >> 3);
+  const int head0 = first + (lane >> 3);
   const int half = a.rot_dim / 2;
-  const bool turns = unit < a.rot_dim / 16 && (!kAppend || (int)blockIdx.y * 8 * kHeads < a.hq + a.hkv);
+  const bool turns = unit < a.rot_dim / 16 && (!kAppend || first < a.hq + a.hkv);
   const bool pairs_apart = !kAdjacent && unit < a.rot_dim / 16;
   const int oa = pairs_apart ? 8 * unit : 16 * unit, ob = pairs_apart ? oa + half : oa + 8;
 
@@ -168,12 +173,17 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a) {
   }
 }
 
+// Two heads a lane share its sines and cosines and halve the waves; as long as waves are few (8 a SIMD), more of them
+// hide more.
 template <bool kAdjacent, bool kAppend, bool kFp8>
 void launch(const RopeLaunch& a, hipStream_t stream) {
+  constexpr int64_t kFewWaves = 8192;
   const int heads = a.hq + a.hkv * (kAppend ? 2 : 1);
-  constexpr int kHeads = 1;
-  const dim3 grid((uint32_t)(((int64_t)a.total_rows + 3) / 4), (heads + 8 * kHeads - 1) / (8 * kHeads));
-  rope_kernel<kAdjacent, kAppend, kFp8, kHeads><<<grid, 256, 0, stream>>>(a);
+  const int64_t four_rows = ((int64_t)a.total_rows + 3) / 4, groups = (heads + 7) / 8;
+  if (a.total_rows * groups <= kFewWaves)
+    rope_kernel<kAdjacent, kAppend, kFp8, 1><<<dim3((uint32_t)(four_rows * groups)), 256, 0, stream>>>(a);
+  else
+    rope_kernel<kAdjacent, kAppend, kFp8, 2><<<dim3((uint32_t)(four_rows * ((groups + 1) / 2))), 256, 0, stream>>>(a);
 }
 
 }  // namespace
