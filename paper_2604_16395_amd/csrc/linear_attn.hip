@@ -114,7 +114,6 @@ __device__ inline Piece find_unit(const LinearLaunch& a, int32_t idx) {
 // ---- recurrent form ----
 
 constexpr int kSliceCols = 32;       // columns of a recurrent workgroup
-static_assert(kLinearShortTokens <= 16, "partial sums of all tokens in LDS");
 
 __device__ inline f32x4 unpack4(const u32x2& x) { return f32x4{bf16lo(x[0]), bf16hi(x[0]), bf16lo(x[1]), bf16hi(x[1])}; }
 
@@ -136,38 +135,49 @@ __global__ __launch_bounds__(256) void linear_recurrent_kernel(LinearLaunch a) {
     if (si >= 0 && si < a.num_slots) s[j] = *reinterpret_cast<const f32x4*>(a.states + si * slot + at + j * 128);
     else s[j] = f32x4{} + (si == -1 ? 0.f : __builtin_nanf(""));
   }
-  // a token's rows are loaded while the one before is worked on
+  // four tokens' rows are loaded while the four before are worked on
+  constexpr int kAhead = 4;
   const uint16_t* kp = a.k + row0 * a.k_stride + g * 128 + 4 * kg;
   const uint16_t* vp = a.v + row0 * a.v_stride + g * 128 + col0 + 4 * vq;
   const uint16_t* qp = a.q + row0 * a.q_stride + h * 128 + 4 * kg;
-  u32x2 kn{}, vn{}, qn{};
-  auto next = [&](int t) {
-    if (t >= C) return;
-    kn = *reinterpret_cast<const u32x2_any*>(kp + t * a.k_stride);
-    vn = *reinterpret_cast<const u32x2_any*>(vp + t * a.v_stride);
-    qn = *reinterpret_cast<const u32x2_any*>(qp + t * a.q_stride);
+  u32x2 kn[kAhead] = {}, vn[kAhead] = {}, qn[kAhead] = {};
+  auto load = [&](int t0) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (t0 + i >= C) break;
+      kn[i] = *reinterpret_cast<const u32x2_any*>(kp + (t0 + i) * a.k_stride);
+      vn[i] = *reinterpret_cast<const u32x2_any*>(vp + (t0 + i) * a.v_stride);
+      qn[i] = *reinterpret_cast<const u32x2_any*>(qp + (t0 + i) * a.q_stride);
+    }
   };
-  next(0);
+  load(0);
   const float decay = (float)exp(clean_log(a.log_decay[h]));
 
-  for (int t = 0; t < C; ++t) {
-    const f32x4 k = unpack4(kn), v = unpack4(vn), q = unpack4(qn);
-    next(t + 1);
-    f32x4 o{};
+  for (int t0 = 0; t0 < C; t0 += kAhead) {
+    u32x2 kc[kAhead], vc[kAhead], qc[kAhead];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int i = 0; i < kAhead; ++i) kc[i] = kn[i], vc[i] = vn[i], qc[i] = qn[i];
+    if (t0 + kAhead < C) load(t0 + kAhead);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (t0 + i >= C) break;
+      const f32x4 k = unpack4(kc[i]), v = unpack4(vc[i]), q = unpack4(qc[i]);
+      f32x4 o{};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          s[j][c] = __builtin_fmaf(s[j][c], decay, k[j] * v[c]);
+          o[c] = __builtin_fmaf(q[j], s[j][c], o[c]);
+        }
+      }
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        s[j][c] = __builtin_fmaf(s[j][c], decay, k[j] * v[c]);
-        o[c] = __builtin_fmaf(q[j], s[j][c], o[c]);
+        o[c] += u2f(__builtin_amdgcn_update_dpp(0, f2u(o[c]), 0x128, 0xF, 0xF, false));   // row_ror:8
+        o[c] = sum_of_four(o[c]);
       }
+      if ((threadIdx.x & 63) < 8) *reinterpret_cast<f32x4*>(&s_part[t0 + i][wave][4 * vq]) = o;
     }
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      o[c] += u2f(__builtin_amdgcn_update_dpp(0, f2u(o[c]), 0x128, 0xF, 0xF, false));   // row_ror:8
-      o[c] = sum_of_four(o[c]);
-    }
-    if ((threadIdx.x & 63) < 8) *reinterpret_cast<f32x4*>(&s_part[t][wave][4 * vq]) = o;
   }
   if (so >= 0 && so < a.num_slots) {
 #pragma unroll
