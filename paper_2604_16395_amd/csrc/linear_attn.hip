@@ -78,7 +78,8 @@ __device__ inline Piece find_unit(const LinearLaunch& a, int32_t idx) {
     const int32_t cut = pieces > 1 ? pieces : 0, entries = cut ? cut + 1 : 0;   // workspace entries
     const int32_t mine = kUnits == kShort ? (len >= 0 && len <= kLinearShortTokens) : kUnits == kPieces ? pieces : cut;
     int32_t before = 0, ws_before = 0;   // units that come before this lane's request's, and entries
-    if constexpr (kUnits == kShort) {
+    if (a.num_reqs == 1) {
+    } else if constexpr (kUnits == kShort) {
       before = wave_scan(mine) - mine;
     } else {
       ws_before = wave_scan(entries) - entries;
@@ -359,6 +360,18 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
     load(0);
   }
 
+  // state: register (m, i) is key dim 32 m + dim(i), column 32 wave + n
+  auto dim = [&](int i) { return 16 * (i >> 3) + 8 * half + 4 * ((i >> 2) & 1) + (i & 3); };
+  f32x16 S[4];
+  const bool own_state = kOutputs ? !cut : p.seg == 0;   // the request's, not the workspace's or none
+  const float* from = own_state ? (si >= 0 && si < a.num_slots ? a.states + si * slot + (int64_t)h * kState : nullptr)
+                      : kOutputs ? ws : nullptr;
+  const float none = !own_state || si == -1 ? 0.f : __builtin_nanf("");
+#pragma unroll
+  for (int m = 0; m < 4; ++m)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) S[m][i] = from ? from[(32 * m + dim(i)) * 128 + 32 * wave + n] : none;
+
   // Operand addresses within a stage; chunk bits are apart from the rest, so other chunks are an exclusive or away.
   const int rows = n * kRow + ((half ^ perm(n)) << 4);   // row n, dims 16 s + 8 half .. + 7: ^ s << 5
   const int j = lane & 15, b4 = (lane >> 4) & 1, trow = 8 * half + (j >> 2);
@@ -391,17 +404,6 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
   for (int i = 0; i < 16; ++i) fade[i] = power(log2_decay, kB - 1 - key_of(i));
   const float since = a.scale * power(log2_decay, n + 1);
 
-  // state: register (m, i) is key dim 32 m + dim(i), column 32 wave + n
-  auto dim = [&](int i) { return 16 * (i >> 3) + 8 * half + 4 * ((i >> 2) & 1) + (i & 3); };
-  f32x16 S[4];
-  const bool own_state = kOutputs ? !cut : p.seg == 0;   // the request's, not the workspace's or none
-  const float* from = own_state ? (si >= 0 && si < a.num_slots ? a.states + si * slot + (int64_t)h * kState : nullptr)
-                      : kOutputs ? ws : nullptr;
-  const float none = !own_state || si == -1 ? 0.f : __builtin_nanf("");
-#pragma unroll
-  for (int m = 0; m < 4; ++m)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) S[m][i] = from ? from[(32 * m + dim(i)) * 128 + 32 * wave + n] : none;
   if (!kOutputs && p.seg == 0) {   // the state before piece 0 stays: the request may advance in place
     const float f = power(log2_decay, len);
 #pragma unroll
