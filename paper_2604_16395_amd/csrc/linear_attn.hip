@@ -2,26 +2,35 @@
 //
 //   S <- l S + k_i v_i^T,   out_i = scale * q_i S      (S [128 k][128 v] in fp32, l = exp(log_decay))
 //
-// Requests of up to kShortTokens new tokens take the recurrent form: a workgroup takes 32 columns of one
+// Requests of up to kLinearShortTokens new tokens take the recurrent form: a workgroup takes 32 columns of one
 // (request, head) state.  Thread (kg, vq) keeps rows 4 kg .. + 3 and columns 4 vq .. + 3 of them in
 // registers over the request's tokens, so the state is read and written once; a row's part of q S is
-// summed over the eight row groups of a wave by lane swaps and over the four waves through LDS.
+// summed over the eight row groups of a wave by lane swaps and over the four waves through LDS.  Bound by the
+// states: 64 requests of a token, 32 heads, 270 MB, 51.6 us, 5.2 TB/s; one request 3.9 us, by its chain of loads.
 //
 // Longer chunks take the blocked form, 32 tokens at a time: with n of them valid (zero rows behind),
 //   out_i = scale (sum_{j <= i} l^(i-j) (q_i . k_j) v_j + l^(i+1) q_i S),
 //   S'    = l^n S + sum_j k_j (l^(n-1-j) v_j)^T,
-// all products on v_mfma_f32_32x32x16_bf16.  A workgroup of four waves takes one head of one piece of a
-// request; wave w owns columns 32 w .. + 31 of S (64 accumulators a lane) and of the output, and every
-// wave forms the block's 32 x 32 scores itself, so waves share nothing but the Q, K and V tiles.
-//   * Scores come out transposed (A = K rows, B = Q rows), so that each lane holds one query i and the
-//     keys j = 8 b + 4 half + a, the order in which the transposing LDS read (ds_read_b64_tr_b16) hands
-//     out V's and K's columns: P is an operand of the next product as it stands.
+// all products on the bf16 MFMA.  A workgroup of four waves takes one head of one piece of a request; wave w owns
+// columns 32 w .. + 31 of S (64 accumulators a lane) and of the output.  Waves share the Q, K and V tiles, and
+// the block's scores, of which each forms a quarter (16 x 16), one block ahead.
+//   * Scores come out transposed (A = K rows, B = Q rows): a lane holds one query and four keys, which it
+//     writes as a part of that query's row; the rows are read back as an operand against V's columns, which the
+//     transposing LDS read (ds_read_b64_tr_b16) hands out in the same order of keys.
 //   * Accumulator row 16 s + 8 b + 4 half + a of a state tile holds key dim 16 s + 8 half + 4 b + a of it
 //     (the K columns are read in that order), so that S^T is an operand against Q's rows as they lie.
-//   * Factors that are no bf16 values are sums of bf16 terms: P and S (for the output, bf16 in the end)
-//     two, off by 2^-17; l^(n-1-j) v (for the state, fp32) three, exact to 2^-25.
-// A piece of a chunk needs the state before it.  Chunks that are cut take three launches: the pieces' own
-// states, each in its slot of the workspace; their running sum under the decay; then the blocks.
+//   * Factors that are no bf16 values are sums of bf16 terms.  For outputs, bf16 in the end, two terms do (scores,
+//     S, and l^(n-1-j) v in the running S of a piece: off by 2^-16); for the state that the call returns three,
+//     off by 2^-24.  One term in S would save 2% of a long prompt's time and make the error against 64 bits
+//     1.4 times that of the final rounding alone.
+// Two workgroups fit a CU (80 KiB of LDS, 256 registers a lane).  16 columns a wave and eight waves a workgroup took 1.25
+// times as long: every wave reads all of K and Q from LDS.
+//
+// A piece of a chunk needs the state before it.  Chunks that are cut take three launches: what each piece alone
+// makes of its tokens, in its place of the workspace; their running sum under the decay; then the blocks,
+// which read K and V a second time.  Bound by the memory: 32768 tokens of 32 heads, 1.08 GB, 386 us (130 for the
+// pieces' own states, 12 for the sums, 244 to 290 for the blocks; 362 with the loads and stores alone).  Short
+// chunks are bound by the blocks one after another, 1.9 us each with one workgroup on a CU: 512 tokens 28.4 us.
 #include "launch.h"
 #include "s2l_device.h"
 

@@ -79,7 +79,10 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a) {
   const int oa = pairs_apart ? 8 * unit : 16 * unit, ob = pairs_apart ? oa + half : oa + 8;
 
   RowPlace at{0, 0};
-  if (kAppend || a.positions == nullptr) at = place_row(a.prefix_lens, a.cu_chunk, a.num_reqs, (int32_t)row);
+  if (kAppend || a.positions == nullptr) {
+    if (row >= a.cu_chunk[a.num_reqs]) return;   // the device lengths hold less than the host copies: no row's page
+    at = place_row(a.prefix_lens, a.cu_chunk, a.num_reqs, (int32_t)row);
+  }
 
   u32x4 xa[kHeads], xb[kHeads];
 #pragma unroll

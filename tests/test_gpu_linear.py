@@ -274,3 +274,89 @@ def test_a_hybrid_step():
     o_ref = ref_batch_attn(bf16_bits_to_f32(from_bf16(q)).astype(np.float64), from_bf16(cache.k_pages), from_bf16(cache.v_pages),
                            tables, P.astype(np.int32), C.astype(np.int32), np.concatenate([[0], np.cumsum(C)]).astype(np.int32), hq, SCALE)[0]
     assert float(np.abs(bf16_to_f64(out) - o_ref).max()) <= 2e-2
+
+
+@pytest.mark.parametrize("hq,hkv", [(32, 4), (6, 3)])
+def test_many_requests(hq, hkv):
+    """More requests than one search step holds, whole and cut, short and empty ones among them."""
+    rng = np.random.default_rng(24)
+    C = np.concatenate([rng.integers(0, 8, 60), rng.integers(6, 300, 70), [700, 0, 5, 6]])
+    rng.shuffle(C)
+    long = int(np.argmax(C))
+    Step(C, hq, hkv, seed=24).run_and_check([0, 1, 63, 64, 65, 127, 128, 133, long])
+
+
+def test_whole_chunks_of_many_heads():
+    """Enough workgroups that no chunk is cut: states in place, with and without one to begin with."""
+    C = [200, 64, 129, 31, 200, 96, 200, 7, 200, 200, 161, 33]
+    s = Step(C, 64, 8, seed=25, slot_in=[0, -1, 2, 3, 4, 5, 6, -1, 8, 9, 10, 11], slot_out=list(range(12)), num_slots=12)
+    assert s2l.s2l_linear_attn_workspace_bytes(s.batch, 64) == 0
+    s.run_and_check([0, 1, 3, 7, 11])
+
+
+def test_rows_shared_and_far_apart():
+    """A key row for all tokens (stride 0), and rows further apart than the fast copies take."""
+    for C in ([3], [70], [300]):
+        s = Step(C, 2, 2, seed=26)
+        s.k = s.k[:1].expand(s.T, 2, 128)
+        s.run_and_check()
+    s = Step([9], 2, 2, seed=27)
+    far = torch.empty(9 * ((1 << 24) + 8), dtype=torch.bfloat16, device=DEV).view(9, -1)[:, :256].unflatten(1, (2, 128))
+    s.q = far.copy_(s.q[:9])
+    s.run_and_check()
+
+
+def test_workspace():
+    s = Step([900, 40], 2, 2, seed=28)
+    need = s2l.s2l_linear_attn_workspace_bytes(s.batch, 2)
+    assert need > 0
+    before = [s.states.clone(), s.out.clone()]
+    for ws in (None, torch.empty(need - 1, dtype=torch.uint8, device=DEV)):
+        with pytest.raises(s2l.S2LError) as e:
+            s2l.s2l_linear_attn(s.state, s.batch, s.q, s.k, s.v, SCALE, s.out, ws)
+        assert e.value.status == -3
+    odd = torch.empty(need + 32, dtype=torch.uint8, device=DEV)[4:]
+    with pytest.raises(s2l.S2LError) as e:
+        s2l.s2l_linear_attn(s.state, s.batch, s.q, s.k, s.v, SCALE, s.out, odd)
+    assert e.value.status == -1
+    torch.cuda.synchronize()
+    assert same(s.states, before[0]) and same(s.out, before[1])
+    # nothing is expected of what a workspace holds, and nothing past its end is written
+    ws = torch.full((need + 4096,), 0xFF, dtype=torch.uint8, device=DEV)
+    s.before = before[0]
+    s2l.s2l_linear_attn(s.state, s.batch, s.q, s.k, s.v, SCALE, s.out, ws)
+    torch.cuda.synchronize()
+    s.check()
+    assert bool((ws[need:] == 0xFF).all())
+
+
+def test_an_empty_batch():
+    s = Step([0, 0], 2, 1, seed=29, slot_in=[1, -1], slot_out=[2, 3], num_slots=4)
+    s.run_and_check()
+    none = s2l.Batch([], [], np.zeros((0, 1), np.int32))
+    empty = torch.zeros(0, dtype=torch.int32, device=DEV)
+    rows = torch.zeros((0, 2, 128), dtype=torch.bfloat16, device=DEV)
+    assert s2l.s2l_linear_attn_workspace_bytes(none, 2) == 0
+    s2l.s2l_linear_attn(s2l.LinearState(s.states, s.state.log_decay, empty, empty), none, rows, rows, rows, SCALE, rows)
+    rope = s2l.Rope(torch.ones(64, device=DEV))
+    s2l.s2l_rope_qk(none, rope, rows, rows)
+    cache = s2l.PagedKVCache(*(torch.zeros((1, 2, 16, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2)))
+    s2l.s2l_rope_kv_append(cache, none, rope, None, None, rows, rows)
+    torch.cuda.synchronize()
+    assert not bool(cache.k_pages.any())
+
+
+def test_two_streams_at_once():
+    """Two batches on two streams, each with its own workspace, give what they give alone."""
+    a, b = Step([700, 3], 4, 4, seed=30), Step([90, 1200, 1], 4, 2, seed=31)
+    for s in (a, b):
+        s.run()
+        torch.cuda.synchronize()
+        s.alone = [s.out.clone(), s.states.clone()]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(3):
+        for s, stream in zip((a, b), streams):
+            s2l.s2l_linear_attn(s.state, s.batch, s.q, s.k, s.v, SCALE, s.out, s.ws, stream)
+    torch.cuda.synchronize()
+    for s in (a, b):
+        assert same(s.out, s.alone[0]) and same(s.states, s.alone[1])

@@ -282,3 +282,37 @@ def test_plain_calls_are_marshalled_natively(monkeypatch):
         got = [both(r) for r in ropes] + [linear()]
     assert all(same(a, b) for x, y in zip(ref, got) for a, b in zip(x, y))
     assert same(got[1][0], got[2][0]) and not same(got[0][0], got[1][0])
+
+
+def test_append_rotates_queries_in_place():
+    """q_out may be q: a view of the projected row that k and v are views of too."""
+    gen = torch.Generator(device=DEV).manual_seed(11)
+    P, C, hq, hkv = [7, 0], [40, 9], 8, 2
+    T = sum(C)
+    batch, rope = s2l.Batch(P, C, np.arange(8, dtype=np.int32).reshape(2, 4)), s2l.Rope(torch.from_numpy(freqs(64)).to(DEV))
+    caches = [s2l.PagedKVCache(*(torch.zeros((8, hkv, 16, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2))) for _ in range(2)]
+    qkv = rows(gen, T, hq + 2 * hkv, pad=1)
+    before, out = qkv.clone(), torch.empty((T, hq, 128), dtype=torch.bfloat16, device=DEV)
+    views = qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:]
+    s2l.s2l_rope_kv_append(caches[0], batch, rope, views[0], out, views[1], views[2])
+    s2l.s2l_rope_kv_append(caches[1], batch, rope, views[0], views[0], views[1], views[2])
+    torch.cuda.synchronize()
+    assert same(qkv[:T, :hq], out) and same(qkv[:, hq:], before[:, hq:]) and same(qkv[T:], before[T:])
+    assert same(caches[0].k_pages, caches[1].k_pages) and same(caches[0].v_pages, caches[1].v_pages)
+
+
+def test_wide_rows_take_two_heads_a_lane():
+    """Enough rows for the form with two heads a lane, head counts that fill its last group in part."""
+    gen = torch.Generator(device=DEV).manual_seed(12)
+    for hq, hkv in ((17, 2), (9, 9), (1, 33)):
+        T = 9000
+        inv = freqs(48)
+        q, k = rows(gen, T, hq), rows(gen, T, hkv)
+        q_out, k_out = torch.zeros_like(q), torch.zeros_like(k)
+        P, C = [5, 1000], [8000, 1000]
+        s2l.s2l_rope_qk(s2l.Batch(P, C, np.zeros((2, 1), np.int32)), s2l.Rope(torch.from_numpy(inv).to(DEV)), q, q_out, k, k_out)
+        torch.cuda.synchronize()
+        pick = torch.arange(0, T, 97, device=DEV)
+        pos = positions_of(P, C)[None][:, ::97]
+        check(q_out[pick], q[pick], pos, inv, [0] * 48, False)
+        check(k_out[pick], k[pick], pos, inv, [0] * 48, False)
