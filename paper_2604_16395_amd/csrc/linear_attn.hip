@@ -46,8 +46,18 @@ constexpr int kState = 128 * 128;    // elements of one state
 __device__ inline double clean_log(float g) {
   return g > 0.f ? 0.0 : g < -1e4f ? -1e4 : (double)g;
 }
-// l^n, the exponent in 64 bits so that far tokens lose nothing but the last rounding.
-__device__ inline float power(double log2_decay, int n) { return __builtin_amdgcn_exp2f((float)(log2_decay * n)); }
+// log2 of a decay in two fp32 terms, and powers of the decay: the exponent is off by its last rounding, which costs
+// l^n at most 2^-25 of itself where it matters (|x| 2^-|x| is below 0.54).
+struct Decay {
+  float hi, lo;
+  __device__ explicit Decay(float log_decay) {
+    const double l = clean_log(log_decay) * 1.4426950408889634;
+    hi = (float)l;
+    lo = (float)(l - (double)hi);
+  }
+  __device__ float exponent(int n) const { return __builtin_fmaf((float)n, lo, (float)n * hi); }
+  __device__ float power(int n) const { return __builtin_amdgcn_exp2f(exponent(n)); }
+};
 
 // Piece `seg` of request `req`: what a workgroup works on.
 struct Piece {
@@ -279,7 +289,7 @@ __device__ inline void lds_barrier() { __asm__ volatile("s_waitcnt lgkmcnt(0)\n\
 // too), and a copy of the request's state.
 // kDirect: tiles are copied straight into LDS, kStages - 1 blocks ahead; rows at addresses or strides that
 // those copies do not take go through registers, one block ahead.
-constexpr double kMostBehind = 60.0;
+constexpr float kMostBehind = 60.f;
 constexpr int kScores = kB * 2 * kB;     // bytes of a block's scores in one term: rows of a query's 32 bf16
 template <bool kOutputs, bool kDirect>
 __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
@@ -297,6 +307,7 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
   const int h0 = (int)(blockIdx.x / 8) % group;
   if (unit >= a.num_units * a.hkv) return;
   const int g = unit % a.hkv, h = g * group + h0;
+  const float log_decay = a.log_decay[h];
   Piece p = find_unit<kOutputs ? kPieces : kCutPieces>(a, unit / a.hkv);
   if (p.req < 0) return;
   p.seg = __builtin_amdgcn_readfirstlane(p.seg);
@@ -372,6 +383,7 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
   // state: register (m, i) is key dim 32 m + dim(i), column 32 wave + n
   auto dim = [&](int i) { return 16 * (i >> 3) + 8 * half + 4 * ((i >> 2) & 1) + (i & 3); };
   f32x16 S[4];
+  const Decay decay(log_decay);
   const bool own_state = kOutputs ? !cut : p.seg == 0;   // the request's, not the workspace's or none
   const float* from = own_state ? (si >= 0 && si < a.num_slots ? a.states + si * slot + (int64_t)h * kState : nullptr)
                       : kOutputs ? ws : nullptr;
@@ -402,19 +414,18 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
 #pragma unroll
   for (int k2 = 0; k2 < 2; ++k2) score_from[k2] = n * 2 * kB + (((2 * k2 + half) ^ ((n >> 2) & 3)) << 4);
 
-  const double log_decay = clean_log(a.log_decay[h]), log2_decay = log_decay * 1.4426950408889634;
   auto key_of = [&](int i) { return 16 * (i >> 3) + 8 * half + (i & 7); };   // of a column operand's element
   float within[4], fade[16];   // scale l^(query - key), 0 for later keys; l^(kB-1-key)
   if constexpr (kOutputs) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) within[i] = query0 >= key0 + i ? a.scale * power(log2_decay, query0 - key0 - i) : 0.f;
+    for (int i = 0; i < 4; ++i) within[i] = query0 >= key0 + i ? a.scale * decay.power(query0 - key0 - i) : 0.f;
   }
 #pragma unroll
-  for (int i = 0; i < 16; ++i) fade[i] = power(log2_decay, kB - 1 - key_of(i));
-  const float since = a.scale * power(log2_decay, n + 1);
+  for (int i = 0; i < 16; ++i) fade[i] = decay.power(kB - 1 - key_of(i));
+  const float since = a.scale * decay.power(n + 1);
 
   if (!kOutputs && p.seg == 0) {   // the state before piece 0 stays: the request may advance in place
-    const float f = power(log2_decay, len);
+    const float f = decay.power(len);
 #pragma unroll
     for (int m = 0; m < 4; ++m)
 #pragma unroll
@@ -482,15 +493,15 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
     // when it is behind by a factor of more than 2^kMostBehind (or at the end), and what joins it is blown up
     // by as much.
     const int after = behind + valid;
-    const bool fades = kOutputs && (b + 1 == blocks || -log2_decay * after > kMostBehind);
+    const bool fades = kOutputs && (b + 1 == blocks || -decay.exponent(after) > kMostBehind);
     float f[16];
     if (valid == kB) {
-      const float join = power(log2_decay, kOutputs ? (fades ? 0 : -after) : len - (nth(b) + 1) * kB);
+      const float join = decay.power(kOutputs ? (fades ? 0 : -after) : len - (nth(b) + 1) * kB);
 #pragma unroll
       for (int i = 0; i < 16; ++i) f[i] = fade[i] * join;
     } else {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) f[i] = power(log2_decay, max(valid - 1 - key_of(i), 0));
+      for (int i = 0; i < 16; ++i) f[i] = decay.power(max(valid - 1 - key_of(i), 0));
     }
 
     bool bad = false;
@@ -543,7 +554,7 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
         o = mfma(sx.t[0], q, o);
       }
       if (fades) {
-        const float by = power(log2_decay, after);
+        const float by = decay.power(after);
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
@@ -562,7 +573,7 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
     };
     join_state(vx[0].t, vx[1].t, kTerms);
     if constexpr (kOutputs) {
-      const float reach = since * power(log2_decay, behind);
+      const float reach = since * decay.power(behind);
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[i] *= reach;
 #pragma unroll
@@ -646,12 +657,12 @@ __global__ __launch_bounds__(256) void linear_carry_kernel(LinearLaunch a) {
     ws += __builtin_amdgcn_readlane(sum, 63);
   }
   if (pieces == 0 || ws + pieces >= a.ws_states) return;
-  const double log_decay = clean_log(a.log_decay[h]);
-  const float fade = (float)exp(log_decay * a.piece_tokens), fade_last = (float)exp(log_decay * (len - (pieces - 1) * a.piece_tokens));
   const int so = a.slot_out[req];
   const int64_t slot = (int64_t)a.hq * kState, at = (int64_t)h * kState / 4 + blockIdx.x * 256 + threadIdx.x;
   f32x4* p = reinterpret_cast<f32x4*>(a.ws + ws * slot) + at;
   f32x4 sum = p[slot / 4];
+  const double log_decay = clean_log(a.log_decay[h]);
+  const float fade = (float)exp(log_decay * a.piece_tokens), fade_last = (float)exp(log_decay * (len - (pieces - 1) * a.piece_tokens));
   constexpr int kAhead = 8;   // loads do not wait for one another
   for (int s0 = 2; s0 <= pieces; s0 += kAhead) {
     f32x4 x[kAhead];
