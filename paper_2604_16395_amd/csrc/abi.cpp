@@ -638,29 +638,56 @@ double linear_cost(const s2l_batch* b, int32_t hq, int32_t num_cus, int64_t piec
   return t;
 }
 
-// How linear attention cuts the batch: requests stay whole unless shorter pieces are estimated to be faster.
-// Against the fastest of the measured piece lengths of each of those batches the choice takes 1.01 of the time in the
-// geometric mean and 1.09 at most (examples, 32 heads: 2048 tokens whole 131 us, in pieces of 256 46 us; 16 requests
-// of 1024 tokens whole 139 us, in pieces of 512 241).
-s2l::LinearPlan linear_plan(const s2l_batch* b, int32_t hq, int32_t num_cus) {
-  s2l::LinearPlan p = {};
-  int64_t longest = 0, total = 0;
+// The same for whole requests with half of a head's columns a workgroup.  A block takes 1.62 us with a CU to itself
+// and 2.12 us with two workgroups on it; busy CUs take 1.35 us for each and 1.5 us for each unit's states, and units
+// of equal length come in rounds, of 1.5 us a block and 2.2 us.
+double linear_narrow_cost(const s2l_batch* b, int32_t hq, int32_t num_cus) {
+  double units = 0, blocks = 0, longest = 0;
   for (int32_t r = 0; r < b->num_reqs; ++r) {
     const int32_t c = b->chunk_lens_host[r];
     if (c <= s2l::kLinearShortTokens) continue;
+    const double n = (double)s2l::ceil_div64(c, s2l::kLinearBlockTokens);
+    units += 1;
+    blocks += n;
+    longest = std::max(longest, n);
+  }
+  const double per_cu = 2.0 * hq / num_cus, rounds = std::ceil(units * per_cu - 1e-9), mean = blocks / units;
+  return 5.1 + std::max({longest * (1.62 + 0.25 * std::min(2.0, units * per_cu)), (1.35 * blocks + 1.5 * units) * per_cu,
+                         rounds * (1.5 * mean * mean / longest + 2.2)});
+}
+
+// How linear attention cuts the batch: requests stay whole unless shorter pieces are estimated to be faster, and a
+// head of a whole request gets two workgroups where that is estimated to be faster still: its blocks' chain is
+// shorter, but every block costs 1.25 times as much.  32 heads, one workgroup a head and two: a chunk of 64 tokens
+// 10.1 us and 8.4, of 256 22.0 and 18.1; 8 requests of 389 to 1024 tokens 79 and 72, 16 of 512 89 and 109.
+// Against the fastest of the measured piece lengths of each of those batches the choice takes 1.01 of the time in the
+// geometric mean and 1.13 at most (examples, 32 heads: 2048 tokens whole 131 us, in pieces of 256 46 us; 16 requests
+// of 1024 tokens whole 139 us, in pieces of 512 241).
+s2l::LinearPlan linear_plan(const s2l_batch* b, int32_t hq, int32_t num_cus) {
+  s2l::LinearPlan p = {};
+  int64_t longest = 0, total = 0, units = 0;
+  for (int32_t r = 0; r < b->num_reqs; ++r) {
+    const int32_t c = b->chunk_lens_host[r];
+    if (c <= s2l::kLinearShortTokens) continue;
+    ++units;
     longest = std::max(longest, s2l::ceil_div64(c, s2l::kLinearBlockTokens));
     total += s2l::ceil_div64(c, s2l::kLinearBlockTokens);
   }
   int64_t blocks = std::max<int64_t>(longest, 1);
+  double best = linear_cost(b, hq, num_cus, blocks);
   // more pieces only add work: of no use where the CUs have enough of it without
   if ((double)total * hq < 2 * (double)longest * num_cus) {
-    double best = linear_cost(b, hq, num_cus, blocks);
     for (const int64_t n : {2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {
       const int64_t k = s2l::ceil_div64(longest, n);
       if (k < 2 && n > 2) break;
       const double cost = linear_cost(b, hq, num_cus, k);
       if (cost < best) best = cost, blocks = k;
     }
+  }
+  // with more units the CUs are busy either way; the other estimate is some 5 % low for uneven chunks
+  if (units > 0 && (double)units * hq <= 16.0 * num_cus && linear_narrow_cost(b, hq, num_cus) < 1.05 * best) {
+    p.narrow = true;
+    blocks = std::max<int64_t>(longest, 1);
   }
   p.piece_tokens = (int32_t)(blocks * s2l::kLinearBlockTokens);
   for (int32_t r = 0; r < b->num_reqs; ++r) {

@@ -133,6 +133,7 @@ struct LinearPlan {          // how the batch is cut, from the host lengths
   int32_t pieces;            // of all requests that are not short
   int32_t cut_reqs, ws_states;   // requests of more than one piece; one state before, between and after them
   int32_t short_reqs;
+  bool narrow;               // no request is cut, and a workgroup takes half of a head's columns
 };
 hipError_t launch_linear_attn(const LinearLaunch& a, const LinearPlan& plan, hipStream_t stream);
 

@@ -24,13 +24,15 @@
 //     off by 2^-24.  One term in S would save 2% of a long prompt's time and make the error against 64 bits
 //     1.4 times that of the final rounding alone.
 // Two workgroups fit a CU (80 KiB of LDS, 256 registers a lane).  16 columns a wave and eight waves a workgroup took 1.25
-// times as long: every wave reads all of K and Q from LDS.
+// times as long: every wave reads all of K and Q from LDS.  Few whole chunks take 16 columns a wave all the same, and
+// two workgroups a head (linear_narrow_kernel).
 //
 // A piece of a chunk needs the state before it.  Chunks that are cut take three launches: what each piece alone
 // makes of its tokens, in its place of the workspace; their running sum under the decay; then the blocks,
-// which read K and V a second time.  Bound by the memory: 32768 tokens of 32 heads, 1.08 GB, 386 us (130 for the
-// pieces' own states, 12 for the sums, 244 to 290 for the blocks; 362 with the loads and stores alone).  Short
-// chunks are bound by the blocks one after another, 1.9 us each with one workgroup on a CU: 512 tokens 28.4 us.
+// which read K and V a second time.  Bound by the memory: 32768 tokens of 32 heads, 1.08 GB, 380 us (130 for the
+// pieces' own states, 12 for the sums, 233 to 290 for the blocks; 362 with the loads and stores alone).  Short
+// chunks are bound by the blocks one after another and by the start of each launch (a unit's search 1 us, its states
+// and first tiles 3): 32 heads, 64 tokens 8.4 us, 256 18.1, 512 28 to 32 either way, 2048 in pieces 49.
 #include "launch.h"
 #include "s2l_device.h"
 
@@ -234,6 +236,14 @@ __device__ inline bf16x8 read_columns(const uint8_t* x, const uint8_t* y) {
 }
 __device__ inline bf16x8 read_row(const uint8_t* p) { return *reinterpret_cast<const bf16x8*>(p); }
 
+__device__ inline bf16x8 read_halves(const uint8_t* x, const uint8_t* y) {
+  const u32x2 a = *reinterpret_cast<const u32x2*>(x), b = *reinterpret_cast<const u32x2*>(y);
+  return __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
+}
+
+__device__ inline f32x4 mfma16(const bf16x8& a, const bf16x8& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
 __device__ inline f32x16 mfma(const bf16x8& a, const bf16x8& b, const f32x16& c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
@@ -629,6 +639,282 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
   }
 }
 
+// The blocked form of whole chunks with half of a head's columns a workgroup, 16 a wave.  Where there are few
+// workgroups, the blocks one after another are the time, and a wave has half as much to do in each: 1.62 us a block
+// instead of 1.94.  Where there are many, reading K and Q for half as many columns costs 1.25 times as much.
+// Other than above, products are 16 x 16 x 32 and state register (t, i) is key dim 16 t + 4 quarter + i of column
+// n: two of its quads are an operand's eight key dims, and Q's rows are read in the same halves.
+template <bool kDirect>
+__global__ __launch_bounds__(256, 2) void linear_narrow_kernel(LinearLaunch a) {
+  constexpr int kTiles = 3, kStages = 3, kStage = kTiles * kTile, kRing = kStages * kStage;
+  constexpr int kCopies = 2 * kTiles, kStores = 2;   // a wave's, for a block
+  __shared__ __attribute__((aligned(1024))) uint8_t s_ring[kRing];
+  __shared__ __attribute__((aligned(1024))) uint8_t s_score[4 * kScores];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 15, quarter = lane >> 4;
+  const int group = a.hq / a.hkv;
+  // the workgroups of one key head's queries follow one another on one XCD, which then reads K and V once
+  const int unit = (int)(blockIdx.x / (16 * group)) * 8 + (int)(blockIdx.x % 8);
+  const int h0 = (int)(blockIdx.x / 8) % (2 * group);
+  if (unit >= a.num_units * a.hkv) return;
+  const int g = unit % a.hkv, h = g * group + (h0 >> 1), col0 = 64 * (h0 & 1) + 16 * wave;
+  const float log_decay = a.log_decay[h];
+  Piece p = find_unit<kPieces>(a, unit / a.hkv);
+  if (p.req < 0) return;
+  const int len = __builtin_amdgcn_readfirstlane(p.len), blocks = (len + kB - 1) / kB;
+  const int64_t row0 = __builtin_amdgcn_readfirstlane(p.row);
+  const int si = __builtin_amdgcn_readfirstlane(p.slot_in), so = __builtin_amdgcn_readfirstlane(p.slot_out);
+  const int64_t slot = (int64_t)a.hq * kState;
+
+  // this wave's rows 8 wave + 4 d + (lane / 16) of each tile, 16 bytes a lane
+  const int srow = 8 * wave + quarter;
+  const uint16_t* src[3] = {a.k + row0 * a.k_stride + g * 128, a.v + row0 * a.v_stride + g * 128, a.q + row0 * a.q_stride + h * 128};
+  const int64_t stride[3] = {a.k_stride, a.v_stride, a.q_stride};
+  const uint32_t ring0 = (uint32_t)(uintptr_t)(lds_void*)s_ring;
+  uint32_t off[kTiles][2];
+  u32x4 st[kTiles][2];
+  auto copy = [&](int block, int at) {      // straight into LDS; rows past the chunk read as zero
+    const int rows = min(kB, len - block * kB);
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      const i32x4 rs = sgpr_rsrc(src[t] + (int64_t)block * kB * stride[t], (rows - 1) * (int32_t)stride[t] * 2 + kRow);
+#pragma unroll
+      for (int d = 0; d < 2; ++d)
+        lds_dma_b128(rs, off[t][d], __builtin_amdgcn_readfirstlane(ring0 + at + t * kTile + (8 * wave + 4 * d) * kRow));
+    }
+  };
+  auto load = [&](int block) {
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int d = 0; d < 2; ++d) {
+        const int64_t row = (int64_t)block * kB + srow + 4 * d;
+        st[t][d] = u32x4{};
+        if (row < len) st[t][d] = *reinterpret_cast<const u32x4_any*>(src[t] + row * stride[t] + 8 * n);
+      }
+  };
+  auto store = [&](int at) {
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int d = 0; d < 2; ++d) {
+        const int row = srow + 4 * d;
+        *reinterpret_cast<u32x4*>(s_ring + at + t * kTile + row * kRow + ((n ^ perm(row)) << 4)) = st[t][d];
+      }
+  };
+  if constexpr (kDirect) {
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int d = 0; d < 2; ++d) {
+        const int row = srow + 4 * d;
+        off[t][d] = (uint32_t)row * (uint32_t)stride[t] * 2 + ((n ^ perm(row)) << 4);
+      }
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s)
+      if (s < blocks) copy(s, s * kStage);
+  } else {
+    load(0);
+  }
+
+  const Decay decay(log_decay);
+  const int state0 = 4 * quarter * 128 + col0 + n;
+  f32x4 S[8];
+  const float* from = si >= 0 && si < a.num_slots ? a.states + si * slot + (int64_t)h * kState : nullptr;
+  const float none = si == -1 ? 0.f : __builtin_nanf("");
+#pragma unroll
+  for (int t = 0; t < 8; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) S[t][i] = from ? from[state0 + (16 * t + i) * 128] : none;
+
+  // Operand addresses within a stage; chunk bits are apart from the rest, so other chunks are an exclusive or away.
+  // Scores: dims 32 s + 8 quarter .. + 7 of a row, ^ s << 6.  Against the state: dims 32 s + 4 quarter .. + 3, and 16
+  // on (^ 32), of row n, ^ s << 6.  Columns: lane n of a quarter addresses columns 4 (n % 4) .. + 3 of row
+  // 8 quarter + n / 4, and of the fourth on; key dims 16 t .. + 15: ^ t << 5.
+  const int row8 = 2 * kTile + n * kRow + (((quarter >> 1) ^ perm(n)) << 4) + 8 * (quarter & 1);
+  int kcol[2], vcol[2];
+#pragma unroll
+  for (int y = 0; y < 2; ++y) {
+    const int row = 8 * quarter + 4 * y + (n >> 2), chunk = (n >> 1) & 1;
+    kcol[y] = row * kRow + ((chunk ^ perm(row)) << 4) + 8 * (n & 1);
+    vcol[y] = kTile + row * kRow + (((col0 / 8 + chunk) ^ perm(row)) << 4) + 8 * (n & 1);
+  }
+  // this wave's 16 queries by 16 keys; results are keys key0 .. + 3 of query0
+  const int query0 = 16 * (wave >> 1) + n, key0 = 16 * (wave & 1) + 4 * quarter;
+  const int krow = (16 * (wave & 1) + n) * kRow + ((quarter ^ perm(n)) << 4);
+  const int qrow = 2 * kTile + query0 * kRow + ((quarter ^ perm(n)) << 4);
+  const int score_to = query0 * 2 * kB + (((key0 >> 3) ^ ((query0 >> 2) & 3)) << 4) + 8 * (quarter & 1);
+  const int score_from = n * 2 * kB + ((quarter ^ ((n >> 2) & 3)) << 4);   // keys 8 quarter .. + 7 of queries n, n + 16
+
+  float within[4], fade[8];   // scale l^(query - key), 0 for later keys; l^(kB-1-key) of key 8 quarter + i
+#pragma unroll
+  for (int i = 0; i < 4; ++i) within[i] = query0 >= key0 + i ? a.scale * decay.power(query0 - key0 - i) : 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) fade[i] = decay.power(kB - 1 - 8 * quarter - i);
+  const float since[2] = {a.scale * decay.power(n + 1), a.scale * decay.power(n + 17)};
+
+  if constexpr (!kDirect) {
+    store(0);
+    if (1 < blocks) {
+      load(1);
+      store(kStage);
+      if (2 < blocks) load(2);
+    }
+  }
+  auto scores = [&](int stage, int parity) {
+    f32x4 sc{};
+#pragma unroll
+    for (int s = 0; s < 4; ++s) sc = mfma16(read_row(s_ring + ((stage + krow) ^ s << 6)), read_row(s_ring + ((stage + qrow) ^ s << 6)), sc);
+    float y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = query0 >= key0 + i ? sc[i] * within[i] : 0.f;
+    uint8_t* const to = s_score + 2 * kScores * parity + score_to;
+    const uint32_t w0 = pack_bf16x2(y[0], y[1]), w1 = pack_bf16x2(y[2], y[3]);
+    *reinterpret_cast<u32x2*>(to) = u32x2{w0, w1};
+    take_off(w0, y[0], y[1]);
+    take_off(w1, y[2], y[3]);
+    *reinterpret_cast<u32x2*>(to + kScores) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+  };
+  if (kDirect && blocks > 1) tile_barrier<kCopies>();
+  else if (kDirect) tile_barrier<0>();
+  else lds_barrier();
+  scores(0, 0);
+
+  int behind = 0;      // tokens that S has yet to fade by: the state is l^behind S
+  int at = 0;          // the block's stage
+  for (int b = 0; b < blocks; ++b) {
+    // the next block's tile has to be there too, for its scores
+    if constexpr (!kDirect) lds_barrier();
+    else if (b == 0) tile_barrier<0>();
+    else if (b + 1 < blocks) tile_barrier<kStores>();
+    else lds_barrier();
+    const int next = at + kStage == kRing ? 0 : at + kStage;
+    if constexpr (kDirect) {
+      // the stage before this one's is read out
+      if (b + 2 < blocks) copy(b + 2, at == 0 ? kRing - kStage : at - kStage);
+      __asm__ volatile("" ::: "memory");   // the block's stores are younger than the copies
+    }
+    const int valid = min(kB, len - b * kB);
+    const bf16x8 vc = read_columns(s_ring + at + vcol[0], s_ring + at + vcol[1]);
+    u32x4 vw = __builtin_bit_cast(u32x4, vc);
+
+    // values of v that are not finite: as above
+    float probe = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) probe = probe_bf16x2(vw[i], probe);
+    const bool bad = __ballot(probe != probe) != 0;
+    int bad_row = kB;    // the first such row of column n
+    if (bad) {
+      int from_row = kB;
+#pragma unroll
+      for (int i = 7; i >= 0; --i) {
+        const uint32_t w = vw[i >> 1], bits = i & 1 ? w >> 16 : w & 0xFFFFu;
+        if ((bits & 0x7F80u) == 0x7F80u) {
+          from_row = 8 * quarter + i;
+          vw[i >> 1] = w & (i & 1 ? 0x0000FFFFu : 0xFFFF0000u);
+        }
+      }
+      from_row = min(from_row, __shfl_xor(from_row, 16, 64));
+      bad_row = min(from_row, __shfl_xor(from_row, 32, 64));
+    }
+
+    const int after = behind + valid;
+    const bool fades = b + 1 == blocks || -decay.exponent(after) > kMostBehind;
+    float f[8];
+    if (valid == kB) {
+      const float join = decay.power(fades ? 0 : -after);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = fade[i] * join;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = decay.power(max(valid - 1 - 8 * quarter - i, 0));
+    }
+
+    // the next block's scores (of a block that there is not: of what lies there, and not used)
+    scores(next, (b + 1) & 1);
+    float x[8];
+    {
+      const u32x4 w = __builtin_bit_cast(u32x4, vc);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = (i & 1 ? bf16hi(w[i >> 1]) : bf16lo(w[i >> 1])) * f[i];
+    }
+    const Terms<3> vx = split<3>(x);
+
+    f32x4 o[2] = {};
+    const int row = at + row8;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      float z[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) z[i] = S[2 * s + (i >> 2)][i & 3];
+      const Terms<2> sx = split<2>(z);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const bf16x8 q = read_halves(s_ring + (row ^ s << 6) + 16 * u * kRow, s_ring + (row ^ (s << 6 | 32)) + 16 * u * kRow);
+        o[u] = mfma16(sx.t[1], q, o[u]);
+        o[u] = mfma16(sx.t[0], q, o[u]);
+      }
+    }
+    if (fades) {
+      const float by = decay.power(after);
+#pragma unroll
+      for (int t = 0; t < 8; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) S[t][i] *= by;
+    }
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      const bf16x8 kk = read_columns(s_ring + ((at + kcol[0]) ^ t << 5), s_ring + ((at + kcol[1]) ^ t << 5));
+#pragma unroll
+      for (int i = 2; i >= 0; --i) S[t] = mfma16(kk, vx.t[i], S[t]);
+    }
+    const float late = decay.power(behind);
+    const bf16x8 vv = __builtin_bit_cast(bf16x8, vw);
+    uint16_t* dst = a.out + (row0 + b * kB + n) * a.out_stride + h * 128 + col0 + 4 * quarter;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const float reach = since[u] * late;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[u][i] *= reach;
+      const uint8_t* sr = s_score + 2 * kScores * (b & 1) + score_from + 16 * u * 2 * kB;
+      o[u] = mfma16(vv, read_row(sr + kScores), o[u]);
+      o[u] = mfma16(vv, read_row(sr), o[u]);
+    }
+    if (bad) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (16 * u + n >= __shfl(bad_row, 4 * quarter + i, 64)) o[u][i] = __builtin_nanf("");
+    }
+    const u32x2 y[2] = {{pack_bf16x2(o[0][0], o[0][1]), pack_bf16x2(o[0][2], o[0][3])},
+                        {pack_bf16x2(o[1][0], o[1][1]), pack_bf16x2(o[1][2], o[1][3])}};
+    if (valid == kB) {       // kStores stores, which the next tile_barriers count on
+      *reinterpret_cast<u32x2_any*>(dst) = y[0];
+      *reinterpret_cast<u32x2_any*>(dst + 16 * a.out_stride) = y[1];
+    } else {
+      if (n < valid) *reinterpret_cast<u32x2_any*>(dst) = y[0];
+      if (n + 16 < valid) *reinterpret_cast<u32x2_any*>(dst + 16 * a.out_stride) = y[1];
+    }
+    behind = fades ? 0 : after;
+    at = next;
+    if constexpr (!kDirect) {
+      if (b + 2 < blocks) {
+        store(next + kStage == kRing ? 0 : next + kStage);
+        if (b + 3 < blocks) load(b + 3);
+      }
+    }
+  }
+
+  if (so >= 0 && so < a.num_slots) {
+    float* to = a.states + so * slot + (int64_t)h * kState;
+#pragma unroll
+    for (int t = 0; t < 8; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) to[state0 + (16 * t + i) * 128] = S[t][i];
+  }
+}
+
 // The states between the pieces of cut requests: workspace entry s + 1 of a request holds what piece s
 // alone makes of its tokens (piece 0: of the request's state too), and gets the sum with the entry before it, faded
 // by piece s; the last one goes to the request's slot.  A thread takes four elements of one head's
@@ -700,7 +986,12 @@ hipError_t launch_linear_attn(const LinearLaunch& launch, const LinearPlan& plan
     else linear_block_kernel<false, false><<<blocks(a.num_units), 256, 0, stream>>>(a);
     linear_carry_kernel<<<dim3(kState / 1024, a.hq, plan.cut_reqs), 256, 0, stream>>>(a);
   }
-  if (plan.pieces > 0) {
+  if (plan.pieces > 0 && plan.narrow) {
+    a.num_units = plan.pieces;
+    const dim3 grid((uint32_t)(((int64_t)a.num_units * a.hkv + 7) / 8 * 16 * group));
+    if (qkv) linear_narrow_kernel<true><<<grid, 256, 0, stream>>>(a);
+    else linear_narrow_kernel<false><<<grid, 256, 0, stream>>>(a);
+  } else if (plan.pieces > 0) {
     a.num_units = plan.pieces;
     if (qkv) linear_block_kernel<true, true><<<blocks(a.num_units), 256, 0, stream>>>(a);
     else linear_block_kernel<true, false><<<blocks(a.num_units), 256, 0, stream>>>(a);

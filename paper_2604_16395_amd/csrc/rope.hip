@@ -9,7 +9,7 @@
 // follow one another); lane l holds unit l % 8 of head l / 8, the 16 elements of 8 pairs in two 16-byte
 // chunks, so that a lane's 8 sines and cosines serve all its heads and rows of a head are read and
 // written whole.  Units past the rotated dims, and V's, are copied.  Nothing is shared between waves: no LDS, no barrier.
-// Bound by the memory for many rows: 35104 rows of 32 + 8 + 8 heads, 863 MB, 158 us, 5.5 TB/s (168 with one head a
+// Bound by the memory for many rows: 35107 rows of 32 + 8 + 8 heads, 863 MB, 158 us, 5.5 TB/s (168 with one head a
 // lane; 217 with one head a lane and the groups of a row far apart); by the chain of loads for few: one row 3.1 us, 512
 // rows 4.5 us (4.8 with two heads a lane).
 #include "launch.h"

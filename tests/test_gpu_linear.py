@@ -294,6 +294,38 @@ def test_whole_chunks_of_many_heads():
     s.run_and_check([0, 1, 3, 7, 11])
 
 
+@pytest.mark.parametrize("R,hq,hkv", [(2, 4, 2), (5, 8, 8), (70, 64, 8)])
+def test_whole_chunks_few_and_many(R, hq, hkv):
+    """Chunks in one launch, from workgroups that wait for CUs down to less than one for each: the outputs, the same
+    at odd addresses, and values that are not finite."""
+    C = [6 + (37 * r) % 91 for r in range(R)]
+    a, b = (Step(C, hq, hkv, seed=29, slot_in=[-1] + list(range(1, R)), slot_out=list(range(R)), num_slots=R) for _ in range(2))
+    assert s2l.s2l_linear_attn_workspace_bytes(a.batch, hq) == 0
+    a.run_and_check([0, 1, R - 1])
+    odd = torch.zeros((a.T + 1, (hq + 2 * hkv) * 128 + 3), dtype=torch.bfloat16, device=DEV)[:, 1:-2].unflatten(1, (hq + 2 * hkv, 128))
+    odd.copy_(b.qkv)
+    b.q, b.k, b.v = odd[:, :hq], odd[:, hq:hq + hkv], odd[:, hq + hkv:]
+    b.run()
+    torch.cuda.synchronize()
+    assert same(a.out, b.out) and same(a.states, b.states)
+    states, clean, bad = a.before, a.out.clone(), C[0] + 33     # in the second block of request 1
+    for values in (a.q, b.q), (a.v, b.v):
+        for s, t in zip((a, b), values):
+            kept = t[bad, 1, 70].clone()
+            t[bad, 1, 70] = float("inf")
+            s.states.copy_(states)
+            s.run()
+            torch.cuda.synchronize()
+            wrong = ~torch.isfinite(s.out[:s.T].float())
+            if t is s.q:        # a query reaches its own row of its head
+                assert bool(wrong[bad, 1].all()) and int(wrong.sum()) == 128
+            else:               # a value its column of the rows from its own on, in all heads that share it
+                rows, heads = slice(bad, C[0] + C[1]), slice(hq // hkv, 2 * hq // hkv)
+                assert bool(wrong[rows, heads, 70].all()) and int(wrong.sum()) == (C[0] + C[1] - bad) * (hq // hkv)
+            assert torch.equal(s.out[:s.T][~wrong], clean[:s.T][~wrong])
+            t[bad, 1, 70] = kept
+
+
 def test_rows_shared_and_far_apart():
     """A key row for all tokens (stride 0), and rows further apart than the fast copies take."""
     for C in ([3], [70], [300]):
