@@ -208,9 +208,10 @@ typedef struct s2l_rope {
  *   q: device bf16, row i of request r at element (cu_chunk[r] + i) * q_stride, its Hq heads of 128 one
  *      after another; q_out likewise with q_out_stride.  k, k_out likewise; Hkv 0 and NULL for none.
  *      An output may be its own input with the same stride; otherwise outputs overlap nothing.
- *   Strides are in elements; of the outputs (and, beyond one row, of the inputs) at least heads * 128.
- *      Rows from T on are not touched.  Any element alignment is taken; 16 bytes are fastest.
- * Errors: EINVAL (nulls, negative or inconsistent arguments), ENOTSUP (rot_dim, axes), EHIP.
+ *   Strides are in elements; the outputs' at least heads * 128 (beyond one row), the inputs' any from 0 (one
+ *      row for all).  Rows from T on are not touched.  Any element alignment is taken; 16 bytes are fastest.
+ * Errors: EINVAL (nulls, negative or inconsistent arguments), ENOTSUP (rot_dim, axes, more than 2^26 rows of
+ *      each 16 heads), EHIP.
  */
 s2l_status s2l_rope_qk(const s2l_batch* batch, const s2l_rope* rope, const void* q, int64_t q_stride,
                        int32_t num_q_heads, void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride,
@@ -265,10 +266,12 @@ s2l_status s2l_linear_attn_workspace_bytes(const s2l_batch* batch, int32_t num_q
  *   q, k, v, out: device bf16 rows with strides as in s2l_rope_qk (Hq, Hkv, Hkv and Hq heads of 128);
  *                 out overlaps nothing that is read.  Rows from T on are not touched.
  *   workspace   : device, ws_bytes >= s2l_linear_attn_workspace_bytes(...); NULL when that is 0.
- * Precision: states and sums in fp32; where the bf16 MFMA takes a product, factors that are not bf16
- * values go as the sum of two of them (2^-16 relative) for outputs, of three for states.  A value of v that is not finite reaches the rows from
- * its own on, and the state, as a value that is not finite.
- * Errors: EINVAL, EWORKSPACE, ENOTSUP (more than 65535 requests or heads), EHIP.
+ * Precision: states and sums in fp32.  Where the bf16 MFMA takes a product, factors that are not bf16
+ * values go as the sum of two of them (2^-16 relative) for outputs, of three for states.  Chunks scale what
+ * joins a state by up to 2^60 on the way: states and products k v below 2^66 in magnitude are safe from
+ * overflow.  A value of v that is not finite reaches the rows from its own on, and the state, as a value that
+ * is not finite.
+ * Errors: EINVAL, EWORKSPACE, ENOTSUP (more than 65535 requests or heads, or 2^23 requests times heads), EHIP.
  */
 s2l_status s2l_linear_attn(const s2l_linear_state* state, const s2l_batch* batch, const void* q, int64_t q_stride,
                            const void* k, int64_t k_stride, const void* v, int64_t v_stride, int32_t num_kv_heads,

@@ -158,17 +158,22 @@ class Rope:
     (2 i, 2 i + 1) instead of (i, i + rot_dim / 2).  scale: a factor on the rotated dims."""
 
     def __init__(self, inv_freq, positions=None, pair_axes=None, adjacent=False, scale=1.0):
-        _check(inv_freq, torch.float32, "inv_freq")
-        if inv_freq.dim() != 1 or not 1 <= inv_freq.shape[0] <= HEAD_DIM // 2:
-            raise ValueError(f"inv_freq must be a vector of 1 to {HEAD_DIM // 2} pairs")
+        self.inv_freq = inv_freq
+        self._check_freq()
         pair_axes = [0] * inv_freq.shape[0] if pair_axes is None else [int(a) for a in pair_axes]
         if len(pair_axes) != inv_freq.shape[0] or min(pair_axes) < 0 or max(pair_axes) >= _lib.S2L_ROPE_MAX_AXES:
             raise ValueError(f"pair_axes must name an axis below {_lib.S2L_ROPE_MAX_AXES} for each of the "
                              f"{inv_freq.shape[0]} pairs")
-        self.inv_freq, self.positions, self.adjacent, self.scale = inv_freq, positions, bool(adjacent), float(scale)
+        self.positions, self.adjacent, self.scale = positions, bool(adjacent), float(scale)
         self.pair_axis = bytes(pair_axes) + bytes(64 - len(pair_axes))
 
+    def _check_freq(self):
+        _check(self.inv_freq, torch.float32, "inv_freq")
+        if self.inv_freq.dim() != 1 or not 1 <= self.inv_freq.shape[0] <= HEAD_DIM // 2:
+            raise ValueError(f"inv_freq must be a vector of 1 to {HEAD_DIM // 2} pairs")
+
     def c(self, total_tokens, device):
+        self._check_freq()       # the attribute may be another by now
         p = self.positions
         if p is not None and (p.dtype != torch.int32 or p.dim() not in (1, 2) or p.stride(-1) != 1 and p.shape[-1] > 1
                               or p.shape[-1] < total_tokens or p.dim() == 2 and p.shape[0] > 1 and p.stride(0) < 0):
@@ -189,17 +194,21 @@ class LinearState:
     state) is read, slot_out (-1: not kept) is written; the same slot advances in place."""
 
     def __init__(self, states, log_decay, slot_in, slot_out):
-        _check(states, torch.float32, "states")
-        _check(log_decay, torch.float32, "log_decay")
-        if states.dim() != 4 or tuple(states.shape[2:]) != (HEAD_DIM, HEAD_DIM) or log_decay.shape != states.shape[1:2]:
-            raise ValueError(f"states must be [slots][Hq][{HEAD_DIM}][{HEAD_DIM}] and log_decay [Hq]")
         self.states, self.log_decay, self.slot_in, self.slot_out = states, log_decay, slot_in, slot_out
+        self._check_states()
+
+    def _check_states(self):
+        _check(self.states, torch.float32, "states")
+        _check(self.log_decay, torch.float32, "log_decay")
+        if self.states.dim() != 4 or tuple(self.states.shape[2:]) != (HEAD_DIM, HEAD_DIM) or self.log_decay.shape != self.states.shape[1:2]:
+            raise ValueError(f"states must be [slots][Hq][{HEAD_DIM}][{HEAD_DIM}] and log_decay [Hq]")
 
     @property
     def num_heads(self):
         return self.states.shape[1]
 
     def c(self, num_reqs, device):
+        self._check_states()     # the attributes may be others by now
         for t, name in ((self.slot_in, "slot_in"), (self.slot_out, "slot_out")):
             _check(t, torch.int32, name)
             if t.dim() != 1 or t.shape[0] != num_reqs:

@@ -715,6 +715,9 @@ s2l_status rope_launch(const char* what, const s2l_kv_cache* cache, const s2l_ba
   if ((st = check_rope(rope, T)) != S2L_OK) return st;
   if (hq < 0 || hkv < 0) return fail(S2L_EINVAL, "head counts must be >= 0 (hq=%d hkv=%d)", hq, hkv);
   if (hq > 65535 || hkv > 65535) return fail(S2L_ENOTSUP, "%s supports at most 65535 heads of a kind", what);
+  // a launch holds 2^24 workgroups of 256: four rows and, where there are many, 16 heads each
+  if ((T + 3) / 4 * (((int64_t)hq + (cache ? 2 : 1) * (int64_t)hkv + 15) / 16) >= (1 << 24))
+    return fail(S2L_ENOTSUP, "%s: %lld rows of so many heads are more than one launch takes", what, (long long)T);
   if (hq > 0 && ((st = check_tensor("q", q, q_stride, hq, false, T)) != S2L_OK ||
                  (st = check_tensor("q_out", q_out, q_out_stride, hq, true, T)) != S2L_OK))
     return st;
@@ -899,6 +902,9 @@ s2l_status s2l_linear_attn(const s2l_linear_state* state, const s2l_batch* batch
   if (hq % hkv != 0) return fail(S2L_EINVAL, "num_heads %d is not a multiple of num_kv_heads %d", hq, hkv);
   if (batch->num_reqs > 65535 || hq > 65535)
     return fail(S2L_ENOTSUP, "linear_attn supports at most 65535 requests and heads");
+  // a launch holds 2^24 workgroups of 256, one a head and chunk that is not cut (chunks are where there are few)
+  if ((int64_t)batch->num_reqs * hq > (1 << 23))
+    return fail(S2L_ENOTSUP, "%d requests of %d heads are more than one launch takes", batch->num_reqs, hq);
   if (batch->num_reqs > 0) {
     if (!state->states || !state->log_decay || !state->slot_in || !state->slot_out)
       return fail(S2L_EINVAL, "states, log_decay, slot_in or slot_out is NULL");
@@ -911,6 +917,7 @@ s2l_status s2l_linear_attn(const s2l_linear_state* state, const s2l_batch* batch
       (st = check_tensor("v", v, v_stride, hkv, false, T)) != S2L_OK ||
       (st = check_tensor("out", out, out_stride, hq, true, T)) != S2L_OK)
     return st;
+  if (T > 0 && (out == q || out == k || out == v)) return fail(S2L_EINVAL, "out must not be q, k or v");
   int32_t cus;
   if ((st = query_cus(&cus)) != S2L_OK) return st;
   const s2l::LinearPlan plan = linear_plan(batch, hq, cus);

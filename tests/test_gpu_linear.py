@@ -100,6 +100,12 @@ def test_slots(C):
     t.run_and_check()
 
 
+@pytest.mark.parametrize("C", [[2, 5, 1], [70, 40, 9], [600, 900, 33]])
+def test_continuations_of_one_state(C):
+    """Requests that all go on from the same slot, one of them without keeping what it makes of it."""
+    Step(C, 4, 2, seed=30, slot_in=[1, 1, 1], slot_out=[0, -1, 2], num_slots=3).run_and_check()
+
+
 @pytest.mark.parametrize("C", [[5, 2], [300, 70]])
 def test_slots_out_of_range(C):
     """A bad slot to read makes NaN of the request; a bad slot to write stores nothing; others are as ever."""

@@ -76,6 +76,13 @@ def test_null_structs_and_lengths():
     assert _qk(_rope(), b)[0] == EINVAL and _append(_rope(), b, _cache())[0] == EINVAL
 
 
+def test_rows_beyond_one_launch():
+    b, keep = _batch([0, 0], [1 << 25, 1 << 25])
+    assert _qk(_rope(), b, hq=14, hkv=2, qs=2048, qos=2048)[0] == ENOTSUP
+    b, keep = _batch([0] * 8, [1 << 23] * 8, max_pages=1 << 20)
+    assert _append(_rope(), b, _cache())[0] == ENOTSUP
+
+
 def _linear(state, batch, q=FAKE, qs=1024, k=FAKE, ks=256, v=FAKE, vs=256, hkv=2, scale=0.1, out=FAKE, os_=1024, ws=FAKE, n=1 << 40):
     return _status("s2l_linear_attn", byref(state) if state else None, byref(batch) if batch else None, q, qs, k, ks, v, vs, hkv,
                    scale, out, os_, ws, n, None)
@@ -118,6 +125,17 @@ def test_linear_null_structs_and_sizes():
     assert _linear(_state(), b)[0] == EINVAL
 
 
+def test_linear_heads_beyond_one_launch_and_outputs_in_place():
+    b, keep = _batch([0] * 1025, [1] * 1025)
+    st, msg = _linear(_state(num_heads=8192), b, qs=1 << 20, os_=1 << 20)
+    assert st == ENOTSUP and msg
+    b, keep = _batch([0], [4])
+    other = FAKE + 4096
+    for kw in (dict(k=other, v=other), dict(q=other, v=other), dict(q=other, k=other)):
+        st, msg = _linear(_state(), b, **kw)
+        assert st == EINVAL and "out must not be" in msg
+
+
 def test_pair_axes():
     assert s2l.rope_pair_axes((2, 1, 1)) == [0, 0, 1, 2]
     assert s2l.rope_pair_axes((4, 2, 2), cyclic=True) == [0, 1, 2, 0, 1, 2, 0, 0]
@@ -151,6 +169,12 @@ def test_the_package_refuses_what_it_cannot_pass_on():
     for bad in (slots.long(), torch.zeros(2, dtype=torch.int32)):
         with pytest.raises(ValueError):
             s2l.LinearState(states, decay, bad, slots).c(1, states.device)
+    # attributes exchanged after the checks of the constructor
+    state, rope = s2l.LinearState(states, decay, slots, slots), s2l.Rope(inv)
+    state.states, rope.inv_freq = states[:, :4], inv.double()
+    for obj, n in ((state, 1), (rope, 4)):
+        with pytest.raises(ValueError):
+            obj.c(n, inv.device)
     with pytest.raises(ValueError):
         s2l.s2l_linear_attn(s2l.LinearState(states, decay, slots, slots), batch, q, k, k, 0.1, q, None, 0)
     with pytest.raises(ValueError):
