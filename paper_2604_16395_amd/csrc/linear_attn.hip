@@ -32,7 +32,7 @@
 // which read K and V a second time.  Bound by the memory: 32768 tokens of 32 heads, 1.08 GB, 380 us (130 for the
 // pieces' own states, 12 for the sums, 233 to 290 for the blocks; 362 with the loads and stores alone).  Short
 // chunks are bound by the blocks one after another and by the start of each launch (a unit's search 1 us, its states
-// and first tiles 3): 32 heads, 64 tokens 8.4 us, 256 18.1, 512 28 to 32 either way, 2048 in pieces 49.
+// and first tiles 3): 32 heads, 64 tokens 8.2 us, 256 17.3, 512 28 to 32 either way, 2048 in pieces 49.
 #include "launch.h"
 #include "s2l_device.h"
 
@@ -640,8 +640,8 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
 }
 
 // The blocked form of whole chunks with half of a head's columns a workgroup, 16 a wave.  Where there are few
-// workgroups, the blocks one after another are the time, and a wave has half as much to do in each: 1.62 us a block
-// instead of 1.94.  Where there are many, reading K and Q for half as many columns costs 1.25 times as much.
+// workgroups, the blocks one after another are the time, and a wave has half as much to do in each: 1.53 us a block
+// instead of 1.94 (1.62 with the operands read where they are used).  Where there are many, reading K and Q for half as many columns costs 1.25 times as much.
 // Other than above, products are 16 x 16 x 32 and state register (t, i) is key dim 16 t + 4 quarter + i of column
 // n: two of its quads are an operand's eight key dims, and Q's rows are read in the same halves.
 template <bool kDirect>
@@ -761,10 +761,15 @@ __global__ __launch_bounds__(256, 2) void linear_narrow_kernel(LinearLaunch a) {
       if (2 < blocks) load(2);
     }
   }
-  auto scores = [&](int stage, int parity) {
+  bf16x8 sk[4], sq[4];
+  auto read_scores = [&](int stage) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s) sk[s] = read_row(s_ring + ((stage + krow) ^ s << 6)), sq[s] = read_row(s_ring + ((stage + qrow) ^ s << 6));
+  };
+  auto scores = [&](int parity) {
     f32x4 sc{};
 #pragma unroll
-    for (int s = 0; s < 4; ++s) sc = mfma16(read_row(s_ring + ((stage + krow) ^ s << 6)), read_row(s_ring + ((stage + qrow) ^ s << 6)), sc);
+    for (int s = 0; s < 4; ++s) sc = mfma16(sk[s], sq[s], sc);
     float y[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] = query0 >= key0 + i ? sc[i] * within[i] : 0.f;
@@ -778,7 +783,8 @@ __global__ __launch_bounds__(256, 2) void linear_narrow_kernel(LinearLaunch a) {
   if (kDirect && blocks > 1) tile_barrier<kCopies>();
   else if (kDirect) tile_barrier<0>();
   else lds_barrier();
-  scores(0, 0);
+  read_scores(0);
+  scores(0);
 
   int behind = 0;      // tokens that S has yet to fade by: the state is l^behind S
   int at = 0;          // the block's stage
@@ -795,7 +801,16 @@ __global__ __launch_bounds__(256, 2) void linear_narrow_kernel(LinearLaunch a) {
       __asm__ volatile("" ::: "memory");   // the block's stores are younger than the copies
     }
     const int valid = min(kB, len - b * kB);
+    // all of the block's operands are read ahead of what waits for them
     const bf16x8 vc = read_columns(s_ring + at + vcol[0], s_ring + at + vcol[1]);
+    read_scores(next);
+    bf16x8 qh[4][2];
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        qh[s][u] = read_halves(s_ring + ((at + row8) ^ s << 6) + 16 * u * kRow, s_ring + ((at + row8) ^ (s << 6 | 32)) + 16 * u * kRow);
+    __builtin_amdgcn_sched_barrier(0);
     u32x4 vw = __builtin_bit_cast(u32x4, vc);
 
     // values of v that are not finite: as above
@@ -831,7 +846,11 @@ __global__ __launch_bounds__(256, 2) void linear_narrow_kernel(LinearLaunch a) {
     }
 
     // the next block's scores (of a block that there is not: of what lies there, and not used)
-    scores(next, (b + 1) & 1);
+    scores((b + 1) & 1);
+    bf16x8 kk[8];
+#pragma unroll
+    for (int t = 0; t < 8; ++t) kk[t] = read_columns(s_ring + ((at + kcol[0]) ^ t << 5), s_ring + ((at + kcol[1]) ^ t << 5));
+    __builtin_amdgcn_sched_barrier(0);
     float x[8];
     {
       const u32x4 w = __builtin_bit_cast(u32x4, vc);
@@ -841,7 +860,6 @@ __global__ __launch_bounds__(256, 2) void linear_narrow_kernel(LinearLaunch a) {
     const Terms<3> vx = split<3>(x);
 
     f32x4 o[2] = {};
-    const int row = at + row8;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       float z[8];
@@ -850,9 +868,8 @@ __global__ __launch_bounds__(256, 2) void linear_narrow_kernel(LinearLaunch a) {
       const Terms<2> sx = split<2>(z);
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const bf16x8 q = read_halves(s_ring + (row ^ s << 6) + 16 * u * kRow, s_ring + (row ^ (s << 6 | 32)) + 16 * u * kRow);
-        o[u] = mfma16(sx.t[1], q, o[u]);
-        o[u] = mfma16(sx.t[0], q, o[u]);
+        o[u] = mfma16(sx.t[1], qh[s][u], o[u]);
+        o[u] = mfma16(sx.t[0], qh[s][u], o[u]);
       }
     }
     if (fades) {
@@ -864,9 +881,8 @@ __global__ __launch_bounds__(256, 2) void linear_narrow_kernel(LinearLaunch a) {
     }
 #pragma unroll
     for (int t = 0; t < 8; ++t) {
-      const bf16x8 kk = read_columns(s_ring + ((at + kcol[0]) ^ t << 5), s_ring + ((at + kcol[1]) ^ t << 5));
 #pragma unroll
-      for (int i = 2; i >= 0; --i) S[t] = mfma16(kk, vx.t[i], S[t]);
+      for (int i = 2; i >= 0; --i) S[t] = mfma16(kk[t], vx.t[i], S[t]);
     }
     const float late = decay.power(behind);
     const bf16x8 vv = __builtin_bit_cast(bf16x8, vw);
