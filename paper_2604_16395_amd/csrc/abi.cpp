@@ -638,9 +638,9 @@ double linear_cost(const s2l_batch* b, int32_t hq, int32_t num_cus, int64_t piec
   return t;
 }
 
-// The same for whole requests with half of a head's columns a workgroup.  A block takes 1.53 us with a CU to itself
-// and 2.03 us with two workgroups on it; busy CUs take 1.35 us for each and 1.5 us for each unit's states, and units
-// of equal length come in rounds, of 1.5 us a block and 2.2 us.
+// The same for whole requests with half of a head's columns a workgroup.  A block takes 1.43 us with a CU to itself
+// and up to 2.09 us where the others keep two workgroups on every CU; busy CUs take 1.35 us for each and 1.5 us for
+// each unit's states, and units of equal length come in rounds, of 1.5 us a block and 2.2 us.
 double linear_narrow_cost(const s2l_batch* b, int32_t hq, int32_t num_cus) {
   double units = 0, blocks = 0, longest = 0;
   for (int32_t r = 0; r < b->num_reqs; ++r) {
@@ -652,16 +652,16 @@ double linear_narrow_cost(const s2l_batch* b, int32_t hq, int32_t num_cus) {
     longest = std::max(longest, n);
   }
   const double per_cu = 2.0 * hq / num_cus, rounds = std::ceil(units * per_cu - 1e-9), mean = blocks / units;
-  return 5.1 + std::max({longest * (1.53 + 0.25 * std::min(2.0, units * per_cu)), (1.35 * blocks + 1.5 * units) * per_cu,
+  return 5.2 + std::max({longest * (1.43 + 0.33 * std::min(2.0, blocks * per_cu / longest)), (1.35 * blocks + 1.5 * units) * per_cu,
                          rounds * (1.5 * mean * mean / longest + 2.2)});
 }
 
 // How linear attention cuts the batch: requests stay whole unless shorter pieces are estimated to be faster, and a
 // head of a whole request gets two workgroups where that is estimated to be faster still: its blocks' chain is
 // shorter, but every block costs 1.25 times as much.  32 heads, one workgroup a head and two: a chunk of 64 tokens
-// 10.1 us and 8.2, of 256 21.9 and 17.2; 8 requests of 389 to 1024 tokens 79 and 67, 16 of 512 78 and 99.
+// 10.1 us and 8.1, of 256 21.9 and 17.0; 8 requests of 389 to 1024 tokens 79 and 66, 16 of 512 78 and 99.
 // Against the fastest of the measured piece lengths of each of those batches the choice takes 1.01 of the time in the
-// geometric mean and 1.11 at most (examples, 32 heads: 2048 tokens whole 131 us, in pieces of 256 46 us; 16 requests
+// geometric mean and 1.08 at most (examples, 32 heads: 2048 tokens whole 131 us, in pieces of 256 46 us; 16 requests
 // of 1024 tokens whole 139 us, in pieces of 512 241).
 s2l::LinearPlan linear_plan(const s2l_batch* b, int32_t hq, int32_t num_cus) {
   s2l::LinearPlan p = {};

@@ -32,7 +32,7 @@
 // which read K and V a second time.  Bound by the memory: 32768 tokens of 32 heads, 1.08 GB, 380 us (130 for the
 // pieces' own states, 12 for the sums, 233 to 290 for the blocks; 362 with the loads and stores alone).  Short
 // chunks are bound by the blocks one after another and by the start of each launch (a unit's search 1 us, its states
-// and first tiles 3): 32 heads, 64 tokens 8.2 us, 256 17.3, 512 28 to 32 either way, 2048 in pieces 49.
+// and first tiles 3): 32 heads, 64 tokens 8.1 us, 256 17.0, 512 28 to 30 either way, 2048 in pieces 49.
 #include "launch.h"
 #include "s2l_device.h"
 
@@ -640,8 +640,9 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
 }
 
 // The blocked form of whole chunks with half of a head's columns a workgroup, 16 a wave.  Where there are few
-// workgroups, the blocks one after another are the time, and a wave has half as much to do in each: 1.53 us a block
-// instead of 1.94 (1.62 with the operands read where they are used).  Where there are many, reading K and Q for half as many columns costs 1.25 times as much.
+// workgroups, the blocks one after another are the time, and a wave has half as much to do in each: 1.43 us a block
+// instead of 1.94 (1.62 with the operands read where they are used).  Where there are many, reading K and Q for half
+// as many columns costs 1.25 times as much.
 // Other than above, products are 16 x 16 x 32 and state register (t, i) is key dim 16 t + 4 quarter + i of column
 // n: two of its quads are an operand's eight key dims, and Q's rows are read in the same halves.
 template <bool kDirect>
@@ -731,7 +732,12 @@ __global__ __launch_bounds__(256, 2) void linear_narrow_kernel(LinearLaunch a) {
   // Scores: dims 32 s + 8 quarter .. + 7 of a row, ^ s << 6.  Against the state: dims 32 s + 4 quarter .. + 3, and 16
   // on (^ 32), of row n, ^ s << 6.  Columns: lane n of a quarter addresses columns 4 (n % 4) .. + 3 of row
   // 8 quarter + n / 4, and of the fourth on; key dims 16 t .. + 15: ^ t << 5.
-  const int row8 = 2 * kTile + n * kRow + (((quarter >> 1) ^ perm(n)) << 4) + 8 * (quarter & 1);
+  int row8[2];   // of query n, of query n + 16
+  row8[0] = 2 * kTile + n * kRow + (((quarter >> 1) ^ perm(n)) << 4) + 8 * (quarter & 1);
+  row8[1] = row8[0] + 16 * kRow;
+  // Hidden from the compiler: two 8-byte reads a fixed distance apart become one instruction, which takes 16 lanes at a
+  // time, whose reads lie on half of the banks (17% of the cycles were conflicts; now 8%).
+  __asm__("" : "+v"(row8[1]));
   int kcol[2], vcol[2];
 #pragma unroll
   for (int y = 0; y < 2; ++y) {
@@ -809,7 +815,7 @@ __global__ __launch_bounds__(256, 2) void linear_narrow_kernel(LinearLaunch a) {
     for (int s = 0; s < 4; ++s)
 #pragma unroll
       for (int u = 0; u < 2; ++u)
-        qh[s][u] = read_halves(s_ring + ((at + row8) ^ s << 6) + 16 * u * kRow, s_ring + ((at + row8) ^ (s << 6 | 32)) + 16 * u * kRow);
+        qh[s][u] = read_halves(s_ring + ((at + row8[u]) ^ s << 6), s_ring + ((at + row8[u]) ^ (s << 6 | 32)));
     __builtin_amdgcn_sched_barrier(0);
     u32x4 vw = __builtin_bit_cast(u32x4, vc);
 
