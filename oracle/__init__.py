@@ -21,6 +21,8 @@ Modules:
 * :mod:`oracle.paged_kv`  - page/slot addressing, page append (scatter) and gather.
 * :mod:`oracle.attention` - chunk attention by definition (per-row loops and a blocked
   two-pass form), brute-force full causal attention, and the log-sum-exp merge.
+* :mod:`oracle.rotary` - rotary positions by float64 angles, any pairing and axes.
+* :mod:`oracle.linear_attn` - linear attention with a decay, token after token.
 
 Every function works in float64 (bf16 and fp8 values convert to float64 exactly).
 Parity status of each function is recorded in its docstring; all are pinned by the
