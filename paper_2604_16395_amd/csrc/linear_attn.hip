@@ -6,7 +6,9 @@
 // (request, head) state.  Thread (kg, vq) keeps rows 4 kg .. + 3 and columns 4 vq .. + 3 of them in
 // registers over the request's tokens, so the state is read and written once; a row's part of q S is
 // summed over the eight row groups of a wave by lane swaps and over the four waves through LDS.  Bound by the
-// states: 64 requests of a token, 32 heads, 270 MB, 51.6 us, 5.2 TB/s; one request 3.9 us, by its chain of loads.
+// states: 64 requests of a token, 32 heads, 270 MB, 48.9 us, 5.5 TB/s; one request 3.7 us, by its chain of loads.
+// The launch has workgroups for every request, and those of long ones leave: a search for the short ones took
+// 51.5 us there, 632 instead of 390 for 2048 requests of 8 heads; 64 chunks of 100 tokens and one token cost 2% more.
 //
 // Longer chunks take the blocked form, 32 tokens at a time: with n of them valid (zero rows behind),
 //   out_i = scale (sum_{j <= i} l^(i-j) (q_i . k_j) v_j + l^(i+1) q_i S),
@@ -80,14 +82,12 @@ __device__ inline int32_t wave_scan(int32_t x) {
   return x;
 }
 
-// The idx-th of the batch's units, 64 requests at a time, all that is known of them in one round of loads.  Units
-// are the short requests (kShort), or the pieces of the others: of all, or (kCutPieces) of those that are cut.
-// Pieces come longest first (by eighths of the longest): the longest then have a CU of their own while there
-// are fewer than CUs, and do not begin last (11 requests of 17 to 2048 tokens, 32 heads: 199 us in the batch's
-// order, 141 in this).
-enum Units { kShort, kPieces, kCutPieces };
-template <Units kUnits>
-__device__ inline Piece find_unit(const LinearLaunch& a, int32_t idx) {
+// The idx-th of the batch's pieces of long requests (of all of them, or kCut: of those that are cut), 64 requests at a
+// time, all that is known of them in one round of loads.  Pieces come longest first (by eighths of the longest): the
+// longest then have a CU of their own while there are fewer than CUs, and do not begin last (11 requests of 17 to
+// 2048 tokens, 32 heads: 199 us in the batch's order, 141 in this).
+template <bool kCut>
+__device__ inline Piece find_piece(const LinearLaunch& a, int32_t idx) {
   const int lane = threadIdx.x & 63;
   int32_t ws = 0;
   for (int32_t r0 = 0; r0 < a.num_reqs; r0 += 64) {
@@ -97,12 +97,9 @@ __device__ inline Piece find_unit(const LinearLaunch& a, int32_t idx) {
     const int32_t len = lane < count ? l : -1;
     const int32_t pieces = len > kLinearShortTokens ? (len + a.piece_tokens - 1) / a.piece_tokens : 0;
     const int32_t cut = pieces > 1 ? pieces : 0, entries = cut ? cut + 1 : 0;   // workspace entries
-    const int32_t mine = kUnits == kShort ? (len >= 0 && len <= kLinearShortTokens) : kUnits == kPieces ? pieces : cut;
+    const int32_t mine = kCut ? cut : pieces;
     int32_t before = 0, ws_before = 0;   // units that come before this lane's request's, and entries
-    if (a.num_reqs == 1) {
-    } else if constexpr (kUnits == kShort) {
-      before = wave_scan(mine) - mine;
-    } else {
+    if (a.num_reqs > 1) {
       ws_before = wave_scan(entries) - entries;
       const int32_t size = len < a.piece_tokens ? len : a.piece_tokens;
       const int32_t eighth = min(7, (int32_t)((float)size * (8.f / (float)a.unit_tokens)));
@@ -139,23 +136,28 @@ constexpr int kSliceCols = 32;       // columns of a recurrent workgroup
 
 __device__ inline f32x4 unpack4(const u32x2& x) { return f32x4{bf16lo(x[0]), bf16hi(x[0]), bf16lo(x[1]), bf16hi(x[1])}; }
 
-__global__ __launch_bounds__(256) void linear_recurrent_kernel(LinearLaunch a) {
+// The four slices of a state follow one another on one XCD (51.1 us without), five workgroups at a time on a CU: more of
+// them spread over more pages of the memory (seven 50.4 us, 2048 requests of 8 heads 391 and with four 364), and fewer
+// leave a rest (64 requests of 8 heads 13.2 us, with four 14.3).
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(5, 5))) void linear_recurrent_kernel(LinearLaunch a) {
   __shared__ float s_part[kLinearShortTokens][4][kSliceCols];
-  const Piece p = find_unit<kShort>(a, blockIdx.z);
-  if (p.req < 0) return;
-  const int h = blockIdx.y, col0 = (int)blockIdx.x * kSliceCols;
-  const int C = p.len, si = p.slot_in, so = p.slot_out;
-  const int64_t row0 = p.row;
+  const int r = blockIdx.y, h = (int)(blockIdx.x / 32) * 8 + (int)(blockIdx.x % 8), col0 = (int)(blockIdx.x / 8 % 4) * kSliceCols;
+  if (h >= a.hq) return;
+  const int C = a.chunk_lens[r], si = a.slot_in[r], so = a.slot_out[r];
+  const int64_t row0 = a.cu_chunk[r];
+  if (C > kLinearShortTokens) return;
   const int g = h / (a.hq / a.hkv);
   const int vq = threadIdx.x & 7, kg = threadIdx.x >> 3, wave = threadIdx.x >> 6;
   const int64_t at = (int64_t)h * kState + (4 * kg) * 128 + col0 + 4 * vq;   // within a slot
   const int64_t slot = (int64_t)a.hq * kState;
 
   f32x4 s[4];
+  if (si >= 0 && si < a.num_slots) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    if (si >= 0 && si < a.num_slots) s[j] = *reinterpret_cast<const f32x4*>(a.states + si * slot + at + j * 128);
-    else s[j] = f32x4{} + (si == -1 ? 0.f : __builtin_nanf(""));
+    for (int j = 0; j < 4; ++j) s[j] = *reinterpret_cast<const f32x4*>(a.states + si * slot + at + j * 128);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s[j] = f32x4{} + (si == -1 ? 0.f : __builtin_nanf(""));
   }
   // four tokens' rows are loaded while the four before are worked on
   constexpr int kAhead = 4;
@@ -318,7 +320,7 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
   if (unit >= a.num_units * a.hkv) return;
   const int g = unit % a.hkv, h = g * group + h0;
   const float log_decay = a.log_decay[h];
-  Piece p = find_unit<kOutputs ? kPieces : kCutPieces>(a, unit / a.hkv);
+  Piece p = find_piece<!kOutputs>(a, unit / a.hkv);
   if (p.req < 0) return;
   p.seg = __builtin_amdgcn_readfirstlane(p.seg);
   p.len = __builtin_amdgcn_readfirstlane(p.len);
@@ -660,7 +662,7 @@ __global__ __launch_bounds__(256, 2) void linear_narrow_kernel(LinearLaunch a) {
   if (unit >= a.num_units * a.hkv) return;
   const int g = unit % a.hkv, h = g * group + (h0 >> 1), col0 = 64 * (h0 & 1) + 16 * wave;
   const float log_decay = a.log_decay[h];
-  Piece p = find_unit<kPieces>(a, unit / a.hkv);
+  Piece p = find_piece<false>(a, unit / a.hkv);
   if (p.req < 0) return;
   const int len = __builtin_amdgcn_readfirstlane(p.len), blocks = (len + kB - 1) / kB;
   const int64_t row0 = __builtin_amdgcn_readfirstlane(p.row);
@@ -1019,7 +1021,7 @@ hipError_t launch_linear_attn(const LinearLaunch& launch, const LinearPlan& plan
     else linear_block_kernel<true, false><<<blocks(a.num_units), 256, 0, stream>>>(a);
   }
   if (plan.short_reqs > 0)
-    linear_recurrent_kernel<<<dim3(128 / kSliceCols, a.hq, plan.short_reqs), 256, 0, stream>>>(a);
+    linear_recurrent_kernel<<<dim3(32 * ((a.hq + 7) / 8), a.num_reqs), 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
