@@ -596,117 +596,6 @@ s2l_status check_rope(const s2l_rope* rope, int64_t T) {
   return S2L_OK;
 }
 
-// Estimated time in us of linear attention's blocked form where requests are cut into pieces of
-// piece_blocks blocks of 32 tokens.  A workgroup takes the blocks of a (piece, head) one after another, so the longest piece's
-// chain is one bound; blocks and states over all CUs are the other, with a part of the longest piece
-// where a CU gets more than one.  Cut requests' own states take a launch of the same kind, and the sums between them
-// read and write every state once.  Constants: a fit (0.07 rms of the logarithm) to 600 measured layers (51 batches of 1
-// to 96 requests of 17 to 32768 tokens, 8 to 64 heads, each in up to 16 piece lengths); single ones make up for one
-// another and are no times of parts.
-double linear_cost(const s2l_batch* b, int32_t hq, int32_t num_cus, int64_t piece_blocks) {
-  double units = 0, cut = 0, cut_units = 0, blocks = 0, cut_blocks = 0, states = 0, longest = 0;
-  for (int32_t r = 0; r < b->num_reqs; ++r) {
-    const int32_t c = b->chunk_lens_host[r];
-    if (c <= s2l::kLinearShortTokens) continue;
-    const int64_t n = s2l::ceil_div64(c, s2l::kLinearBlockTokens), k = s2l::ceil_div64(n, piece_blocks);
-    units += (double)k;
-    blocks += (double)n;
-    longest = std::max(longest, (double)std::min(n, piece_blocks));
-    if (k == 1) {
-      states += 2;
-    } else {
-      states += (double)k;
-      cut += 1;
-      cut_units += (double)k;
-      cut_blocks += (double)n;
-    }
-  }
-  const double per_cu = (double)hq / num_cus;   // of units and blocks, each once a head
-  // units of equal length come in rounds: a CU takes two of them in less than twice one's time
-  const auto rounds = [&](double n, double n_blocks, double one, double two) {
-    const double m = std::ceil(n * per_cu - 1e-9), odd = m - 2 * std::floor(m / 2);
-    return n_blocks / (n * longest) * (std::floor(m / 2) * two + odd * one);
-  };
-  const double chain = longest * (1.94 + 0.05 * std::min(1.0, units * per_cu));
-  const double uneven = 0.05 * std::min(1.0, std::max(0.0, units * per_cu - 1));
-  double t = 6.7 + std::max({chain, (2.16 * blocks + 2.16 * states) * per_cu + uneven * longest * 1.99,
-                             rounds(units, blocks, longest * 1.99, 2 * (2.16 * longest + 2.16 * states / units))});
-  if (cut_units > 0)
-    t += 6.2 + std::max({longest * 0.67, (0.2 * cut_blocks + 2.16 * cut_units) * per_cu,
-                         rounds(cut_units, cut_blocks, longest * 0.67, 2 * (0.2 * longest + 2.16))}) +
-         8.9 * (cut_units + cut) * per_cu;
-  return t;
-}
-
-// The same for whole requests with half of a head's columns a workgroup.  A block takes 1.43 us with a CU to itself
-// and up to 2.09 us where the others keep two workgroups on every CU; busy CUs take 1.35 us for each and 1.5 us for
-// each unit's states, and units of equal length come in rounds, of 1.5 us a block and 2.2 us.
-double linear_narrow_cost(const s2l_batch* b, int32_t hq, int32_t num_cus) {
-  double units = 0, blocks = 0, longest = 0;
-  for (int32_t r = 0; r < b->num_reqs; ++r) {
-    const int32_t c = b->chunk_lens_host[r];
-    if (c <= s2l::kLinearShortTokens) continue;
-    const double n = (double)s2l::ceil_div64(c, s2l::kLinearBlockTokens);
-    units += 1;
-    blocks += n;
-    longest = std::max(longest, n);
-  }
-  const double per_cu = 2.0 * hq / num_cus, rounds = std::ceil(units * per_cu - 1e-9), mean = blocks / units;
-  return 5.2 + std::max({longest * (1.43 + 0.33 * std::min(2.0, blocks * per_cu / longest)), (1.35 * blocks + 1.5 * units) * per_cu,
-                         rounds * (1.5 * mean * mean / longest + 2.2)});
-}
-
-// How linear attention cuts the batch: requests stay whole unless shorter pieces are estimated to be faster, and a
-// head of a whole request gets two workgroups where that is estimated to be faster still: its blocks' chain is
-// shorter, but every block costs 1.25 times as much.  32 heads, one workgroup a head and two: a chunk of 64 tokens
-// 10.1 us and 8.1, of 256 21.9 and 17.0; 8 requests of 389 to 1024 tokens 79 and 66, 16 of 512 78 and 99.
-// Against the fastest of the measured piece lengths of each of those batches the choice takes 1.01 of the time in the
-// geometric mean and 1.08 at most (examples, 32 heads: 2048 tokens whole 131 us, in pieces of 256 46 us; 16 requests
-// of 1024 tokens whole 139 us, in pieces of 512 241).
-s2l::LinearPlan linear_plan(const s2l_batch* b, int32_t hq, int32_t num_cus) {
-  s2l::LinearPlan p = {};
-  int64_t longest = 0, total = 0, units = 0;
-  for (int32_t r = 0; r < b->num_reqs; ++r) {
-    const int32_t c = b->chunk_lens_host[r];
-    if (c <= s2l::kLinearShortTokens) continue;
-    ++units;
-    longest = std::max(longest, s2l::ceil_div64(c, s2l::kLinearBlockTokens));
-    total += s2l::ceil_div64(c, s2l::kLinearBlockTokens);
-  }
-  int64_t blocks = std::max<int64_t>(longest, 1);
-  double best = linear_cost(b, hq, num_cus, blocks);
-  // more pieces only add work: of no use where the CUs have enough of it without
-  if ((double)total * hq < 2 * (double)longest * num_cus) {
-    for (const int64_t n : {2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {
-      const int64_t k = s2l::ceil_div64(longest, n);
-      if (k < 2 && n > 2) break;
-      const double cost = linear_cost(b, hq, num_cus, k);
-      if (cost < best) best = cost, blocks = k;
-    }
-  }
-  // with more units the CUs are busy either way; the other estimate is some 5 % low for uneven chunks
-  if (units > 0 && (double)units * hq <= 16.0 * num_cus && linear_narrow_cost(b, hq, num_cus) < 1.05 * best) {
-    p.narrow = true;
-    blocks = std::max<int64_t>(longest, 1);
-  }
-  p.piece_tokens = (int32_t)(blocks * s2l::kLinearBlockTokens);
-  for (int32_t r = 0; r < b->num_reqs; ++r) {
-    const int32_t c = b->chunk_lens_host[r];
-    if (c <= s2l::kLinearShortTokens) {
-      ++p.short_reqs;
-      continue;
-    }
-    const int32_t n = (int32_t)s2l::ceil_div64(c, p.piece_tokens);
-    p.pieces += n;
-    p.unit_tokens = std::max(p.unit_tokens, std::min(c, p.piece_tokens));
-    if (n > 1) ++p.cut_reqs, p.ws_states += n + 1;
-  }
-  return p;
-}
-size_t linear_bytes(const s2l::LinearPlan& p, int32_t hq) {
-  return (size_t)p.ws_states * hq * s2l::kHeadDim * s2l::kHeadDim * sizeof(float);
-}
-
 s2l_status rope_launch(const char* what, const s2l_kv_cache* cache, const s2l_batch* batch, const s2l_rope* rope,
                        int64_t T, const void* q, int64_t q_stride, int32_t hq, void* q_out, int64_t q_out_stride,
                        const void* k, int64_t k_stride, int32_t hkv, void* k_out, int64_t k_out_stride, const void* v,
@@ -885,7 +774,7 @@ s2l_status s2l_linear_attn_workspace_bytes(const s2l_batch* batch, int32_t num_q
   if (num_q_heads <= 0) return fail(S2L_EINVAL, "num_q_heads must be > 0");
   int32_t cus;
   if ((st = query_cus(&cus)) != S2L_OK) return st;
-  *bytes_out = linear_bytes(linear_plan(batch, num_q_heads, cus), num_q_heads);
+  *bytes_out = s2l::linear_bytes(s2l::linear_plan(batch, num_q_heads, cus), num_q_heads);
   return ok();
 }
 
@@ -920,8 +809,8 @@ s2l_status s2l_linear_attn(const s2l_linear_state* state, const s2l_batch* batch
   if (T > 0 && (out == q || out == k || out == v)) return fail(S2L_EINVAL, "out must not be q, k or v");
   int32_t cus;
   if ((st = query_cus(&cus)) != S2L_OK) return st;
-  const s2l::LinearPlan plan = linear_plan(batch, hq, cus);
-  if (const size_t need = linear_bytes(plan, hq); need > 0) {
+  const s2l::LinearPlan plan = s2l::linear_plan(batch, hq, cus);
+  if (const size_t need = s2l::linear_bytes(plan, hq); need > 0) {
     if (!workspace) return fail(S2L_EWORKSPACE, "workspace is NULL");
     if (ws_bytes < need) return fail(S2L_EWORKSPACE, "workspace %zu bytes < %zu needed", ws_bytes, need);
     if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return fail(S2L_EINVAL, "workspace must be aligned to 16 bytes");

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "linear_plan.h"
 #include "plan_rules.h"
 
 namespace s2l {
@@ -122,18 +123,6 @@ struct LinearLaunch {        // linear attention (linear_attn.hip)
   float scale;
   float* ws;                 // [ws_states][hq][128][128]: states around the pieces of cut requests
   int32_t piece_tokens, unit_tokens, ws_states, num_units;   // from the plan, per launch
-};
-// Requests of at most kLinearShortTokens new tokens are advanced token by token, the others in blocks.  32 heads, token
-// by token against in blocks: 64 requests of 4 tokens 53.0 against 62.7 us, of 5 63.5 against 63.6, of 8 69.3 against
-// 67.2; 8 requests of 5 11.0 against 11.2, of 8 13.0 against 11.2; one request 5.4 against 8.3, of 12 7.9 against 8.4.
-constexpr int32_t kLinearShortTokens = 5, kLinearBlockTokens = 32;
-struct LinearPlan {          // how the batch is cut, from the host lengths
-  int32_t piece_tokens;      // longer requests are cut into pieces of so many tokens (a multiple of a block)
-  int32_t unit_tokens;       // the longest piece's
-  int32_t pieces;            // of all requests that are not short
-  int32_t cut_reqs, ws_states;   // requests of more than one piece; one state before, between and after them
-  int32_t short_reqs;
-  bool narrow;               // no request is cut, and a workgroup takes half of a head's columns
 };
 hipError_t launch_linear_attn(const LinearLaunch& a, const LinearPlan& plan, hipStream_t stream);
 
