@@ -58,6 +58,12 @@ __device__ inline void unpack8(const u32x4& x, float* y) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) y[2 * i] = bf16lo(x[i]), y[2 * i + 1] = bf16hi(x[i]);
 }
+// (a, b) turned.  Products and sums are written out as the fused operations that they are: left to the compiler, the forms
+// of the kernel could round differently, and pages must be those of the separate calls bit for bit.
+__device__ inline void turn(float a, float b, float cs, float sn, float* ya, float* yb) {
+  *ya = __builtin_fmaf(a, cs, -(b * sn));
+  *yb = __builtin_fmaf(b, cs, a * sn);
+}
 // As the append without rotation: code = e4m3(fp32(x) * fp32(1 / scale)).
 __device__ inline u32x2 encode8(const u32x4& x, float inv) {
   return u32x2{f32x4_to_fp8x4(bf16lo(x[0]) * inv, bf16hi(x[0]) * inv, bf16lo(x[1]) * inv, bf16hi(x[1]) * inv),
@@ -109,10 +115,10 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a) {
     for (int i = 0; i < 8; ++i) {
       const uint32_t axis = axes >> (2 * i) & 3;
       const double p = axis & 2 ? (axis & 1 ? pos[3] : pos[2]) : (axis & 1 ? pos[1] : pos[0]);
-      const double t = p * ((double)(i < 4 ? f0[i & 3] : f1[i & 3]) * 0.15915494309189535);
-      const float turn = (float)(t - __builtin_rint(t));
-      cs[i] = a.scale * __builtin_amdgcn_cosf(turn);
-      sn[i] = a.scale * __builtin_amdgcn_sinf(turn);
+      const double f = (double)(i < 4 ? f0[i & 3] : f1[i & 3]) * 0.15915494309189535;
+      const float angle = (float)__builtin_fma(p, f, -__builtin_rint(p * f));
+      cs[i] = a.scale * __builtin_amdgcn_cosf(angle);
+      sn[i] = a.scale * __builtin_amdgcn_sinf(angle);
     }
   }
 
@@ -129,27 +135,15 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a) {
       float x[8], y[8];
       unpack8(xa[j], x);
       unpack8(xb[j], y);
-      if constexpr (kAdjacent) {
-        float u[8], w[8];
+      float u[8], w[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          u[2 * i] = x[2 * i] * cs[i] - x[2 * i + 1] * sn[i];
-          u[2 * i + 1] = x[2 * i + 1] * cs[i] + x[2 * i] * sn[i];
-          w[2 * i] = y[2 * i] * cs[4 + i] - y[2 * i + 1] * sn[4 + i];
-          w[2 * i + 1] = y[2 * i + 1] * cs[4 + i] + y[2 * i] * sn[4 + i];
-        }
-        xa[j] = pack8(u);
-        xb[j] = pack8(w);
-      } else {
-        float u[8], w[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          u[i] = x[i] * cs[i] - y[i] * sn[i];
-          w[i] = y[i] * cs[i] + x[i] * sn[i];
-        }
-        xa[j] = pack8(u);
-        xb[j] = pack8(w);
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (!kAdjacent) turn(x[i], y[i], cs[i], sn[i], &u[i], &w[i]);
+        else if (i < 4) turn(x[2 * i], x[2 * i + 1], cs[i], sn[i], &u[2 * i], &u[2 * i + 1]);
+        else turn(y[2 * i - 8], y[2 * i - 7], cs[i], sn[i], &w[2 * i - 8], &w[2 * i - 7]);
       }
+      xa[j] = pack8(u);
+      xb[j] = pack8(w);
     }
     if (h < a.hq) {
       uint16_t* dst = a.q_out + row * a.q_out_stride + h * 128;
