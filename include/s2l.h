@@ -262,7 +262,8 @@ typedef struct s2l_linear_state {
 s2l_status s2l_linear_attn_workspace_bytes(const s2l_batch* batch, int32_t num_q_heads, size_t* bytes_out);
 
 /*
- * The chunks of a varlen batch (of any mix of lengths; prefix lengths and block tables are not read).
+ * The chunks of a varlen batch (of any mix of lengths; the device prefix lengths and block tables are not read
+ * and may be NULL).
  *   q, k, v, out: device bf16 rows with strides as in s2l_rope_qk (Hq, Hkv, Hkv and Hq heads of 128);
  *                 out overlaps nothing that is read.  Rows from T on are not touched.
  *   workspace   : device, ws_bytes >= s2l_linear_attn_workspace_bytes(...); NULL when that is 0.

@@ -559,11 +559,12 @@ s2l_status attn_launch(const s2l_kv_cache* cache, const s2l_batch* batch, const 
   return ok();
 }
 
-// The batch of a call that rows alone matter to (no pages): lengths, and the device arrays that find a row.
-s2l_status check_rows(const s2l_batch* b, int64_t* total_tokens) {
+// The batch of a call that rows alone matter to (no pages): lengths, and the device arrays that find a row, with the prefix
+// lengths where rows have positions.
+s2l_status check_rows(const s2l_batch* b, bool positions, int64_t* total_tokens) {
   s2l_status st = check_batch(b, false, total_tokens);
   if (st != S2L_OK) return st;
-  if (b->num_reqs > 0 && (!b->prefix_lens || !b->chunk_lens || !b->cu_chunk))
+  if (b->num_reqs > 0 && ((positions && !b->prefix_lens) || !b->chunk_lens || !b->cu_chunk))
     return fail(S2L_EINVAL, "a device batch array is NULL");
   return S2L_OK;
 }
@@ -750,7 +751,7 @@ s2l_status s2l_rope_qk(const s2l_batch* batch, const s2l_rope* rope, const void*
                        int32_t num_kv_heads, void* k_out, int64_t k_out_stride, void* stream) {
   s2l_status st;
   int64_t T = 0;
-  if ((st = check_rows(batch, &T)) != S2L_OK) return st;
+  if ((st = check_rows(batch, true, &T)) != S2L_OK) return st;
   return rope_launch("rope_qk", nullptr, batch, rope, T, q, q_stride, num_q_heads, q_out, q_out_stride, k, k_stride,
                      num_kv_heads, k_out, k_out_stride, nullptr, 0, stream);
 }
@@ -785,7 +786,7 @@ s2l_status s2l_linear_attn(const s2l_linear_state* state, const s2l_batch* batch
   s2l_status st;
   int64_t T = 0;
   if (!state) return fail(S2L_EINVAL, "state is NULL");
-  if ((st = check_rows(batch, &T)) != S2L_OK) return st;
+  if ((st = check_rows(batch, false, &T)) != S2L_OK) return st;
   const int32_t hq = state->num_heads, hkv = num_kv_heads;
   if (hq <= 0 || hkv <= 0) return fail(S2L_EINVAL, "head counts must be > 0 (hq=%d hkv=%d)", hq, hkv);
   if (hq % hkv != 0) return fail(S2L_EINVAL, "num_heads %d is not a multiple of num_kv_heads %d", hq, hkv);

@@ -1,0 +1,31 @@
+"""Calls of the rotation, the rotating append and linear attention without a GPU: what is asked of arguments that a call
+does not read, and of those on other devices."""
+import pytest
+
+from paper_2604_16395_amd import _lib
+from tests.test_abi_cpu import _batch
+from tests.test_rope_linear_abi_cpu import _linear, _qk, _rope, _state
+
+
+@pytest.mark.parametrize("name", ["prefix_lens", "block_tables"])
+def test_linear_attention_asks_for_no_array_that_it_does_not_read(name):
+    """The batch is taken: what is refused next is the scale."""
+    b, keep = _batch([3], [4])
+    setattr(b, name, None)
+    st, msg = _linear(_state(), b, scale=float("inf"))
+    assert st == _lib.S2L_EINVAL and msg == "scale must be finite"
+
+
+@pytest.mark.parametrize("name", ["chunk_lens", "cu_chunk", "prefix_lens_host", "chunk_lens_host"])
+def test_linear_attention_asks_for_the_arrays_that_it_reads(name):
+    b, keep = _batch([3], [4])
+    setattr(b, name, None)
+    st, msg = _linear(_state(), b)
+    assert st == _lib.S2L_EINVAL and "NULL" in msg
+
+
+def test_the_rotation_asks_for_prefix_lengths():
+    b, keep = _batch([3], [4])
+    b.prefix_lens = None
+    st, msg = _qk(_rope(), b)
+    assert st == _lib.S2L_EINVAL and "NULL" in msg
