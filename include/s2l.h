@@ -256,7 +256,8 @@ typedef struct s2l_linear_state {
 
 /*
  * Workspace bytes that s2l_linear_attn needs for this batch (states at the boundaries of the pieces
- * that long chunks are cut into; 0 when none is).  A host computation from the host length copies.
+ * that long chunks are cut into; 0 when none is).  A host computation from the host length copies and the
+ * CU count of the current device, which has to be the call's.
  * Errors: EINVAL (nulls, negative lengths, head count), EHIP (the CU count query).
  */
 s2l_status s2l_linear_attn_workspace_bytes(const s2l_batch* batch, int32_t num_q_heads, size_t* bytes_out);

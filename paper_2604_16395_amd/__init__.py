@@ -22,6 +22,7 @@ attention keeps a state a request instead of pages (``LinearState``)::
     ws = torch.empty(s2l_linear_attn_workspace_bytes(batch, Hq), dtype=torch.uint8, device="cuda")
     s2l_linear_attn(state, batch, q, k, v, 128 ** -0.5, out, ws)
 """
+import contextlib
 import ctypes
 
 import numpy as np
@@ -325,9 +326,12 @@ def s2l_rope_kv_append(cache, batch, rope, q, q_out, k, v, stream=None):
 
 
 def s2l_linear_attn_workspace_bytes(batch, num_q_heads):
+    """Workspace bytes of the batch's s2l_linear_attn, which cuts chunks by the CUs of the batch's device."""
     bc = batch.c()
     n = ctypes.c_size_t(0)
-    _lib.call("s2l_linear_attn_workspace_bytes", ctypes.byref(bc), num_q_heads, ctypes.byref(n))
+    device = batch.chunk_lens.device
+    with torch.cuda.device(device) if device.type == "cuda" else contextlib.nullcontext():
+        _lib.call("s2l_linear_attn_workspace_bytes", ctypes.byref(bc), num_q_heads, ctypes.byref(n))
     return n.value
 
 

@@ -1,7 +1,12 @@
 """Calls of the rotation, the rotating append and linear attention without a GPU: what is asked of arguments that a call
 does not read, and of those on other devices."""
-import pytest
+import contextlib
+import types
 
+import pytest
+import torch
+
+import paper_2604_16395_amd as s2l
 from paper_2604_16395_amd import _lib
 from tests.test_abi_cpu import _batch
 from tests.test_rope_linear_abi_cpu import _linear, _qk, _rope, _state
@@ -29,3 +34,22 @@ def test_the_rotation_asks_for_prefix_lengths():
     b.prefix_lens = None
     st, msg = _qk(_rope(), b)
     assert st == _lib.S2L_EINVAL and "NULL" in msg
+
+
+@pytest.mark.parametrize("device,current", [("cuda:1", ["cuda:1"]), ("cuda:0", ["cuda:0"]), ("cpu", [])])
+def test_workspaces_are_sized_on_the_batch_s_device(monkeypatch, device, current):
+    """As the call itself runs there: another device current may have another number of CUs."""
+    seen, now = [], []
+
+    @contextlib.contextmanager
+    def use(d):
+        now.append(str(d))
+        yield
+        now.pop()
+
+    b, keep = _batch([3], [4])
+    batch = types.SimpleNamespace(c=lambda: b, chunk_lens=types.SimpleNamespace(device=torch.device(device)))
+    monkeypatch.setattr(torch.cuda, "device", use)
+    monkeypatch.setattr(_lib, "call", lambda name, *args: seen.append((name, list(now))))
+    assert s2l.s2l_linear_attn_workspace_bytes(batch, 8) == 0
+    assert seen == [("s2l_linear_attn_workspace_bytes", current)]
