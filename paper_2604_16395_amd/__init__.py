@@ -320,6 +320,9 @@ def s2l_rope_kv_append(cache, batch, rope, q, q_out, k, v, stream=None):
     vp, vs, hv = _rows(v, "v", batch)
     _same_heads(hk, cache.num_kv_heads, "k and the cache")
     _same_heads(hv, cache.num_kv_heads, "v and the cache")
+    for name in ("k_pages", "v_pages", "k_scale", "v_scale") if cache.fp8 else ("k_pages", "v_pages"):
+        if getattr(cache, name).device != batch.chunk_lens.device:
+            raise ValueError(f"{name} is on {getattr(cache, name).device}, the batch on {batch.chunk_lens.device}")
     cc, bc, rc = cache.c(), batch.c(), rope.c(batch.total_tokens, batch.chunk_lens.device)
     _call_on(batch, "s2l_rope_kv_append", ctypes.byref(cc), ctypes.byref(bc), ctypes.byref(rc), qp, qs, hq, op, os_, kp, ks, vp, vs,
              stream=stream)

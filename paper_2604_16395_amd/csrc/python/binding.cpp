@@ -249,6 +249,16 @@ bool attr_tensor(PyObject* o, PyObject* name, PyObject* dtype, long dev, void** 
   return t && tensor(t.o, dtype, p) && numel(t.o, n) && on_device(t.o, dev);
 }
 
+// The cache's pages, and the scales that e4m3 pages come with, are on the device.
+bool cache_on_device(PyObject* o, const s2l_kv_cache& c, long dev) {
+  PyObject* const names[] = {s_k_pages, s_v_pages, s_k_scale, s_v_scale};
+  for (int i = 0; i < (c.dtype == S2L_KV_FP8_E4M3 ? 4 : 2); ++i) {
+    const Ref t(PyObject_GetAttr(o, names[i]));
+    if (!t || !on_device(t.o, dev)) return false;
+  }
+  return true;
+}
+
 bool rope_arg(PyObject* o, int64_t tokens, long dev, s2l_rope* r) {
   if ((PyObject*)Py_TYPE(o) != rope_type) return false;
   *r = s2l_rope{};
@@ -399,7 +409,8 @@ PyObject* rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int64_t tokens;
   long dev;
   void* stream;
-  if (n != 8 || !cache_arg(a[0], &cache) || !batch_on_device(a[1], &batch, &tokens, &dev) || !rope_arg(a[2], tokens, dev, &rope) ||
+  if (n != 8 || !cache_arg(a[0], &cache) || !batch_on_device(a[1], &batch, &tokens, &dev) || !cache_on_device(a[0], cache, dev) ||
+      !rope_arg(a[2], tokens, dev, &rope) ||
       !k.take(a[5], tokens, dev) || !v.take(a[6], tokens, dev) || k.heads != cache.num_kv_heads || v.heads != k.heads ||
       !stream_arg(a[7], &stream))
     return general();

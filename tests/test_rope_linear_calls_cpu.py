@@ -3,6 +3,7 @@ does not read, and of those on other devices."""
 import contextlib
 import types
 
+import numpy as np
 import pytest
 import torch
 
@@ -53,3 +54,18 @@ def test_workspaces_are_sized_on_the_batch_s_device(monkeypatch, device, current
     monkeypatch.setattr(_lib, "call", lambda name, *args: seen.append((name, list(now))))
     assert s2l.s2l_linear_attn_workspace_bytes(batch, 8) == 0
     assert seen == [("s2l_linear_attn_workspace_bytes", current)]
+
+
+@pytest.mark.parametrize("away", ["k_pages", "v_pages", "k_scale", "v_scale"])
+def test_the_rotating_append_refuses_a_cache_on_another_device(monkeypatch, away):
+    """Its kernel would write through a pointer that is not of its device."""
+    batch = s2l.Batch([16], [4], np.zeros((1, 2), np.int32), device="cpu")
+    pages = [torch.zeros((2, 2, 16, 128), dtype=torch.uint8, device="meta" if away == n else "cpu") for n in ("k_pages", "v_pages")]
+    scales = [torch.ones(2, device="meta" if away == n else "cpu") for n in ("k_scale", "v_scale")]
+    rows = torch.zeros((4, 2, 128), dtype=torch.bfloat16)
+    monkeypatch.setattr(s2l, "_rows", lambda t, name, batch: (None, 256, t.shape[1]))   # as of tensors on the batch's GPU
+    monkeypatch.setattr(s2l, "_call_on", lambda *args, **kw: None)
+    with pytest.raises(ValueError, match=f"{away} is on meta"):
+        s2l.s2l_rope_kv_append(s2l.PagedKVCache(*pages, *scales), batch, s2l.Rope(torch.ones(64)), None, None, rows, rows, 0)
+    fine = s2l.PagedKVCache(*(torch.zeros((2, 2, 16, 128), dtype=torch.bfloat16) for _ in range(2)))
+    s2l.s2l_rope_kv_append(fine, batch, s2l.Rope(torch.ones(64)), None, None, rows, rows, 0)
