@@ -269,10 +269,11 @@ s2l_status s2l_linear_attn_workspace_bytes(const s2l_batch* batch, int32_t num_q
  *                 out overlaps nothing that is read.  Rows from T on are not touched.
  *   workspace   : device, ws_bytes >= s2l_linear_attn_workspace_bytes(...); NULL when that is 0.
  * Precision: states and sums in fp32.  Where the bf16 MFMA takes a product, factors that are not bf16
- * values go as the sum of two of them (2^-16 relative) for outputs, of three for states.  Chunks scale what
- * joins a state by up to 2^60 on the way: states and products k v below 2^66 in magnitude are safe from
- * overflow.  A value of v that is not finite reaches the rows from its own on, and the state, as a value that
- * is not finite.
+ * values go as the sum of two of them (2^-16 relative) for outputs, of three for states.
+ * Range: of more than 5 tokens, chunks scale what joins a state by up to 2^60 on the way, and form q k before they
+ * multiply by v.  With B the state's sum with every term's absolute value, nothing overflows while v, B and the sums
+ * over the 128 dims of |q| B are below 2^67 in magnitude and those of |q k| below 2^127.  A value of v that is not
+ * finite reaches the rows from its own on, and the state, as a value that is not finite.
  * Errors: EINVAL, EWORKSPACE, ENOTSUP (more than 65535 requests or heads, or 2^23 requests times heads), EHIP.
  */
 s2l_status s2l_linear_attn(const s2l_linear_state* state, const s2l_batch* batch, const void* q, int64_t q_stride,
