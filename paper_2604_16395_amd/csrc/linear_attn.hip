@@ -53,8 +53,8 @@ __device__ inline double clean_log(float g) {
 // log2 of a decay in two fp32 terms, and powers of the decay: the whole part of the exponent is taken out before anything is
 // rounded, so that a power is off by the rounding of its fraction (2^-25) and by exp2's (2^-23 at most) however large the
 // exponent.  S is kept up to 2^kMostBehind behind and weights near 1 are products of such powers: with exponents rounded
-// whole (2^-19 at 60) states after 2049 to 4205 tokens were off by up to 2.4e-6 of their norm, like this by 1.7e-7; it costs
-// 0.7 to 1.5% of a call.
+// whole (2^-19 at 60) states after 2049 to 4205 tokens were off by up to 2.4e-6 of their norm, like this by 1.7e-7, for
+// 0.4 to 0.9% of a call's time.
 struct Decay {
   float hi, lo;
   __device__ explicit Decay(float log_decay) {
@@ -484,6 +484,7 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
     scores(0, 0);
   }
   int behind = 0;      // tokens that S has yet to fade by: the state is l^behind S
+  float late = 1.f;    // l^behind
   int at = 0;          // the block's stage
   for (int b = 0; b < blocks; ++b) {
     // With outputs the next block's tile has to be there too, for its scores.
@@ -512,6 +513,7 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
     // by as much.
     const int after = behind + valid;
     const bool fades = kOutputs && (b + 1 == blocks || -decay.exponent(after) > kMostBehind);
+    const float by = kOutputs ? decay.power(after) : 1.f;
     float f[16];
     if (valid == kB) {
       const float join = decay.power(kOutputs ? (fades ? 0 : -after) : len - (nth(b) + 1) * kB);
@@ -572,7 +574,6 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
         o = mfma(sx.t[0], q, o);
       }
       if (fades) {
-        const float by = decay.power(after);
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
@@ -591,7 +592,7 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
     };
     join_state(vx[0].t, vx[1].t, kTerms);
     if constexpr (kOutputs) {
-      const float reach = since * decay.power(behind);
+      const float reach = since * late;
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[i] *= reach;
 #pragma unroll
@@ -628,6 +629,7 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
       }
     }
     behind = fades ? 0 : after;
+    late = fades ? 1.f : by;
     at = at + kStage == kRing ? 0 : at + kStage;
     if constexpr (!kDirect) {
       constexpr int kAhead = kOutputs ? 2 : 1;
@@ -801,6 +803,7 @@ __global__ __launch_bounds__(256, 2) void linear_narrow_kernel(LinearLaunch a) {
   scores(0);
 
   int behind = 0;      // tokens that S has yet to fade by: the state is l^behind S
+  float late = 1.f;    // l^behind
   int at = 0;          // the block's stage
   for (int b = 0; b < blocks; ++b) {
     // the next block's tile has to be there too, for its scores
@@ -849,6 +852,7 @@ __global__ __launch_bounds__(256, 2) void linear_narrow_kernel(LinearLaunch a) {
 
     const int after = behind + valid;
     const bool fades = b + 1 == blocks || -decay.exponent(after) > kMostBehind;
+    const float by = decay.power(after);
     float f[8];
     if (valid == kB) {
       const float join = decay.power(fades ? 0 : -after);
@@ -887,7 +891,6 @@ __global__ __launch_bounds__(256, 2) void linear_narrow_kernel(LinearLaunch a) {
       }
     }
     if (fades) {
-      const float by = decay.power(after);
 #pragma unroll
       for (int t = 0; t < 8; ++t)
 #pragma unroll
@@ -898,7 +901,6 @@ __global__ __launch_bounds__(256, 2) void linear_narrow_kernel(LinearLaunch a) {
 #pragma unroll
       for (int i = 2; i >= 0; --i) S[t] = mfma16(kk[t], vx.t[i], S[t]);
     }
-    const float late = decay.power(behind);
     const bf16x8 vv = __builtin_bit_cast(bf16x8, vw);
     uint16_t* dst = a.out + (row0 + b * kB + n) * a.out_stride + h * 128 + col0 + 4 * quarter;
 #pragma unroll
@@ -927,6 +929,7 @@ __global__ __launch_bounds__(256, 2) void linear_narrow_kernel(LinearLaunch a) {
       if (n + 16 < valid) *reinterpret_cast<u32x2_any*>(dst + 16 * a.out_stride) = y[1];
     }
     behind = fades ? 0 : after;
+    late = fades ? 1.f : by;
     at = next;
     if constexpr (!kDirect) {
       if (b + 2 < blocks) {
