@@ -9,9 +9,9 @@
 // follow one another); lane l holds unit l % 8 of head l / 8, the 16 elements of 8 pairs in two 16-byte
 // chunks, so that a lane's 8 sines and cosines serve all its heads and rows of a head are read and
 // written whole.  Units past the rotated dims, and V's, are copied.  Nothing is shared between waves: no LDS, no barrier.
-// Bound by the memory for many rows: 35107 rows of 32 + 8 + 8 heads, 863 MB, 158 us, 5.5 TB/s (168 with one head a
-// lane; 217 with one head a lane and the groups of a row far apart); by the chain of loads for few: one row 3.1 us, 512
-// rows 4.5 us (4.8 with two heads a lane).
+// Bound by the memory for many rows: 35107 rows of 32 + 8 + 8 heads, 863 MB, 160 us, 5.4 TB/s (171 with one head a
+// lane; 217 with one head a lane and the groups of a row far apart); by the chain of loads for few: one row 2.9 us, 512
+// rows 4.6 us (4.8 with two heads a lane), in a graph, one call after another.
 #include "launch.h"
 #include "s2l.h"
 #include "s2l_device.h"
@@ -170,11 +170,13 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a) {
   }
 }
 
-// Two heads a lane share its sines and cosines and halve the waves; as long as waves are few (8 a SIMD), more of them
-// hide more.
+// Two heads a lane share its sines and cosines and halve the waves; as long as waves are few (6 a SIMD), more of them
+// hide more.  One head a lane and two, us in a graph: 32 + 8 + 8 heads, 512 rows (3072 waves) 4.6 and 4.8, 1024 (6144) 7.9 and
+// 7.9, 1365 (8190) 9.6 and 8.9, 4096 24.0 and 21.8; 64 + 8 + 8 into e4m3 pages, 600 (6000) 8.3 and 8.1, 1000 11.4 and
+// 10.1; 32 + 32 without pages, 768 (6144) 8.4 and 8.4, 1024 10.1 and 10.1.
 template <bool kAdjacent, bool kAppend, bool kFp8>
 void launch(const RopeLaunch& a, hipStream_t stream) {
-  constexpr int64_t kFewWaves = 8192;
+  constexpr int64_t kFewWaves = 6144;
   const int heads = a.hq + a.hkv * (kAppend ? 2 : 1);
   const int64_t four_rows = ((int64_t)a.total_rows + 3) / 4, groups = (heads + 7) / 8;
   if (a.total_rows * groups <= kFewWaves)

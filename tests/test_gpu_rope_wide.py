@@ -1,4 +1,4 @@
-"""GPU: the rotation and the rotating append over enough rows for two heads a lane (more than 8192 waves of 8 heads of a row),
+"""GPU: the rotation and the rotating append over enough rows for two heads a lane (more than 6144 waves of 8 heads of a row),
 where a group of 16 heads can hold queries, keys and values at once; bounds as in test_gpu_rope."""
 import numpy as np
 import pytest
