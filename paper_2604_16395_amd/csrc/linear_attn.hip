@@ -6,9 +6,9 @@
 // (request, head) state.  Thread (kg, vq) keeps rows 4 kg .. + 3 and columns 4 vq .. + 3 of them in
 // registers over the request's tokens, so the state is read and written once; a row's part of q S is
 // summed over the eight row groups of a wave by lane swaps and over the four waves through LDS.  Bound by the
-// states: 64 requests of a token, 32 heads, 270 MB, 48.9 us, 5.5 TB/s; one request 3.7 us, by its chain of loads.
+// states: 64 requests of a token, 32 heads, 270 MB, 49 us, 5.5 TB/s; one request 3.2 us, by its chain of loads.
 // The launch has workgroups for every request, and those of long ones leave: a search for the short ones took
-// 51.5 us there, 632 instead of 390 for 2048 requests of 8 heads; 64 chunks of 100 tokens and one token cost 2% more.
+// 51.5 us there, 632 instead of 392 for 2048 requests of 8 heads; 64 chunks of 100 tokens and one token cost 2% more.
 //
 // Longer chunks take the blocked form, 32 tokens at a time: with n of them valid (zero rows behind),
 //   out_i = scale (sum_{j <= i} l^(i-j) (q_i . k_j) v_j + l^(i+1) q_i S),
@@ -31,10 +31,10 @@
 //
 // A piece of a chunk needs the state before it.  Chunks that are cut take three launches: what each piece alone
 // makes of its tokens, in its place of the workspace; their running sum under the decay; then the blocks,
-// which read K and V a second time.  Bound by the memory: 32768 tokens of 32 heads, 1.08 GB, 380 us (130 for the
-// pieces' own states, 12 for the sums, 233 to 290 for the blocks; 362 with the loads and stores alone).  Short
+// which read K and V a second time.  Bound by the memory: 32768 tokens of 32 heads, 1.08 GB, 372 to 388 us (127 to 142 for
+// the pieces' own states, 12 for the sums, 240 to 310 for the blocks; 362 in all with the loads and stores alone).  Short
 // chunks are bound by the blocks one after another and by the start of each launch (a unit's search 1 us, its states
-// and first tiles 3): 32 heads, 64 tokens 8.1 us, 256 17.0, 512 28 to 30 either way, 2048 in pieces 49.
+// and first tiles 3): 32 heads, 64 tokens 7.9 us, 256 17.2, 512 29 to 30 either way, 2048 in pieces 47.
 #include "launch.h"
 #include "s2l_device.h"
 
@@ -650,9 +650,9 @@ __global__ __launch_bounds__(256, 2) void linear_block_kernel(LinearLaunch a) {
 }
 
 // The blocked form of whole chunks with half of a head's columns a workgroup, 16 a wave.  Where there are few
-// workgroups, the blocks one after another are the time, and a wave has half as much to do in each: 1.43 us a block
-// instead of 1.94 (1.62 with the operands read where they are used).  Where there are many, reading K and Q for half
-// as many columns costs 1.25 times as much.
+// workgroups, the blocks one after another are the time, and a wave has half as much to do in each: 1.5 us a block
+// instead of 2.0 (32 heads, 64 to 512 tokens; 0.2 more with the operands read where they are used).  Where there are many,
+// reading K and Q for half as many columns costs 1.12 to 1.15 times as much (16 requests of 512 and 1024 tokens).
 // Other than above, products are 16 x 16 x 32 and state register (t, i) is key dim 16 t + 4 quarter + i of column
 // n: two of its quads are an operand's eight key dims, and Q's rows are read in the same halves.
 template <bool kDirect>

@@ -13,8 +13,9 @@
 namespace s2l {
 
 // Requests of at most kLinearShortTokens new tokens are advanced token by token, the others in blocks.  32 heads, token
-// by token against in blocks: 64 requests of 4 tokens 53.0 against 62.7 us, of 5 63.5 against 63.6, of 8 69.3 against
-// 67.2; 8 requests of 5 11.0 against 11.2, of 8 13.0 against 11.2; one request 5.4 against 8.3, of 12 7.9 against 8.4.
+// by token against in blocks, us: of 5 tokens one request 4.5 against 6.4, 8 requests 10.4 against 11.3, 64 57.5 against
+// 73; of 6 5.5 against 6.4, 12.5 against 11.2, 68 against 74; of 8 6.4 against 6.5, 14.7 against 11.3, 81 against 74; of 12
+// 8.1 against 6.4, 17.9 against 11.3, 109 against 76.  So the lines cross between 5 and 8, first for a few requests.
 constexpr int32_t kLinearShortTokens = 5, kLinearBlockTokens = 32;
 struct LinearPlan {          // how the batch is cut, from the host lengths
   int32_t piece_tokens;      // longer requests are cut into pieces of so many tokens (a multiple of a block)
@@ -87,11 +88,12 @@ inline double linear_narrow_cost(const s2l_batch* b, int32_t hq, int32_t num_cus
 
 // How linear attention cuts the batch: requests stay whole unless shorter pieces are estimated to be faster, and a
 // head of a whole request gets two workgroups where that is estimated to be faster still: its blocks' chain is
-// shorter, but every block costs 1.25 times as much.  32 heads, one workgroup a head and two: a chunk of 64 tokens
-// 10.1 us and 8.1, of 256 21.9 and 17.0; 8 requests of 389 to 1024 tokens 79 and 66, 16 of 512 78 and 99.
+// shorter, but a block's K and Q are read twice.  32 heads, one workgroup a head and two: a chunk of 64 tokens
+// 10.0 us and 7.9, of 256 22.1 and 17.2; 8 requests of 391 to 1004 tokens 74 and 64, 16 of 512 86 and 97.
 // Against the fastest of the measured piece lengths of each of those batches the choice takes 1.01 of the time in the
 // geometric mean and 1.08 at most (examples, 32 heads: 2048 tokens whole 131 us, in pieces of 256 46 us; 16 requests
-// of 1024 tokens whole 139 us, in pieces of 512 241).
+// of 1024 tokens whole 150 to 155 us, in pieces of 512 245).  (Times here are of calls one after another in a graph, over three
+// sets of tensors in turn.)
 inline LinearPlan linear_plan(const s2l_batch* b, int32_t hq, int32_t num_cus) {
   LinearPlan p = {};
   int64_t longest = 0, total = 0, units = 0;
