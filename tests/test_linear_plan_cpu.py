@@ -34,7 +34,7 @@ def plan(tmp_path_factory):
         pytest.skip("no C++ compiler")
     d = tmp_path_factory.mktemp("linear_plan")
     (d / "plan.cpp").write_text(PROGRAM)
-    subprocess.run([gxx, "-std=c++17", "-O1", "-Wall", "-Wno-unknown-pragmas", "-Werror", "-I", os.path.join(ROOT, "include"), "-I",
+    subprocess.run([gxx, "-std=c++17", "-O1", "-fsanitize=undefined", "-fno-sanitize-recover=undefined", "-Wall", "-Wno-unknown-pragmas", "-Werror", "-I", os.path.join(ROOT, "include"), "-I",
                     os.path.join(ROOT, "paper_2604_16395_amd", "csrc"), "-o", str(d / "plan"), str(d / "plan.cpp")], check=True)
 
     def run(C, hq, cus=256):
