@@ -192,7 +192,8 @@ class Rope:
 class LinearState:
     """A linear attention layer's request states: states fp32 [slots][Hq][128][128], log_decay fp32
     [Hq] (ln of each head's decay, <= 0), and each request's slots, int32 [R]: slot_in (-1: a zero
-    state) is read, slot_out (-1: not kept) is written; the same slot advances in place."""
+    state) is read, slot_out (-1: not kept) is written; the same slot advances in place.  Slots are the
+    caller's: the scheduler and the swap calls move pages alone, a preempted request's state stays in its slot."""
 
     def __init__(self, states, log_decay, slot_in, slot_out):
         self.states, self.log_decay, self.slot_in, self.slot_out = states, log_decay, slot_in, slot_out
