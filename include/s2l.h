@@ -241,9 +241,10 @@ s2l_status s2l_rope_kv_append(const s2l_kv_cache* cache, const s2l_batch* batch,
  *   slot_out : device [R]: the slot that receives the state after P_r + C_r tokens, or -1 for none.
  * slot_in[r] == slot_out[r] advances a state in place; another slot keeps the old one as it is (the
  * snapshot that a streamed context goes back to when an update cuts off what came after it).  C_r = 0
- * copies.  Slots are the caller's to give out; s2l_kv_swap_* and the scheduler move pages alone.  A slot_in outside [-1, num_slots) makes NaN of the request's rows and state; a slot_out
- * outside it stores nothing.  Not checked: slot_out entries >= 0 are distinct, and none is the
- * slot_in of another request of the call.
+ * copies.  Slots are the caller's to give out; s2l_kv_swap_* and the scheduler move pages alone.  A
+ * slot_in outside [-1, num_slots) makes NaN of the request's rows and state; a slot_out outside it
+ * stores nothing.  Not checked: slot_out entries >= 0 are distinct, and none is the slot_in of another
+ * request of the call.
  */
 typedef struct s2l_linear_state {
   float* states;
