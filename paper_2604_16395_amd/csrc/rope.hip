@@ -171,7 +171,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a) {
 }
 
 // Two heads a lane share its sines and cosines and halve the waves; as long as waves are few (6 a SIMD), more of them
-// hide more.  One head a lane and two, us in a graph: 32 + 8 + 8 heads, 512 rows (3072 waves) 4.6 and 4.8, 1024 (6144) 7.9 and
+// hide more.  One head a lane and two, us in a graph: 32 + 8 + 8 heads, 512 rows 4.6 and 4.8, 1024 (6144 waves) 7.9 and
 // 7.9, 1365 (8190) 9.6 and 8.9, 4096 24.0 and 21.8; 64 + 8 + 8 into e4m3 pages, 600 (6000) 8.3 and 8.1, 1000 11.4 and
 // 10.1; 32 + 32 without pages, 768 (6144) 8.4 and 8.4, 1024 10.1 and 10.1.
 template <bool kAdjacent, bool kAppend, bool kFp8>
