@@ -64,8 +64,12 @@ typedef enum s2l_status {
 
 typedef enum s2l_kv_dtype {
   S2L_KV_BF16 = 0,     /* bf16 elements                                                  */
-  S2L_KV_FP8_E4M3 = 1  /* OCP FP8 E4M3 (e4m3fn) codes with per-kv-head fp32 scales       */
+  S2L_KV_FP8_E4M3 = 1, /* OCP FP8 E4M3 (e4m3fn) codes with per-kv-head fp32 scales       */
+  S2L_KV_MXFP4 = 2     /* OCP MXFP4: E2M1 codes, a power of two for each 32 dims of a row */
 } s2l_kv_dtype;
+
+/* Bytes of one (page, kv head) of an MXFP4 pool: 16 x 64 of codes, then 16 x 4 of scales. */
+#define S2L_MXFP4_RUN_BYTES 1088
 
 /*
  * One layer's paged KV cache (Sec. 2.2).  K and V are separate pools, each laid out
@@ -75,11 +79,20 @@ typedef enum s2l_kv_dtype {
  * fp8 cache: the stored code of value x of kv head h is e4m3(fp32(x) * fp32(1/scale[h]))
  * with round-to-nearest-even and saturation to +-448 (NaN stays NaN); the cached value it
  * stands for is decode(code) * scale[h].  Scales are static, chosen by the caller, > 0.
+ *
+ * MXFP4 cache (not in the paper; 4.25 bits an element): pools of [num_pages][num_kv_heads] runs of
+ * S2L_MXFP4_RUN_BYTES, aligned to 16 bytes: of each of the 16 slots 64 bytes of E2M1 codes (dim d in
+ * byte d / 2, the low half first), then of each slot 4 scale bytes, one for each 32 dims (E8M0: byte b
+ * is 2^(b - 127), 255 NaN).  An append chooses them by the OCP rule, with the range of what it writes
+ * kept where bf16 has normal values: of a block with largest magnitude a, exponent
+ * e = max(floor(log2 a) - 2, -125), code = e2m1(x 2^-e), round to nearest even, saturating to +-6; a
+ * block that holds a NaN or an infinity becomes NaN throughout (byte 255, codes 0).  The cached value
+ * is decode(code) 2^e.  Attention takes any byte but 253 and 254, whose values pass bf16's range.
  */
 typedef struct s2l_kv_cache {
-  void* k_pages;          /* device; bf16 or uint8 codes                                   */
+  void* k_pages;          /* device; bf16 elements, uint8 codes or MXFP4 runs               */
   void* v_pages;          /* device; same layout                                           */
-  const float* k_scale;   /* device [num_kv_heads], fp8 only (must be NULL for bf16)       */
+  const float* k_scale;   /* device [num_kv_heads], fp8 only (must be NULL for the others) */
   const float* v_scale;   /* device [num_kv_heads], fp8 only                               */
   int32_t num_pages;
   int32_t num_kv_heads;
@@ -172,7 +185,7 @@ const char* s2l_last_error(void);
  * block_tables[r][p / 16], slot p % 16.  Only those slots are written; every other byte of
  * the pools is left untouched (a partially filled first page keeps its earlier slots).
  *   k_new, v_new : device bf16 [T][Hkv][128].
- * Errors: EINVAL (nulls, negative lengths, fp8 without scales), ERANGE (P_r + C_r >
+ * Errors: EINVAL (nulls, negative lengths, fp8 without scales, MXFP4 pools off 16 bytes), ERANGE (P_r + C_r >
  * max_pages_per_req * 16), ENOTSUP (head_dim/page_size), EHIP.
  */
 s2l_status s2l_kv_append(const s2l_kv_cache* cache, const s2l_batch* batch,
@@ -228,6 +241,39 @@ s2l_status s2l_rope_kv_append(const s2l_kv_cache* cache, const s2l_batch* batch,
                               const void* q, int64_t q_stride, int32_t num_q_heads, void* q_out,
                               int64_t q_out_stride, const void* k, int64_t k_stride, const void* v,
                               int64_t v_stride, void* stream);
+
+/*
+ * Norms of queries and keys for each head before they rotate (not in the paper, whose models have
+ * none): with r = 1 / sqrt(mean of the head's 128 squares + eps), dim d becomes
+ *   x_d r (weight[d] + offset)
+ * in fp32 on the way to the rotation; the result is rounded once, after it.  The squares' sum is fp32:
+ * heads of a norm of 2^64 and more overflow.
+ */
+typedef struct s2l_qk_norm {
+  const void* q_weight;     /* device [128] for all query heads; NULL: factors of 1, without offset */
+  const void* k_weight;     /* device [128] for all key heads, likewise                              */
+  float eps;                /* finite, > 0                                                           */
+  float offset;             /* finite; 1 where weights are kept as their distance from one, else 0   */
+  int32_t weight_dtype;     /* S2L_NORM_BF16 or S2L_NORM_FP32                                        */
+  int32_t reserved;
+} s2l_qk_norm;
+#define S2L_NORM_BF16 0
+#define S2L_NORM_FP32 1
+
+/*
+ * s2l_rope_qk and s2l_rope_kv_append of the normed queries and keys, in their one launch: arguments as
+ * there.  Pages and q_out of the append are bit for bit what s2l_norm_rope_qk followed by s2l_kv_append
+ * gives.  Values are appended as they are.
+ * Errors: as s2l_rope_qk and s2l_rope_kv_append, EINVAL (eps, offset, weight_dtype, weights not aligned
+ * to their elements).
+ */
+s2l_status s2l_norm_rope_qk(const s2l_batch* batch, const s2l_qk_norm* norm, const s2l_rope* rope, const void* q,
+                            int64_t q_stride, int32_t num_q_heads, void* q_out, int64_t q_out_stride, const void* k,
+                            int64_t k_stride, int32_t num_kv_heads, void* k_out, int64_t k_out_stride, void* stream);
+s2l_status s2l_norm_rope_kv_append(const s2l_kv_cache* cache, const s2l_batch* batch, const s2l_qk_norm* norm,
+                                   const s2l_rope* rope, const void* q, int64_t q_stride, int32_t num_q_heads,
+                                   void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride, const void* v,
+                                   int64_t v_stride, void* stream);
 
 /*
  * Linear attention with a decay for each query head, for layers whose cache is a state of fixed size
@@ -290,7 +336,8 @@ s2l_status s2l_linear_attn(const s2l_linear_state* state, const s2l_batch* batch
  * elements of positions 0..n_r-1 of every request, bit-exact (bf16 bits or fp8 codes, not
  * dequantised); n_r = P_r + C_r if include_chunk, else P_r.  Request r's rows go to rows
  * cu_out[r] .. cu_out[r] + n_r - 1 of k_out / v_out, each [rows][Hkv][128] elements of the
- * cache dtype.  Used by the tests and as the dense form of a swap-out.
+ * cache dtype; of an MXFP4 cache [rows][Hkv][68] bytes, aligned to 4: 64 of codes, then 4 scales.
+ * Used by the tests and as the dense form of a swap-out.
  *   cu_out : device int32 [R+1] row offsets chosen by the caller (need not be dense).
  *   k_out, v_out: device, caller-owned, at least max_r(cu_out[r] + n_r) rows.
  * Errors: EINVAL (nulls, negative lengths), ERANGE (P_r + C_r > max_pages_per_req * 16),
@@ -298,6 +345,25 @@ s2l_status s2l_linear_attn(const s2l_linear_state* state, const s2l_batch* batch
  */
 s2l_status s2l_kv_gather(const s2l_kv_cache* cache, const s2l_batch* batch, int32_t include_chunk,
                          const int32_t* cu_out, void* k_out, void* v_out, void* stream);
+
+/*
+ * Read cached K/V back as values: what attention sees of them, for code that takes rows of bf16 (a
+ * cache of another type, a layer of another kind, a check of what quantisation left).
+ *   part: which positions of each request: S2L_READ_PREFIX 0 .. P_r - 1, S2L_READ_ALL
+ *         0 .. P_r + C_r - 1, S2L_READ_CHUNK P_r .. P_r + C_r - 1.
+ *   k_out, v_out: device bf16 [out_rows][Hkv][128], aligned to 16 bytes; row cu_out[r] + i receives the
+ *         part's position number i of request r.  Rows outside [0, out_rows) are not written.
+ *   cu_out: device int32 [R], chosen by the caller (for the chunks, batch->cu_chunk gives dense rows).
+ * bf16 and MXFP4 values are exact (MXFP4 scale bytes 253 and 254 excepted); e4m3 ones are
+ * decode(code) * scale in fp32, rounded to bf16 (attention keeps the scale apart and rounds nothing).
+ * Errors: EINVAL (nulls, negative lengths, part, alignment), ERANGE (P_r + C_r > max_pages_per_req * 16),
+ * ENOTSUP (head_dim/page_size, more than 65535 requests), EHIP.
+ */
+#define S2L_READ_PREFIX 0
+#define S2L_READ_ALL 1
+#define S2L_READ_CHUNK 2
+s2l_status s2l_kv_read(const s2l_kv_cache* cache, const s2l_batch* batch, int32_t part, const int32_t* cu_out,
+                       void* k_out, void* v_out, int64_t out_rows, void* stream);
 
 /*
  * Validation of block-table contents on the device (the block tables of Sec. 2.2's paged
@@ -315,7 +381,7 @@ s2l_status s2l_check_tables(const s2l_kv_cache* cache, const s2l_batch* batch, i
  * memory and come back when it resumes; Sec. 4.2: blocks past an update's LCP are simply
  * dropped).  One layer's pages move between the device pools of `cache` and two pinned
  * host pools host_k, host_v laid out like them, [num_host_pages][num_kv_heads][16][128]
- * of the cache's element type (bf16 or fp8 codes: pages move as bytes, bit-exact).
+ * of the cache's element type, or MXFP4 runs like them (pages move as bytes, bit-exact).
  *   pairs: DEVICE int32 [n][2]; swap_out copies device page pairs[i][0] to host page
  *          pairs[i][1]; swap_in copies host page pairs[i][0] to device page pairs[i][1]
  *          (the scheduler's swap_out / swap_in lists have exactly these forms).  A pair
@@ -383,7 +449,8 @@ s2l_status s2l_attn_plan(const s2l_batch* batch, int32_t num_q_heads, int32_t nu
  *   out[cu_chunk[r]+i][h] = sum_j e^{s_j} V_r[j][g] / sum_j e^{s_j}     (bf16, RNE)
  *   lse[cu_chunk[r]+i][h] = ln sum_j e^{s_j}                             (fp32, optional)
  * K_r/V_r are read from the pages after the step's append (the chunk's own keys included;
- * for an fp8 cache these are its quantised values decode(code) * scale).  Precision: the
+ * for an fp8 or MXFP4 cache these are its quantised values).  A NaN among them reaches the rows that
+ * see its key; of an MXFP4 cache a NaN of V reaches no other row.  Precision: the
  * weights e^{s_j} / sum are applied as bf16 values normalised by their own sum, so out is
  * within about 2^-7 sum_j w_j |V_j - out| + 2^-8 |out| of the exact result; lse is the
  * log of the sum of those bf16 weights (within about 2^-8 of the exact value).
@@ -423,7 +490,7 @@ s2l_status s2l_append_chunk_prefill_attn(const s2l_kv_cache* cache, const s2l_ba
  * correctly rounded), code = e4m3(fp32(q * inv)), round to nearest even, saturating; the
  * result is the attention of those dequantised rows (code * s) over the dequantised cache,
  * to the same rounding contract as s2l_chunk_prefill_attn.  Arguments as there.  Returns
- * S2L_ENOTSUP for a bf16 cache or a plan with 16-column (decode) tiles.  The quantisation is
+ * S2L_ENOTSUP for a bf16 or MXFP4 cache or a plan with 16-column (decode) tiles.  The quantisation is
  * not in the paper: it is a variant of this library for caches that are already e4m3.
  */
 s2l_status s2l_chunk_prefill_attn_q8(const s2l_kv_cache* cache, const s2l_batch* batch, const void* q,

@@ -21,6 +21,16 @@ attention keeps a state a request instead of pages (``LinearState``)::
     s2l_rope_qk(batch, rope, q_raw, q, k_raw, k)                   # a layer without pages
     ws = torch.empty(s2l_linear_attn_workspace_bytes(batch, Hq), dtype=torch.uint8, device="cuda")
     s2l_linear_attn(state, batch, q, k, v, 128 ** -0.5, out, ws)
+
+Where the model norms queries and keys for each head before they rotate, ``s2l_norm_rope_kv_append`` and
+``s2l_norm_rope_qk`` do both in the rotation's launch (``QKNorm``).  A cache may be held in 4 bits: pools of
+``MXFP4_RUN_BYTES`` bytes a page and head, which every call on a cache takes as it takes the others (not the
+attention with quantised queries); ``s2l_kv_read`` reads any cache's rows back as bf16 values::
+
+    pools = [torch.zeros((pages, Hkv, MXFP4_RUN_BYTES), dtype=torch.uint8, device="cuda") for _ in "kv"]
+    cache = PagedKVCache(*pools)
+    s2l_norm_rope_kv_append(cache, batch, QKNorm(q_weight, k_weight), rope, q_raw, q, k_raw, v)
+    s2l_kv_read(cache, batch, S2L_READ_CHUNK, batch.cu_chunk, k_rows, v_rows)
 """
 import contextlib
 import ctypes
@@ -29,18 +39,20 @@ import numpy as np
 import torch
 
 from . import _lib
-from ._lib import (S2L_KV_BF16, S2L_KV_FP8_E4M3, S2LError, S2LLibraryMissing, s2l_plan_info,
-                   s2l_plan_opts)
+from ._lib import (S2L_KV_BF16, S2L_KV_FP8_E4M3, S2L_KV_MXFP4, S2L_READ_ALL, S2L_READ_CHUNK, S2L_READ_PREFIX, S2LError,
+                   S2LLibraryMissing, s2l_plan_info, s2l_plan_opts)
 
-__all__ = ["PagedKVCache", "Batch", "Rope", "LinearState", "rope_pair_axes", "plan_opts", "S2LError", "S2LLibraryMissing",
+__all__ = ["PagedKVCache", "Batch", "Rope", "QKNorm", "LinearState", "rope_pair_axes", "plan_opts", "S2LError", "S2LLibraryMissing",
            "s2l_abi_version", "s2l_kv_append", "s2l_kv_gather", "s2l_kv_swap_out", "s2l_kv_swap_in",
-           "s2l_rope_qk", "s2l_rope_kv_append", "s2l_linear_attn", "s2l_linear_attn_workspace_bytes",
+           "s2l_kv_read", "S2L_READ_PREFIX", "S2L_READ_ALL", "S2L_READ_CHUNK", "MXFP4_RUN_BYTES",
+           "s2l_rope_qk", "s2l_rope_kv_append", "s2l_norm_rope_qk", "s2l_norm_rope_kv_append", "s2l_linear_attn", "s2l_linear_attn_workspace_bytes",
            "s2l_check_tables", "s2l_append_chunk_prefill_attn", "s2l_calib_stream_read", "s2l_calib_mfma_bf16", "s2l_attn_workspace_bytes",
            "s2l_attn_plan", "s2l_chunk_prefill_attn", "s2l_chunk_prefill_attn_q8", "s2l_attn_main", "s2l_split_reduce",
            "s2l_plan_host", "library_path", "plan_status", "s2l_chunk_prefill_attn_noalloc"]
 
 HEAD_DIM = 128
 PAGE_SIZE = 16
+MXFP4_RUN_BYTES = _lib.S2L_MXFP4_RUN_BYTES     # of one page of one kv head: 16 x 64 of codes, 16 x 4 of scales
 
 
 def library_path():
@@ -68,18 +80,26 @@ def _check(t, dtype, name):
 
 
 class PagedKVCache:
-    """One layer's K and V page pools, each [num_pages][Hkv][16][128] (bf16, or uint8 E4M3)."""
+    """One layer's K and V page pools, each [num_pages][Hkv][16][128] (bf16, or uint8 E4M3), or
+    [num_pages][Hkv][MXFP4_RUN_BYTES] uint8 (MXFP4: codes and their scales, no scales apart)."""
 
     def __init__(self, k_pages, v_pages, k_scale=None, v_scale=None):
-        fp8 = k_pages.dtype == torch.uint8
-        _check(k_pages, torch.uint8 if fp8 else torch.bfloat16, "k_pages")
+        mxfp4 = k_pages.dtype == torch.uint8 and k_pages.dim() == 3
+        fp8 = k_pages.dtype == torch.uint8 and not mxfp4
+        _check(k_pages, torch.uint8 if fp8 or mxfp4 else torch.bfloat16, "k_pages")
         _check(v_pages, k_pages.dtype, "v_pages")
         if fp8:
             _check(k_scale, torch.float32, "k_scale")
             _check(v_scale, torch.float32, "v_scale")
+        if mxfp4:
+            if k_pages.shape[2] != MXFP4_RUN_BYTES or v_pages.shape != k_pages.shape:
+                raise ValueError(f"MXFP4 pools must be [num_pages][Hkv][{MXFP4_RUN_BYTES}] of one shape (got "
+                                 f"{tuple(k_pages.shape)} and {tuple(v_pages.shape)})")
+            if k_scale is not None or v_scale is not None:
+                raise ValueError("MXFP4 pools hold their scales: k_scale and v_scale must be None")
         self.k_pages, self.v_pages = k_pages, v_pages
         self.k_scale, self.v_scale = k_scale, v_scale
-        self.fp8 = fp8
+        self.fp8, self.mxfp4 = fp8, mxfp4
 
     @property
     def num_pages(self):
@@ -95,8 +115,8 @@ class PagedKVCache:
             k_scale=self.k_scale.data_ptr() if self.fp8 else None,
             v_scale=self.v_scale.data_ptr() if self.fp8 else None,
             num_pages=self.k_pages.shape[0], num_kv_heads=self.k_pages.shape[1],
-            head_dim=self.k_pages.shape[3], page_size=self.k_pages.shape[2],
-            dtype=S2L_KV_FP8_E4M3 if self.fp8 else S2L_KV_BF16)
+            head_dim=HEAD_DIM if self.mxfp4 else self.k_pages.shape[3], page_size=PAGE_SIZE if self.mxfp4 else self.k_pages.shape[2],
+            dtype=S2L_KV_MXFP4 if self.mxfp4 else S2L_KV_FP8_E4M3 if self.fp8 else S2L_KV_BF16)
 
 
 class Batch:
@@ -189,6 +209,34 @@ class Rope:
                              pair_axis=(ctypes.c_uint8 * 64)(*self.pair_axis))
 
 
+class QKNorm:
+    """The norms of queries and keys for each head: x / sqrt(mean x^2 + eps) * (weight + offset).
+
+    q_weight, k_weight: device [128], both bf16 or both fp32; None: no weight (nor offset).  offset: 1 where
+    weights are kept as their distance from one."""
+
+    def __init__(self, q_weight=None, k_weight=None, eps=1e-6, offset=0.0):
+        self.q_weight, self.k_weight, self.eps, self.offset = q_weight, k_weight, float(eps), float(offset)
+        self._check_weights()
+
+    def _check_weights(self):
+        given = [(w, n) for w, n in ((self.q_weight, "q_weight"), (self.k_weight, "k_weight")) if w is not None]
+        for w, name in given:
+            _check(w, torch.float32 if w.dtype == torch.float32 else torch.bfloat16, name)
+            if tuple(w.shape) != (HEAD_DIM,) or w.dtype != given[0][0].dtype:
+                raise ValueError(f"{name} must be a vector of {HEAD_DIM}, of one type with the other (got {w.dtype}, shape {tuple(w.shape)})")
+        return given
+
+    def c(self, device):
+        given = self._check_weights()     # the attributes may be others by now
+        for w, name in given:
+            if w.device != device:
+                raise ValueError(f"{name} is on {w.device}, the batch on {device}")
+        return _lib.s2l_qk_norm(q_weight=None if self.q_weight is None else self.q_weight.data_ptr(),
+                                k_weight=None if self.k_weight is None else self.k_weight.data_ptr(), eps=self.eps, offset=self.offset,
+                                weight_dtype=_lib.S2L_NORM_FP32 if given and given[0][0].dtype == torch.float32 else _lib.S2L_NORM_BF16)
+
+
 class LinearState:
     """A linear attention layer's request states: states fp32 [slots][Hq][128][128], log_decay fp32
     [Hq] (ln of each head's decay, <= 0), and each request's slots, int32 [R]: slot_in (-1: a zero
@@ -249,7 +297,7 @@ def _load_native():
         device, raw_stream = (getattr(torch._C, n, None) for n in ("_cuda_getDevice", "_cuda_getCurrentRawStream"))
         _native = _lib.binding((torch.Tensor, PagedKVCache, Batch, s2l_plan_opts, s2l_plan_info, torch.cuda.Stream,
                                 torch.bfloat16, torch.float32, torch.uint8, torch.cuda.is_initialized, device, raw_stream,
-                                Rope, LinearState, torch.int32))
+                                Rope, LinearState, torch.int32, QKNorm))
     return _native
 
 
@@ -288,12 +336,8 @@ def _same_heads(a, b, what):
         raise ValueError(f"{what} differ in their heads ({a} and {b})")
 
 
-def s2l_rope_qk(batch, rope, q, q_out, k=None, k_out=None, stream=None):
-    """Rotate the batch's query rows q into q_out and its key rows k (if any) into k_out: bf16
-    [rows][heads][128], rows at any stride; an output may be its own input."""
-    st = (_native or _load_native()).rope_qk(batch, rope, q, q_out, k, k_out, stream)
-    if st is not None:
-        return _lib.failed("s2l_rope_qk", st) if st else None
+def _rotate(name, batch, norm, rope, q, q_out, k, k_out, stream):
+    """s2l_rope_qk, or s2l_norm_rope_qk with a norm."""
     qp, qs, hq = _rows(q, "q", batch)
     op, os_, ho = _rows(q_out, "q_out", batch)
     _same_heads(hq, ho, "q and q_out")
@@ -302,16 +346,14 @@ def s2l_rope_qk(batch, rope, q, q_out, k=None, k_out=None, stream=None):
         kp, ks, hkv = _rows(k, "k", batch)
         kop, kos, ho = _rows(k_out, "k_out", batch)
         _same_heads(hkv, ho, "k and k_out")
-    bc, rc = batch.c(), rope.c(batch.total_tokens, batch.chunk_lens.device)
-    _call_on(batch, "s2l_rope_qk", ctypes.byref(bc), ctypes.byref(rc), qp, qs, hq, op, os_, kp, ks, hkv, kop, kos, stream=stream)
+    device = batch.chunk_lens.device
+    bc, rc = batch.c(), rope.c(batch.total_tokens, device)
+    how = [ctypes.byref(rc)] if norm is None else [ctypes.byref(norm.c(device)), ctypes.byref(rc)]
+    _call_on(batch, name, ctypes.byref(bc), *how, qp, qs, hq, op, os_, kp, ks, hkv, kop, kos, stream=stream)
 
 
-def s2l_rope_kv_append(cache, batch, rope, q, q_out, k, v, stream=None):
-    """s2l_kv_append of the rotated keys and of the values, with the rotated queries in q_out (q and
-    q_out None: none), in one launch; tensors as for s2l_rope_qk."""
-    st = (_native or _load_native()).rope_append(cache, batch, rope, q, q_out, k, v, stream)
-    if st is not None:
-        return _lib.failed("s2l_rope_kv_append", st) if st else None
+def _rotate_append(name, cache, batch, norm, rope, q, q_out, k, v, stream):
+    """s2l_rope_kv_append, or s2l_norm_rope_kv_append with a norm."""
     qp, qs, hq, op, os_ = None, 0, 0, None, 0
     if q is not None:
         qp, qs, hq = _rows(q, "q", batch)
@@ -321,12 +363,58 @@ def s2l_rope_kv_append(cache, batch, rope, q, q_out, k, v, stream=None):
     vp, vs, hv = _rows(v, "v", batch)
     _same_heads(hk, cache.num_kv_heads, "k and the cache")
     _same_heads(hv, cache.num_kv_heads, "v and the cache")
+    _cache_device(cache, batch)
+    device = batch.chunk_lens.device
+    cc, bc, rc = cache.c(), batch.c(), rope.c(batch.total_tokens, device)
+    how = [ctypes.byref(rc)] if norm is None else [ctypes.byref(norm.c(device)), ctypes.byref(rc)]
+    _call_on(batch, name, ctypes.byref(cc), ctypes.byref(bc), *how, qp, qs, hq, op, os_, kp, ks, vp, vs, stream=stream)
+
+
+def _cache_device(cache, batch):
     for name in ("k_pages", "v_pages", "k_scale", "v_scale") if cache.fp8 else ("k_pages", "v_pages"):
         if getattr(cache, name).device != batch.chunk_lens.device:
             raise ValueError(f"{name} is on {getattr(cache, name).device}, the batch on {batch.chunk_lens.device}")
-    cc, bc, rc = cache.c(), batch.c(), rope.c(batch.total_tokens, batch.chunk_lens.device)
-    _call_on(batch, "s2l_rope_kv_append", ctypes.byref(cc), ctypes.byref(bc), ctypes.byref(rc), qp, qs, hq, op, os_, kp, ks, vp, vs,
-             stream=stream)
+
+
+def s2l_rope_qk(batch, rope, q, q_out, k=None, k_out=None, stream=None):
+    """Rotate the batch's query rows q into q_out and its key rows k (if any) into k_out: bf16
+    [rows][heads][128], rows at any stride; an output may be its own input."""
+    st = (_native or _load_native()).rope_qk(batch, rope, q, q_out, k, k_out, stream)
+    if st is not None:
+        return _lib.failed("s2l_rope_qk", st) if st else None
+    _rotate("s2l_rope_qk", batch, None, rope, q, q_out, k, k_out, stream)
+
+
+def s2l_rope_kv_append(cache, batch, rope, q, q_out, k, v, stream=None):
+    """s2l_kv_append of the rotated keys and of the values, with the rotated queries in q_out (q and
+    q_out None: none), in one launch; tensors as for s2l_rope_qk."""
+    st = (_native or _load_native()).rope_append(cache, batch, rope, q, q_out, k, v, stream)
+    if st is not None:
+        return _lib.failed("s2l_rope_kv_append", st) if st else None
+    _rotate_append("s2l_rope_kv_append", cache, batch, None, rope, q, q_out, k, v, stream)
+
+
+def _need_norm(norm):
+    if not isinstance(norm, QKNorm):
+        raise ValueError(f"norm must be a QKNorm (got {type(norm).__name__})")
+
+
+def s2l_norm_rope_qk(batch, norm, rope, q, q_out, k=None, k_out=None, stream=None):
+    """s2l_rope_qk of queries and keys that `norm` (a QKNorm) norms for each head first."""
+    st = (_native or _load_native()).norm_rope_qk(batch, norm, rope, q, q_out, k, k_out, stream)
+    if st is not None:
+        return _lib.failed("s2l_norm_rope_qk", st) if st else None
+    _need_norm(norm)
+    _rotate("s2l_norm_rope_qk", batch, norm, rope, q, q_out, k, k_out, stream)
+
+
+def s2l_norm_rope_kv_append(cache, batch, norm, rope, q, q_out, k, v, stream=None):
+    """s2l_rope_kv_append of queries and keys that `norm` (a QKNorm) norms for each head first."""
+    st = (_native or _load_native()).norm_rope_append(cache, batch, norm, rope, q, q_out, k, v, stream)
+    if st is not None:
+        return _lib.failed("s2l_norm_rope_kv_append", st) if st else None
+    _need_norm(norm)
+    _rotate_append("s2l_norm_rope_kv_append", cache, batch, norm, rope, q, q_out, k, v, stream)
 
 
 def s2l_linear_attn_workspace_bytes(batch, num_q_heads):
@@ -410,6 +498,29 @@ def s2l_kv_gather(cache, batch, include_chunk, cu_out, k_out, v_out, stream=None
     cc, bc = cache.c(), batch.c()
     _lib.call("s2l_kv_gather", ctypes.byref(cc), ctypes.byref(bc), int(include_chunk), _ptr(cu_out),
               _ptr(k_out), _ptr(v_out), _stream(stream))
+
+
+def s2l_kv_read(cache, batch, part, cu_out, k_out, v_out, stream=None):
+    """Read cached K/V back as bf16 values: position number i of request r's part (S2L_READ_PREFIX, _ALL or
+    _CHUNK) goes to row cu_out[r] + i of k_out and v_out, contiguous bf16 [rows][Hkv][128]; rows that they
+    do not have are not written.  cu_out: device int32, a row for each request (batch.cu_chunk for chunks)."""
+    st = (_native or _load_native()).read(cache, batch, part, cu_out, k_out, v_out, stream)
+    if st is not None:
+        return _lib.failed("s2l_kv_read", st) if st else None
+    _check(cu_out, torch.int32, "cu_out")
+    if cu_out.dim() != 1 or cu_out.shape[0] < batch.num_reqs:
+        raise ValueError(f"cu_out must hold a row for each of the {batch.num_reqs} requests")
+    for t, name in ((k_out, "k_out"), (v_out, "v_out")):
+        _check(t, torch.bfloat16, name)
+        if t.dim() != 3 or t.shape[1] != cache.num_kv_heads or t.shape[2] != HEAD_DIM or t.shape[0] != k_out.shape[0]:
+            raise ValueError(f"{name} must be [rows][{cache.num_kv_heads}][{HEAD_DIM}], of as many rows as the other (got {tuple(t.shape)})")
+    for t, name in ((cu_out, "cu_out"), (k_out, "k_out"), (v_out, "v_out")):
+        if t.device != batch.chunk_lens.device:
+            raise ValueError(f"{name} is on {t.device}, the batch on {batch.chunk_lens.device}")
+    _cache_device(cache, batch)
+    cc, bc = cache.c(), batch.c()
+    _call_on(batch, "s2l_kv_read", ctypes.byref(cc), ctypes.byref(bc), int(part), _ptr(cu_out), _ptr(k_out), _ptr(v_out),
+             k_out.shape[0], stream=stream)
 
 
 def s2l_attn_workspace_bytes(batch, num_q_heads, num_kv_heads, opts=None):

@@ -18,7 +18,10 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("S2L_LIBRARY") or os.path.join(_HERE, "libs2l.so")
 
 S2L_OK, S2L_EINVAL, S2L_ERANGE, S2L_EWORKSPACE, S2L_ENOTSUP, S2L_EHIP = 0, -1, -2, -3, -4, -5
-S2L_KV_BF16, S2L_KV_FP8_E4M3 = 0, 1
+S2L_KV_BF16, S2L_KV_FP8_E4M3, S2L_KV_MXFP4 = 0, 1, 2
+S2L_MXFP4_RUN_BYTES = 1088
+S2L_READ_PREFIX, S2L_READ_ALL, S2L_READ_CHUNK = 0, 1, 2
+S2L_NORM_BF16, S2L_NORM_FP32 = 0, 1
 S2L_ROPE_ADJACENT, S2L_ROPE_MAX_AXES = 1, 4
 STATUS_NAMES = {0: "S2L_OK", -1: "S2L_EINVAL", -2: "S2L_ERANGE", -3: "S2L_EWORKSPACE",
                 -4: "S2L_ENOTSUP", -5: "S2L_EHIP"}
@@ -56,6 +59,11 @@ class s2l_plan_info(ctypes.Structure):
 class s2l_rope(ctypes.Structure):
     _fields_ = [("inv_freq", c_vp), ("positions", c_vp), ("pos_stride", c_i64), ("rot_dim", c_i32),
                 ("num_axes", c_i32), ("flags", c_i32), ("scale", ctypes.c_float), ("pair_axis", ctypes.c_uint8 * 64)]
+
+
+class s2l_qk_norm(ctypes.Structure):
+    _fields_ = [("q_weight", c_vp), ("k_weight", c_vp), ("eps", ctypes.c_float), ("offset", ctypes.c_float),
+                ("weight_dtype", c_i32), ("reserved", c_i32)]
 
 
 class s2l_linear_state(ctypes.Structure):
@@ -98,6 +106,7 @@ P_batch = ctypes.POINTER(s2l_batch)
 P_opts = ctypes.POINTER(s2l_plan_opts)
 P_info = ctypes.POINTER(s2l_plan_info)
 P_rope = ctypes.POINTER(s2l_rope)
+P_norm = ctypes.POINTER(s2l_qk_norm)
 P_state = ctypes.POINTER(s2l_linear_state)
 
 # name -> (restype, argtypes); the list of every symbol include/s2l.h declares
@@ -108,10 +117,15 @@ SIGNATURES = {
     "s2l_rope_qk": (c_i32, [P_batch, P_rope, c_vp, c_i64, c_i32, c_vp, c_i64, c_vp, c_i64, c_i32, c_vp, c_i64, c_vp]),
     "s2l_rope_kv_append": (c_i32, [P_cache, P_batch, P_rope, c_vp, c_i64, c_i32, c_vp, c_i64, c_vp, c_i64, c_vp, c_i64,
                                    c_vp]),
+    "s2l_norm_rope_qk": (c_i32, [P_batch, P_norm, P_rope, c_vp, c_i64, c_i32, c_vp, c_i64, c_vp, c_i64, c_i32, c_vp, c_i64,
+                                 c_vp]),
+    "s2l_norm_rope_kv_append": (c_i32, [P_cache, P_batch, P_norm, P_rope, c_vp, c_i64, c_i32, c_vp, c_i64, c_vp, c_i64,
+                                        c_vp, c_i64, c_vp]),
     "s2l_linear_attn_workspace_bytes": (c_i32, [P_batch, c_i32, ctypes.POINTER(ctypes.c_size_t)]),
     "s2l_linear_attn": (c_i32, [P_state, P_batch, c_vp, c_i64, c_vp, c_i64, c_vp, c_i64, c_i32, ctypes.c_float, c_vp,
                                 c_i64, c_vp, ctypes.c_size_t, c_vp]),
     "s2l_kv_gather": (c_i32, [P_cache, P_batch, c_i32, c_vp, c_vp, c_vp, c_vp]),
+    "s2l_kv_read": (c_i32, [P_cache, P_batch, c_i32, c_vp, c_vp, c_vp, c_i64, c_vp]),
     "s2l_check_tables": (c_i32, [P_cache, P_batch, c_vp, c_vp]),
     "s2l_kv_swap_out": (c_i32, [P_cache, c_vp, c_i32, c_vp, c_vp, c_i32, c_vp]),
     "s2l_kv_swap_in": (c_i32, [P_cache, c_vp, c_i32, c_vp, c_vp, c_i32, c_vp]),
@@ -196,7 +210,7 @@ class _NoBinding:
     def _refuse(*_):
         return None
 
-    append = plan = attn = fused = reduce = rope_qk = rope_append = linear = _refuse
+    append = plan = attn = fused = reduce = rope_qk = rope_append = linear = norm_rope_qk = norm_rope_append = read = _refuse
 
 
 def binding(objects):
@@ -217,6 +231,7 @@ def binding(objects):
                       "build it with `python -m paper_2604_16395_amd.build`", RuntimeWarning, stacklevel=3)
         return _NoBinding
     names = ("s2l_kv_append", "s2l_attn_plan", "s2l_chunk_prefill_attn", "s2l_chunk_prefill_attn_q8", "s2l_attn_main",
-             "s2l_append_chunk_prefill_attn", "s2l_split_reduce", "s2l_rope_qk", "s2l_rope_kv_append", "s2l_linear_attn")
+             "s2l_append_chunk_prefill_attn", "s2l_split_reduce", "s2l_rope_qk", "s2l_rope_kv_append", "s2l_linear_attn",
+             "s2l_norm_rope_qk", "s2l_norm_rope_kv_append", "s2l_kv_read")
     _binding.setup(objects, tuple(ctypes.cast(getattr(handle, n), c_vp).value for n in names))
     return _binding

@@ -359,11 +359,21 @@ s2l_status check_cache(const s2l_kv_cache* c, const s2l_batch* b) {
     if (!c->k_scale || !c->v_scale) return fail(S2L_EINVAL, "fp8 cache needs k_scale and v_scale");
   } else if (c->dtype == S2L_KV_BF16) {
     if (c->k_scale || c->v_scale) return fail(S2L_EINVAL, "bf16 cache must pass NULL scales");
+  } else if (c->dtype == S2L_KV_MXFP4) {
+    if (c->k_scale || c->v_scale) return fail(S2L_EINVAL, "MXFP4 cache must pass NULL scales (they are in its pages)");
+    if (reinterpret_cast<uintptr_t>(c->k_pages) % 16 != 0 || reinterpret_cast<uintptr_t>(c->v_pages) % 16 != 0)
+      return fail(S2L_EINVAL, "MXFP4 pages must be aligned to 16 bytes");
   } else {
     return fail(S2L_EINVAL, "unknown kv dtype %d", c->dtype);
   }
   (void)b;
   return S2L_OK;
+}
+
+static_assert(S2L_MXFP4_RUN_BYTES == s2l::kMxRunBytes, "the header's run is the kernels'");
+
+s2l::PageKind page_kind(const s2l_kv_cache* c) {
+  return c->dtype == S2L_KV_MXFP4 ? s2l::kMxfp4Pages : c->dtype == S2L_KV_FP8_E4M3 ? s2l::kE4m3Pages : s2l::kBf16Pages;
 }
 
 s2l::KvLaunch kv_launch(const s2l_kv_cache* c, const s2l_batch* b) {
@@ -380,7 +390,7 @@ s2l::KvLaunch kv_launch(const s2l_kv_cache* c, const s2l_batch* b) {
   a.hkv = c->num_kv_heads;
   a.num_reqs = b->num_reqs;
   a.num_pages = c->num_pages;
-  a.fp8 = c->dtype == S2L_KV_FP8_E4M3;
+  a.kind = page_kind(c);
   return a;
 }
 
@@ -597,8 +607,20 @@ s2l_status check_rope(const s2l_rope* rope, int64_t T) {
   return S2L_OK;
 }
 
-s2l_status rope_launch(const char* what, const s2l_kv_cache* cache, const s2l_batch* batch, const s2l_rope* rope,
-                       int64_t T, const void* q, int64_t q_stride, int32_t hq, void* q_out, int64_t q_out_stride,
+s2l_status check_norm(const s2l_qk_norm* norm) {
+  if (!norm) return fail(S2L_EINVAL, "norm is NULL");
+  if (norm->weight_dtype != S2L_NORM_BF16 && norm->weight_dtype != S2L_NORM_FP32)
+    return fail(S2L_EINVAL, "unknown norm weight dtype %d", norm->weight_dtype);
+  if (!(norm->eps > 0.0f) || !std::isfinite(norm->eps)) return fail(S2L_EINVAL, "norm eps must be finite and > 0");
+  if (!std::isfinite(norm->offset)) return fail(S2L_EINVAL, "norm offset must be finite");
+  const uintptr_t size = norm->weight_dtype == S2L_NORM_FP32 ? 4 : 2;
+  for (const void* w : {norm->q_weight, norm->k_weight})
+    if (reinterpret_cast<uintptr_t>(w) % size != 0) return fail(S2L_EINVAL, "a norm weight is not aligned to its elements");
+  return S2L_OK;
+}
+
+s2l_status rope_launch(const char* what, const s2l_kv_cache* cache, const s2l_batch* batch, const s2l_qk_norm* norm,
+                       const s2l_rope* rope, int64_t T, const void* q, int64_t q_stride, int32_t hq, void* q_out, int64_t q_out_stride,
                        const void* k, int64_t k_stride, int32_t hkv, void* k_out, int64_t k_out_stride, const void* v,
                        int64_t v_stride, void* stream) {
   s2l_status st;
@@ -649,7 +671,15 @@ s2l_status rope_launch(const char* what, const s2l_kv_cache* cache, const s2l_ba
     a.v_pool = cache->v_pages;
     a.k_scale = cache->k_scale;
     a.v_scale = cache->v_scale;
-    a.fp8 = cache->dtype == S2L_KV_FP8_E4M3;
+    a.kind = page_kind(cache);
+  }
+  if (norm) {
+    a.norm = true;
+    a.norm_fp32 = norm->weight_dtype == S2L_NORM_FP32;
+    a.q_weight = norm->q_weight;
+    a.k_weight = norm->k_weight;
+    a.eps = norm->eps;
+    a.offset = norm->offset;
   }
   (void)hipGetLastError();
   hipError_t e = s2l::launch_rope(a, static_cast<hipStream_t>(stream));
@@ -752,7 +782,7 @@ s2l_status s2l_rope_qk(const s2l_batch* batch, const s2l_rope* rope, const void*
   s2l_status st;
   int64_t T = 0;
   if ((st = check_rows(batch, true, &T)) != S2L_OK) return st;
-  return rope_launch("rope_qk", nullptr, batch, rope, T, q, q_stride, num_q_heads, q_out, q_out_stride, k, k_stride,
+  return rope_launch("rope_qk", nullptr, batch, nullptr, rope, T, q, q_stride, num_q_heads, q_out, q_out_stride, k, k_stride,
                      num_kv_heads, k_out, k_out_stride, nullptr, 0, stream);
 }
 
@@ -763,8 +793,32 @@ s2l_status s2l_rope_kv_append(const s2l_kv_cache* cache, const s2l_batch* batch,
   int64_t T = 0;
   if ((st = check_cache(cache, batch)) != S2L_OK) return st;
   if ((st = check_batch(batch, true, &T)) != S2L_OK) return st;
-  return rope_launch("rope_kv_append", cache, batch, rope, T, q, q_stride, num_q_heads, q_out, q_out_stride, k,
+  return rope_launch("rope_kv_append", cache, batch, nullptr, rope, T, q, q_stride, num_q_heads, q_out, q_out_stride, k,
                      k_stride, cache->num_kv_heads, nullptr, 0, v, v_stride, stream);
+}
+
+s2l_status s2l_norm_rope_qk(const s2l_batch* batch, const s2l_qk_norm* norm, const s2l_rope* rope, const void* q,
+                            int64_t q_stride, int32_t num_q_heads, void* q_out, int64_t q_out_stride, const void* k,
+                            int64_t k_stride, int32_t num_kv_heads, void* k_out, int64_t k_out_stride, void* stream) {
+  s2l_status st;
+  int64_t T = 0;
+  if ((st = check_rows(batch, true, &T)) != S2L_OK) return st;
+  if ((st = check_norm(norm)) != S2L_OK) return st;
+  return rope_launch("norm_rope_qk", nullptr, batch, norm, rope, T, q, q_stride, num_q_heads, q_out, q_out_stride, k,
+                     k_stride, num_kv_heads, k_out, k_out_stride, nullptr, 0, stream);
+}
+
+s2l_status s2l_norm_rope_kv_append(const s2l_kv_cache* cache, const s2l_batch* batch, const s2l_qk_norm* norm,
+                                   const s2l_rope* rope, const void* q, int64_t q_stride, int32_t num_q_heads,
+                                   void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride, const void* v,
+                                   int64_t v_stride, void* stream) {
+  s2l_status st;
+  int64_t T = 0;
+  if ((st = check_cache(cache, batch)) != S2L_OK) return st;
+  if ((st = check_batch(batch, true, &T)) != S2L_OK) return st;
+  if ((st = check_norm(norm)) != S2L_OK) return st;
+  return rope_launch("norm_rope_kv_append", cache, batch, norm, rope, T, q, q_stride, num_q_heads, q_out, q_out_stride,
+                     k, k_stride, cache->num_kv_heads, nullptr, 0, v, v_stride, stream);
 }
 
 s2l_status s2l_linear_attn_workspace_bytes(const s2l_batch* batch, int32_t num_q_heads, size_t* bytes_out) {
@@ -883,8 +937,7 @@ static s2l_status kv_swap(const char* what, const s2l_kv_cache* cache, const int
                   what, i ? 'v' : 'k');
     dev_view[i] = attr.devicePointer;
   }
-  const int64_t page_bytes = (int64_t)cache->num_kv_heads * s2l::kPageSize * s2l::kHeadDim *
-                             (cache->dtype == S2L_KV_FP8_E4M3 ? 1 : 2);
+  const int64_t page_bytes = (int64_t)cache->num_kv_heads * s2l::run_bytes(page_kind(cache));
   (void)hipGetLastError();
   hipError_t e = to_host
       ? s2l::launch_kv_page_copy(cache->k_pages, cache->v_pages, dev_view[0], dev_view[1], pairs, n,
@@ -923,6 +976,32 @@ s2l_status s2l_kv_gather(const s2l_kv_cache* cache, const s2l_batch* batch, int3
   hipError_t e = s2l::launch_kv_gather(kv_launch(cache, batch), include_chunk, cu_out, k_out, v_out, max_read,
                                        static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail("kv_gather launch", e);
+  return ok();
+}
+
+s2l_status s2l_kv_read(const s2l_kv_cache* cache, const s2l_batch* batch, int32_t part, const int32_t* cu_out,
+                       void* k_out, void* v_out, int64_t out_rows, void* stream) {
+  s2l_status st;
+  int64_t T = 0;
+  if ((st = check_cache(cache, batch)) != S2L_OK) return st;
+  if ((st = check_batch(batch, true, &T)) != S2L_OK) return st;
+  if (part != S2L_READ_PREFIX && part != S2L_READ_ALL && part != S2L_READ_CHUNK)
+    return fail(S2L_EINVAL, "unknown part %d", part);
+  if (batch->num_reqs > 65535) return fail(S2L_ENOTSUP, "kv_read supports at most 65535 requests");
+  if (out_rows < 0) return fail(S2L_EINVAL, "out_rows %lld < 0", (long long)out_rows);
+  const bool skip_prefix = part == S2L_READ_CHUNK, with_chunk = part != S2L_READ_PREFIX;
+  int32_t max_read = 0;
+  for (int32_t r = 0; r < batch->num_reqs; ++r) {
+    const int32_t p = batch->prefix_lens_host[r], n = p + (with_chunk ? batch->chunk_lens_host[r] : 0), b = skip_prefix ? p : 0;
+    if (n > b) max_read = std::max(max_read, (n - 1) / s2l::kPageSize - b / s2l::kPageSize + 1);
+  }
+  if (max_read > 0 && out_rows > 0 && (!cu_out || !k_out || !v_out)) return fail(S2L_EINVAL, "cu_out/k_out/v_out is NULL");
+  if (reinterpret_cast<uintptr_t>(k_out) % 16 != 0 || reinterpret_cast<uintptr_t>(v_out) % 16 != 0)
+    return fail(S2L_EINVAL, "k_out and v_out must be aligned to 16 bytes");
+  (void)hipGetLastError();
+  hipError_t e = s2l::launch_kv_read(kv_launch(cache, batch), skip_prefix, with_chunk, cu_out, k_out, v_out, out_rows,
+                                     max_read, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail("kv_read launch", e);
   return ok();
 }
 

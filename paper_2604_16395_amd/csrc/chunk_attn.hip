@@ -148,15 +148,15 @@ __device__ inline float merge_weight(float m_s, float mstar) {
 // 8-column-wave bf16 kernel, which runs alone on its CU; two otherwise), or the fp32 rows of a
 // split tile where those are larger (the 8-column-wave e4m3 kernel, whose registers allow one
 // workgroup a CU anyway).
-template <bool kFp8, int kColWaves, int kHalves>
+template <PageKind kKind, int kColWaves, int kHalves>
 struct Ring {
-  static constexpr int kStages = (!kFp8 && kColWaves == 8) ? 4 : 2;
+  static constexpr int kStages = (kKind == kBf16Pages && kColWaves == 8) ? 4 : 2;
   static constexpr int kGroupBytes = 2 * kStages * kTileBytes;
   static constexpr int kTileRows = kColWaves * 32 * kHeadDim * 4;
   static constexpr int kBytes = kHalves * kGroupBytes > kTileRows ? kHalves * kGroupBytes : kTileRows;
 };
 
-template <bool kFp8, int kColWaves, int kHalves, bool kFused, bool kQ8>
+template <PageKind kKind, int kColWaves, int kHalves, bool kFused, bool kQ8>
 __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)) void attn_main_kernel(
     const ItemRec* __restrict__ items, const PlanHeader* __restrict__ hdr, int32_t xcd_items,
     int32_t max_pages, const int32_t* __restrict__ block_tables, const uint16_t* __restrict__ q, int32_t hq,
@@ -165,7 +165,9 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
     const float* __restrict__ kscale, const float* __restrict__ vscale, int32_t hkv, float scale_log2,
     float* __restrict__ partials, const uint16_t* __restrict__ knew, const uint16_t* __restrict__ vnew,
     int64_t total_rows) {
-  using RingT = Ring<kFp8, kColWaves, kHalves>;
+  constexpr bool kFp8 = kKind == kE4m3Pages, kMx = kKind == kMxfp4Pages;
+  constexpr bool kWiden = kKind != kBf16Pages;       // pages that go through registers and are widened to bf16
+  using RingT = Ring<kKind, kColWaves, kHalves>;
   constexpr int kWaves = kColWaves * kHalves;
   constexpr int kS = RingT::kStages;
   static_assert(kHalves == 1 || kHalves == 2, "one or two key-range groups");
@@ -175,10 +177,12 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
   constexpr int kRowsPerWave = 16 / kQuarters;       // key rows each wave moves per tile
   constexpr int kDma = kRowsPerWave / 4;             // bf16: 1 KiB LDS-direct loads per wave
   constexpr int kF8Loads = kRowsPerWave / 8;         // e4m3: 16-byte loads per lane
-  constexpr int kRun = kFp8 ? 16 * 128 : 16 * 128 * 2;   // bytes of one (page, kv head)
+  constexpr int kMxLanes = 64 / kRowsPerWave;        // MXFP4: lanes sharing a row, 8 or 16 bytes of codes each
+  constexpr int kRun = run_bytes(kKind);             // bytes of one (page, kv head)
   constexpr int kKeyBytes = kRun / 16;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[RingT::kBytes];
   __shared__ __attribute__((aligned(256))) int32_t s_pages[kWaves][2][64];   // next page windows
+  __shared__ int32_t s_nan[kMx ? kMxScaleBytes : 1];   // MXFP4: the first key whose V is NaN, of each 32 dims
 
   // the item (one scalar load) and the device plan's item count, fetched together.  When
   // the items cost about the same, consecutive items (one kv head's pages) go to one XCD's
@@ -240,13 +244,18 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
   for (int j = 0; j <= kS; ++j) pg[j] = scalar_load(bt + min((lo >> 4) + 4 * j + pw, last_page));
 
   // Q^T operand: lane (n, half) holds Q[col][16 ks + 8 half .. +7] for ks = 0..7.
+  if constexpr (kMx) {   // before the barriers that tile stores come after
+    if (threadIdx.x < kMxScaleBytes) s_nan[threadIdx.x] = 0x7FFFFFFF;
+    wait_lgkmcnt0();
+    __builtin_amdgcn_s_barrier();
+  }
   bf16x8 qf[8];
   // kQ8: the column quantised to e4m3 with its own scale sq = max |Q[col]| / 448 (1 for a
   // zero column; both divisions correctly rounded, codes RNE with saturation, as the page
   // encoder); for the fp8 MFMA of k-half j lane (n, half) holds the codes of
   // Q[col][32 (2 j + half) + b], b < 32, and the scores take sq in their scale.
   i32x8 q8[2];
-  if constexpr (!kFp8) {
+  if constexpr (!kWiden) {
     // copied through LDS below, so that its latency overlaps that of the first K and V tiles
   } else if constexpr (!kQ8) {
     const uint16_t* qrow = q + ((int64_t)(row0 + (valid ? tok : 0)) * hq + (valid ? hq_col : 0)) * 128 + 8 * half;
@@ -320,15 +329,19 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
 
   // Tile loads: column wave cw moves rows [s0, s0 + kRowsPerWave) of page pw of each tile.
   const int s0 = (cw % kQuarters) * kRowsPerWave;
-  uint32_t kvo[kFp8 ? kF8Loads : kDma], vvo[kFp8 ? kF8Loads : kDma];
+  uint32_t kvo[kWiden ? kF8Loads : kDma], vvo[kWiden ? kF8Loads : kDma];
   // Fused append (bf16, page-aligned prefixes): keys at or past P, the chunk's own, are
   // copied straight from the new K/V rows (row stride hkv * 256 bytes) instead of the pages,
   // which this same launch writes; kno / vno are the lane offsets for that source.
-  static_assert(!(kFp8 && kFused), "the fused append is for bf16 pages");
+  static_assert(!(kWiden && kFused), "the fused append is for bf16 pages");
   static_assert(!kQ8 || kFp8, "Q is quantised only against e4m3 pages");
   const uint32_t new_stride = (uint32_t)hkv * kRowBytes;
-  uint32_t kno[kFp8 ? 1 : kDma], vno[kFp8 ? 1 : kDma];
-  if constexpr (!kFp8) {
+  uint32_t kno[kWiden ? 1 : kDma], vno[kWiden ? 1 : kDma];
+  if constexpr (kMx) {
+    // lane l takes row s0 + l / kMxLanes, the same part of it in codes and scales: kvo[0] and vvo[0]
+    kvo[0] = (s0 + lane / kMxLanes) * kMxCodeBytes + lane % kMxLanes * (kMxCodeBytes / kMxLanes);
+    vvo[0] = kMxScalesAt + (s0 + lane / kMxLanes) * kMxScaleBytes + lane % kMxLanes * kMxScaleBytes / kMxLanes;
+  } else if constexpr (!kFp8) {
     // LDS-direct load d writes tile rows 16 pw + s0 + 4d + (l >> 4), chunk l & 15: it
     // fetches the source chunk that the row's permutation puts there.
 #pragma unroll
@@ -402,17 +415,45 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
     }
   };
   struct F8Stage {
-    u32x4 x[kF8Loads];
+    u32x4 x[kF8Loads];   // MXFP4: the codes in x[0] (the lower half of it with eight bytes a lane)
+    uint32_t scale;      // MXFP4: their scale byte
   };
   auto f8_load = [&](F8Stage& st, const char* base, int32_t pg, int kb, const uint32_t* vo) {
-    const int bytes = __builtin_amdgcn_readfirstlane(clamp16(hi - (kb + 16 * pw)) * kKeyBytes);
+    const int keys = clamp16(hi - (kb + 16 * pw));
+    const int bytes = __builtin_amdgcn_readfirstlane(kMx ? kRun : keys * kKeyBytes);
     const auto rs = make_rsrc(base + (int64_t)pg * page_stride, bytes);
+    if constexpr (kMx) {   // keys at or past `hi`: past the run, so zeros
+      const bool past = s0 + lane / kMxLanes >= keys;
+      const uint32_t co = past ? (uint32_t)kRun : kvo[0], so = past ? (uint32_t)kRun : vvo[0];
+      if constexpr (kMxLanes == 4) {
+        st.x[0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, co, 0, 0));
+      } else {
+        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rs, co, 0, 0));
+        st.x[0] = u32x4{x[0], x[1], 0u, 0u};
+      }
+      st.scale = __builtin_amdgcn_raw_buffer_load_b8(rs, so, 0, 0);
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < kF8Loads; ++i)
       st.x[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, vo[i], 0, 0));
   };
-  // e4m3 -> bf16 into the permuted rows: 16 codes = bf16 chunks 2f, 2f + 1.
-  auto f8_store = [&](const F8Stage& st, int dst, bool is_k) {
+  // e4m3 -> bf16 into the permuted rows: 16 codes = bf16 chunks 2f, 2f + 1.  MXFP4: 16 or 32 codes, the
+  // chunks from 16 f / kMxLanes on; a NaN block of V (of the tile at key kb) goes in as zeros, and its key
+  // into s_nan: 0 times NaN would reach the columns that do not see the key.
+  auto f8_store = [&](const F8Stage& st, int dst, bool is_k, int kb) {
+    if constexpr (kMx) {
+      const int row = 16 * pw + s0 + lane / kMxLanes, f = lane % kMxLanes;
+      const int sw = is_k ? (row & 15) : ((row & 3) << 2);
+      uint8_t* rp = smem + grp_base + dst + row * kRowBytes;
+      const bool bad = !is_k && st.scale == 255u;
+      if (__builtin_amdgcn_ballot_w64(bad) != 0 && bad) atomicMin(&s_nan[f * kMxScaleBytes / kMxLanes], kb + row);
+      const float scale = mx_scale(bad ? 0u : st.scale);
+#pragma unroll
+      for (int i = 0; i < 16 / kMxLanes; ++i)
+        *reinterpret_cast<u32x4*>(rp + (((16 / kMxLanes * f + i) ^ sw) << 4)) = fp4x8_to_bf16x8(bad ? 0u : st.x[0][i], scale);
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < kF8Loads; ++i) {
       constexpr int kLpr = 8 / kF8Loads;
@@ -653,7 +694,7 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
     constexpr int kJ = decltype(stage)::value;
     const int kcur = kKBase + ((kJ + 1) % kS) * kTileBytes;   // K(t + 1)
     const int vcur = kVBase + kJ * kTileBytes;                // V(t)
-    if constexpr (!kFp8) {
+    if constexpr (!kWiden) {
       // K(t + 1) and V(t) are this wave's copies issued before the last 2 kS - 4 groups of
       // kDma; after the barrier every wave's share of them is in LDS, and every wave has
       // finished iteration t - 1, whose stages the copies below overwrite.
@@ -673,7 +714,7 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
     // The copies into the stages just freed are issued from inside the first step (after its
     // second slot), where the MFMAs already in flight hide their scalar address work.
     auto copies = [&]() {
-      if constexpr (!kFp8) {
+      if constexpr (!kWiden) {
         dma_rows(false, pg_klast, lo + (t + kS - 1) * kKvTile, kVBase + ((kJ + kS - 1) % kS) * kTileBytes);
         dma_rows(true, pg_knext, lo + (t + kS) * kKvTile, kKBase + kJ * kTileBytes);
         pg_klast = pg_knext;
@@ -708,11 +749,11 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
       sc = sn;
       lsum_p = ls;
     }
-    if constexpr (kFp8) {
+    if constexpr (kWiden) {
       // K(t + 2) into stage t % 2 (K(t) there was last read in iteration t - 1), V(t + 1)
       // into stage (t + 1) % 2 (V(t - 1) there likewise)
-      f8_store(kst, kKBase + kJ * kTileBytes, true);
-      f8_store(vst, kVBase + ((kJ + 1) % 2) * kTileBytes, false);
+      f8_store(kst, kKBase + kJ * kTileBytes, true, lo + (t + 2) * kKvTile);
+      f8_store(vst, kVBase + ((kJ + 1) % 2) * kTileBytes, false, lo + (t + 1) * kKvTile);
     }
   };
 
@@ -771,7 +812,7 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
     // 8q/2kv, 256 columns) from 16.0 to 13.1 us, a first 512-token chunk (32q/8kv) from 19.7 to
     // 16.7 us and the fused 8K-prefix layer from 76.9 to 74.6 us, against Q loaded into registers
     // and waited for before the first copy.
-    if constexpr (!kFp8) {
+    if constexpr (!kWiden) {
       constexpr int kEarly = kS / 2;    // tiles copied before Q has been read
       fetch_window(0, 1);
       if (ntiles > 64 - kS - 2) fetch_window(64, 0);
@@ -831,10 +872,10 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
       f8_load(vst, vpb, pg[0], lo, vvo);
       fetch_window(0, 1);
       if (ntiles > 64 - kS - 2) fetch_window(64, 0);
-      f8_store(kst, kKBase, true);
-      f8_store(vst, kVBase, false);
+      f8_store(kst, kKBase, true, lo);
+      f8_store(vst, kVBase, false, lo);
       f8_load(kst, kpb, pg[1], lo + kKvTile, kvo);
-      f8_store(kst, kKBase + kTileBytes, true);
+      f8_store(kst, kKBase + kTileBytes, true, lo + kKvTile);
       pg_klast = pg[1];
       pg_knext = pg[2];
       // the windows, and every load: one still pending in the compiler's count on some path
@@ -890,7 +931,7 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
   }
   if (ntiles > 0) {
     // last tile (t = ntiles - 1): sub-block 2t+1 takes the softmax, P(2t) V, then P(2t+1) V
-    if constexpr (!kFp8) wait_vmcnt<0>();
+    if constexpr (!kWiden) wait_vmcnt<0>();
     else wait_lgkmcnt0();
     __builtin_amdgcn_s_barrier();
     const int vlast = kVBase + (t % kS) * kTileBytes;
@@ -903,6 +944,16 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
     settle(sc, pb, ls);
     pv_acc(pb, vlast + kSubBytes);
   }
+
+  // The factor of dim block db of this column: MXFP4 blocks of V share the MFMA's, and are NaN from the
+  // first key on that made one NaN.
+  float v_nan[4] = {1.f, 1.f, 1.f, 1.f};
+  if constexpr (kMx) {
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+      if (s_nan[db] <= horizon) v_nan[db] = __builtin_nanf("");
+  }
+  auto v_of = [&](int db) { return kMx ? v_nan[db] : v_mul; };
 
   float l_fin = sum_with_partner(l_run);
   float m_fin = l_fin > 0.f ? m_run : -INFINITY;     // -inf: no visible key in this range
@@ -930,8 +981,8 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           *reinterpret_cast<f32x4*>(xs + (col * 32 + ((8 * db + 2 * j + half) ^ (col & 15))) * 4) =
-              f32x4{o[db][4 * j] * v_mul, o[db][4 * j + 1] * v_mul, o[db][4 * j + 2] * v_mul,
-                    o[db][4 * j + 3] * v_mul};
+              f32x4{o[db][4 * j] * v_of(db), o[db][4 * j + 1] * v_of(db), o[db][4 * j + 2] * v_of(db),
+                    o[db][4 * j + 3] * v_of(db)};
       wait_lgkmcnt0();
       __builtin_amdgcn_s_barrier();
       const auto prs = make_rsrc(acc, (int32_t)acc_bytes);
@@ -959,12 +1010,13 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
     }
     if (!valid) return;
     if (ns == 1) {
-      const float inv = v_mul / l_fin;
+      const float inv_l = v_mul / l_fin;
       // the lane pair holds dims 8 j + {0..3} and 8 j + {4..7} of a block: exchanged so that the
       // lower lane stores the eight dims of an even j, the upper one those of the next j
       uint16_t* orow = out + ((int64_t)(row0 + tok) * hq + hq_col) * 128 + 8 * half;
 #pragma unroll
-      for (int db = D0; db < D0 + kDb; ++db)
+      for (int db = D0; db < D0 + kDb; ++db) {
+        const float inv = kMx ? inv_l * v_nan[db] : inv_l;
 #pragma unroll
         for (int j = 0; j < 4; j += 2) {
           u32x2 w[2];   // [first, second word of the lane's four dims of j and of j + 1]
@@ -974,6 +1026,7 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
                                pack_bf16x2(o[db][4 * j + 4 + 2 * e] * inv, o[db][4 * j + 5 + 2 * e] * inv));
           *reinterpret_cast<u32x4*>(orow + 32 * db + 8 * j) = u32x4{w[0][0], w[1][0], w[0][1], w[1][1]};
         }
+      }
       if (lse != nullptr && half == 0 && D0 == 0)
         lse[(int64_t)(row0 + tok) * hq + hq_col] = (m_fin + __log2f(l_fin)) * kLn2;
       return;
@@ -988,8 +1041,8 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
     for (int db = D0; db < D0 + kDb; ++db)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const f32x4 w = {o[db][4 * j] * v_mul, o[db][4 * j + 1] * v_mul, o[db][4 * j + 2] * v_mul,
-                         o[db][4 * j + 3] * v_mul};
+        const f32x4 w = {o[db][4 * j] * v_of(db), o[db][4 * j + 1] * v_of(db), o[db][4 * j + 2] * v_of(db),
+                         o[db][4 * j + 3] * v_of(db)};
         *reinterpret_cast<f32x4*>(arow + 32 * db + 8 * j) = w;
       }
     if (half == 0 && D0 == 0) *reinterpret_cast<f32x4*>(ml + 4 * prow) = f32x4{m_fin, l_fin, 0.f, 0.f};
@@ -1148,12 +1201,12 @@ __global__ __launch_bounds__(256) void split_reduce_kernel(const PlanHeader* __r
 
 }  // namespace
 
-template <bool kFp8, int kColWaves, int kHalves, bool kFused, bool kQ8 = false>
+template <PageKind kKind, int kColWaves, int kHalves, bool kFused, bool kQ8>
 void launch_main_variant(const AttnLaunch& a, hipStream_t stream) {
   const PlanPtrs pv = plan_ptrs(a.workspace, a.dims);
   const int32_t g = a.hq / a.kv.hkv;
   const uint32_t ginv = ((1u << 24) + (uint32_t)g - 1) / (uint32_t)g;
-  attn_main_kernel<kFp8, kColWaves, kHalves, kFused, kQ8><<<(unsigned)a.dims.num_items, kColWaves * kHalves * 64, 0, stream>>>(
+  attn_main_kernel<kKind, kColWaves, kHalves, kFused, kQ8><<<(unsigned)a.dims.num_items, kColWaves * kHalves * 64, 0, stream>>>(
       pv.items, pv.hdr, a.group_by_xcd ? (int32_t)a.dims.num_items : 0, a.kv.max_pages, a.kv.block_tables,
       static_cast<const uint16_t*>(a.q), a.hq, g, ginv, tile_tokens(g, 32 * kColWaves),
       static_cast<uint16_t*>(a.out), a.lse, a.kv.kpool, a.kv.vpool, a.kv.kscale, a.kv.vscale, a.kv.hkv,
@@ -1161,33 +1214,22 @@ void launch_main_variant(const AttnLaunch& a, hipStream_t stream) {
       static_cast<const uint16_t*>(a.vnew), a.total_rows);
 }
 
-template <bool kFp8>
-void launch_main_dtype(const AttnLaunch& a, hipStream_t stream) {
-  constexpr bool kF = false;
-  if (!kFp8 && a.knew != nullptr) {
-    // append fused into this launch (bf16 pages only)
-    if (a.tile_cols == kMaxTileCols) launch_main_variant<false, 8, 1, true>(a, stream);
-    else if (a.key_halves == 2) launch_main_variant<false, 4, 2, true>(a, stream);
-    else launch_main_variant<false, 4, 1, true>(a, stream);
-    return;
-  }
-  if (kFp8 && a.q8) {
-    // Q quantised to e4m3 and S = Q K^T on the fp8 MFMA (e4m3 pages only)
-    if (a.tile_cols == kMaxTileCols) launch_main_variant<true, 8, 1, false, true>(a, stream);
-    else if (a.key_halves == 2) launch_main_variant<true, 4, 2, false, true>(a, stream);
-    else launch_main_variant<true, 4, 1, false, true>(a, stream);
-    return;
-  }
-  if (a.tile_cols == kMaxTileCols) launch_main_variant<kFp8, 8, 1, kF>(a, stream);
-  else if (a.key_halves == 2) launch_main_variant<kFp8, 4, 2, kF>(a, stream);
-  else launch_main_variant<kFp8, 4, 1, kF>(a, stream);
+// The workgroup's layout, by the plan's tiles.
+template <PageKind kKind, bool kFused, bool kQ8>
+void launch_main_layout(const AttnLaunch& a, hipStream_t stream) {
+  if (a.tile_cols == kMaxTileCols) launch_main_variant<kKind, 8, 1, kFused, kQ8>(a, stream);
+  else if (a.key_halves == 2) launch_main_variant<kKind, 4, 2, kFused, kQ8>(a, stream);
+  else launch_main_variant<kKind, 4, 1, kFused, kQ8>(a, stream);
 }
 
 hipError_t launch_attn_main(const AttnLaunch& a, hipStream_t stream) {
   if (a.dims.num_items <= 0) return hipSuccess;
   if (a.tile_cols == kDecodeTileCols) return launch_attn_decode(a, stream);
-  if (a.kv.fp8) launch_main_dtype<true>(a, stream);
-  else launch_main_dtype<false>(a, stream);
+  if (a.kv.kind == kMxfp4Pages) launch_main_layout<kMxfp4Pages, false, false>(a, stream);
+  else if (a.kv.kind == kE4m3Pages && a.q8) launch_main_layout<kE4m3Pages, false, true>(a, stream);   // Q quantised too
+  else if (a.kv.kind == kE4m3Pages) launch_main_layout<kE4m3Pages, false, false>(a, stream);
+  else if (a.knew != nullptr) launch_main_layout<kBf16Pages, true, false>(a, stream);   // the append in this launch
+  else launch_main_layout<kBf16Pages, false, false>(a, stream);
   return hipGetLastError();
 }
 

@@ -55,8 +55,8 @@ constexpr unsigned kOneWorkgroupLds = 84 * 1024;   // above half of a CU's 160 K
 constexpr int kVRow = kHeadDim * 2;             // bf16 key row in LDS
 // Pages of one wave's tile.  Two tiles are held in registers (one being computed, one in
 // flight), 8 KiB of K and V each way per tile either way, so that two workgroups fit a CU.
-template <bool kFp8>
-constexpr int kTilePages = kFp8 ? 4 : 2;
+template <PageKind kKind>
+constexpr int kTilePages = kKind == kBf16Pages ? 2 : 4;
 constexpr float kDLn2 = 0.6931471805599453f;
 constexpr float kDOverflow = 18446744073709551616.0f;   // 2^64
 constexpr int32_t kDRsrcWord3 = 0x00020000;
@@ -77,13 +77,20 @@ __device__ inline float dmerge_weight(float m_s, float mstar) {
 // One tile's K (A operands) and V (rows on their way to LDS), in registers.
 // fp8: the codes as loaded; they are widened when they are used, so that a load is not waited
 // for where it is issued.
-template <bool kFp8>
+template <PageKind kKind>
 struct TileRegs {
-  u32x4 k[kTilePages<kFp8>][kFp8 ? 2 : 4];   // [page][bf16: k-step; fp8: pair of k-steps]
-  u32x4 v[kTilePages<kFp8>][kFp8 ? 2 : 4];   // [page][row group of 4 (bf16) or 8 (fp8) keys]
+  static constexpr int kLoads = kKind == kBf16Pages ? 4 : kKind == kE4m3Pages ? 2 : 1;   // 1 KiB each of a page
+  u32x4 k[kTilePages<kKind>][kLoads];   // [page][bf16: k-step; fp8: pair of k-steps; MXFP4: a block of dims]
+  u32x4 v[kTilePages<kKind>][kLoads];   // [page][row group of 4 (bf16), 8 (fp8) or 16 (MXFP4) keys]
+};
+template <>
+struct TileRegs<kMxfp4Pages> {
+  static constexpr int kLoads = 1;
+  u32x4 k[kTilePages<kMxfp4Pages>][1], v[kTilePages<kMxfp4Pages>][1];
+  uint32_t ks[kTilePages<kMxfp4Pages>], vs[kTilePages<kMxfp4Pages>];   // their scale bytes
 };
 
-template <bool kFp8>
+template <PageKind kKind>
 __global__ __launch_bounds__(kDecodeWaves * 64, 2) void attn_decode_kernel(
     const ItemRec* __restrict__ items, const PlanHeader* __restrict__ hdr, int32_t xcd_items,
     int32_t max_pages, const int32_t* __restrict__ block_tables, const uint16_t* __restrict__ q, int32_t hq,
@@ -91,12 +98,14 @@ __global__ __launch_bounds__(kDecodeWaves * 64, 2) void attn_decode_kernel(
     uint16_t* __restrict__ out, float* __restrict__ lse, const void* __restrict__ kpool,
     const void* __restrict__ vpool, const float* __restrict__ kscale, const float* __restrict__ vscale, int32_t hkv,
     float scale_log2, float* __restrict__ partials, int64_t total_rows) {
-  constexpr int kPages = kTilePages<kFp8>;
+  constexpr bool kFp8 = kKind == kE4m3Pages, kMx = kKind == kMxfp4Pages;
+  constexpr int kPages = kTilePages<kKind>, kLoads = TileRegs<kKind>::kLoads;
   constexpr int kDTile = 16 * kPages;             // keys per tile
   constexpr int kVWaveBytes = kDTile * kVRow;     // one wave's V tile as bf16 rows
   constexpr int kMergeBytes = kDecodeWaves * 64 * (8 * 16 + 8);   // (O, m, l) of the waves at the end
   constexpr int kSmem = kDecodeWaves * kVWaveBytes > kMergeBytes ? kDecodeWaves * kVWaveBytes : kMergeBytes;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kSmem];
+  __shared__ int32_t s_nan[kMx ? kMxScaleBytes : 1];   // MXFP4: the first key whose V is NaN, of each 32 dims
 
   const int w_item = xcd_items != 0 ? xcd_logical(blockIdx.x, xcd_items) : (int)blockIdx.x;
   const ItemRec it = items[w_item];
@@ -129,8 +138,8 @@ __global__ __launch_bounds__(kDecodeWaves * 64, 2) void attn_decode_kernel(
     v_mul = vscale[g];
   }
 
-  constexpr int kRun = kFp8 ? 16 * kHeadDim : 16 * kHeadDim * 2;   // one (page, kv head)
-  constexpr int kKeyBytes = kRun / 16;
+  constexpr int kRun = run_bytes(kKind);   // one (page, kv head)
+  constexpr int kKeyBytes = kMx ? kMxCodeBytes : kRun / 16;
   const char* kpb = static_cast<const char*>(kpool) + (int64_t)g * kRun;
   const char* vpb = static_cast<const char*>(vpool) + (int64_t)g * kRun;
   const int64_t page_stride = (int64_t)hkv * kRun;
@@ -149,16 +158,21 @@ __global__ __launch_bounds__(kDecodeWaves * 64, 2) void attn_decode_kernel(
   };
   int32_t pg0 = load_pages(0);   // before the Q loads, so that the first tile does not wait for them
   int32_t pg1 = load_pages(1);
+  if constexpr (kMx) {
+    if (threadIdx.x < kMxScaleBytes) s_nan[threadIdx.x] = 0x7FFFFFFF;
+    __syncthreads();
+  }
 
   // Q^T (B operand) of k-step ks: lane (j, q) holds eight dims of Q[column j], the same ones that
   // the K operand holds there.  bf16: 32 ks + 8 q.  fp8: 64 (ks / 2) + 16 q + 8 (ks % 2), so that
-  // one 16-byte load of K's codes serves two k-steps.
+  // one 16-byte load of K's codes serves two k-steps.  MXFP4: 32 q + 8 ks, so that a lane's 16 bytes of
+  // codes are one block of its key, with one scale.
   bf16x8 qf[4];
   {
     const uint16_t* qrow = q + ((int64_t)(row0 + (valid ? tok : 0)) * hq + (valid ? hq_col : 0)) * kHeadDim;
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
-      const int dim = kFp8 ? 64 * (ks >> 1) + 16 * qg + 8 * (ks & 1) : 32 * ks + 8 * qg;
+      const int dim = kMx ? 32 * qg + 8 * ks : kFp8 ? 64 * (ks >> 1) + 16 * qg + 8 * (ks & 1) : 32 * ks + 8 * qg;
       const u32x4 x = valid ? *reinterpret_cast<const u32x4*>(qrow + dim) : u32x4{0, 0, 0, 0};
       qf[ks] = __builtin_bit_cast(bf16x8, x);
     }
@@ -166,22 +180,31 @@ __global__ __launch_bounds__(kDecodeWaves * 64, 2) void attn_decode_kernel(
 
   // Issue the loads of my k-th tile (pages in lanes 0 .. kPages - 1 of pg).  Keys at or past `hi`
   // (and every key of a tile past my last) read as zeros.
-  auto issue = [&](int k, int32_t pg, TileRegs<kFp8>& t) {
+  auto issue = [&](int k, int32_t pg, TileRegs<kKind>& t) {
     const int key0 = lo + (wave + kDecodeWaves * k) * kDTile;
 #pragma unroll
     for (int b = 0; b < kPages; ++b) {
       const int64_t page = __builtin_amdgcn_readlane(pg, b);
       // uniform by construction; readfirstlane lets the compiler see it (a descriptor it
       // must treat as per-lane costs a loop around every load)
-      const int bytes = __builtin_amdgcn_readfirstlane(k < my_n ? clamp16i(hi - (key0 + 16 * b)) * kKeyBytes : 0);
+      const int keys = k < my_n ? clamp16i(hi - (key0 + 16 * b)) : 0;
+      const int bytes = __builtin_amdgcn_readfirstlane(kMx ? kRun : keys * kKeyBytes);
       const auto kr = page_rsrc(kpb + page * page_stride, bytes);
       const auto vr = page_rsrc(vpb + page * page_stride, bytes);
+      if constexpr (kMx) {   // K: key j, block q.  V: key l / 4, block l % 4.  Keys at or past `hi`: past the run
+        const int ko = j < keys ? j : kRun, vo = lane >> 2 < keys ? lane >> 2 : kRun;
+        t.k[b][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kr, ko * kMxCodeBytes + 16 * qg, 0, 0));
+        t.v[b][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vr, vo * kMxCodeBytes + 16 * (lane & 3), 0, 0));
+        t.ks[b] = __builtin_amdgcn_raw_buffer_load_b8(kr, kMxScalesAt + ko * kMxScaleBytes + qg, 0, 0);
+        t.vs[b] = __builtin_amdgcn_raw_buffer_load_b8(vr, kMxScalesAt + vo * kMxScaleBytes + (lane & 3), 0, 0);
+        continue;
+      }
 #pragma unroll
-      for (int i = 0; i < (kFp8 ? 2 : 4); ++i)   // key j, 64 bytes of it over the four q
+      for (int i = 0; i < (kMx ? 0 : kLoads); ++i)   // key j, 64 bytes of it over the four q
         t.k[b][i] =
             __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kr, j * kKeyBytes + 64 * i + 16 * qg, 0, 0));
 #pragma unroll
-      for (int i = 0; i < (kFp8 ? 2 : 4); ++i) {
+      for (int i = 0; i < (kMx ? 0 : kLoads); ++i) {
         // bf16: LDS row 16 b + 4 i + q, position j holds source chunk j ^ 2 (row & 7);
         // fp8: key slot 8 i + l / 8, dims 16 (l % 8) .. + 15
         const int slot = kFp8 ? 8 * i + (lane >> 3) : 4 * i + qg;
@@ -191,11 +214,26 @@ __global__ __launch_bounds__(kDecodeWaves * 64, 2) void attn_decode_kernel(
     }
   };
   // V rows of a tile from registers into this wave's LDS (key-major, permuted chunks).
-  auto stage_v = [&](const TileRegs<kFp8>& t) {
+  // A NaN block of MXFP4 V goes in as zeros, and its key into s_nan: 0 times NaN would reach the columns
+  // that do not see the key.
+  auto stage_v = [&](int k, const TileRegs<kKind>& t) {
+    if constexpr (kMx) {
+#pragma unroll
+      for (int b = 0; b < kPages; ++b) {
+        const int row = 16 * b + (lane >> 2), c0 = 4 * (lane & 3), sw = 2 * (row & 7);
+        const bool bad = t.vs[b] == 255u;
+        if (__builtin_amdgcn_ballot_w64(bad) != 0 && bad) atomicMin(&s_nan[lane & 3], lo + (wave + kDecodeWaves * k) * kDTile + row);
+        const float scale = mx_scale(bad ? 0u : t.vs[b]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<u32x4*>(vbuf + row * kVRow + 16 * ((c0 + i) ^ sw)) = fp4x8_to_bf16x8(bad ? 0u : t.v[b][0][i], scale);
+      }
+      return;
+    }
 #pragma unroll
     for (int b = 0; b < kPages; ++b)
 #pragma unroll
-      for (int i = 0; i < (kFp8 ? 2 : 4); ++i) {
+      for (int i = 0; i < (kMx ? 0 : kLoads); ++i) {
         if constexpr (!kFp8) {
           *reinterpret_cast<u32x4*>(vbuf + (16 * b + 4 * i + qg) * kVRow + 16 * j) = t.v[b][i];
         } else {
@@ -209,8 +247,10 @@ __global__ __launch_bounds__(kDecodeWaves * 64, 2) void attn_decode_kernel(
       }
   };
   // A operand of S^T = K Q^T: k-step ks of page b.
-  auto k_frag = [&](const TileRegs<kFp8>& t, int b, int ks) {
-    if constexpr (!kFp8) {
+  auto k_frag = [&](const TileRegs<kKind>& t, int b, int ks) {
+    if constexpr (kMx) {
+      return __builtin_bit_cast(bf16x8, fp4x8_to_bf16x8(t.k[b][0][ks], mx_scale(t.ks[b])));
+    } else if constexpr (!kFp8) {
       return __builtin_bit_cast(bf16x8, t.k[b][ks]);
     } else {
       const u32x4 c = t.k[b][ks >> 1];
@@ -239,7 +279,7 @@ __global__ __launch_bounds__(kDecodeWaves * 64, 2) void attn_decode_kernel(
   float m_run = 0.f, l_run = 0.f;
 
   // One tile: scores, mask, probabilities (settling the reference), P V.
-  auto compute = [&](int k, const TileRegs<kFp8>& t) {
+  auto compute = [&](int k, const TileRegs<kKind>& t) {
     const int key0 = lo + (wave + kDecodeWaves * k) * kDTile;
     f32x4 s[kPages];
 #pragma unroll
@@ -273,7 +313,7 @@ __global__ __launch_bounds__(kDecodeWaves * 64, 2) void attn_decode_kernel(
     if (k == 0) {   // the reference: this column's exact max over the wave's first 64 keys
       const float t0 = tile_max();
       m_run = t0 == -INFINITY ? 0.f : t0;
-    } else if (!kFp8 && k == 1) {   // the other 32 of them
+    } else if (kKind == kBf16Pages && k == 1) {   // the other 32 of them
       raise(fmaxf(m_run, tile_max()));
     }
     uint32_t pk[2 * kPages];
@@ -309,14 +349,14 @@ __global__ __launch_bounds__(kDecodeWaves * 64, 2) void attn_decode_kernel(
   };
 
   if (my_n > 0) {
-    TileRegs<kFp8> ta, tb;
+    TileRegs<kKind> ta, tb;
     issue(0, pg0, ta);
     int32_t pg2 = load_pages(2);
     // step k: issue tile k+1 (pages known), stage V(k), compute tile k
-    auto step = [&](int k, TileRegs<kFp8>& cur, TileRegs<kFp8>& nxt) {
+    auto step = [&](int k, TileRegs<kKind>& cur, TileRegs<kKind>& nxt) {
       const int32_t p3 = load_pages(k + 3);
       issue(k + 1, pg1, nxt);   // past my last tile: zero-size loads, never used
-      stage_v(cur);
+      stage_v(k, cur);
       compute(k, cur);
       pg1 = pg2;
       pg2 = p3;
@@ -358,6 +398,9 @@ __global__ __launch_bounds__(kDecodeWaves * 64, 2) void attn_decode_kernel(
   float* acc = partials + it.part_off;
   float* mlp = acc + (int64_t)ns * C * hq * kHeadDim;
   const int64_t prow = ((int64_t)it.s * C + tok) * hq + hq_col;
+  if constexpr (kMx) {   // this wave's dims are one block
+    if (s_nan[wave] <= horizon) v_mul = __builtin_nanf("");
+  }
   const float inv = v_mul / lstar;
 #pragma unroll
   for (int d = 0; d < 2; ++d) {
@@ -384,8 +427,8 @@ __global__ __launch_bounds__(kDecodeWaves * 64, 2) void attn_decode_kernel(
 
 }  // namespace
 
-template <bool kFp8>
-void launch_decode_dtype(const AttnLaunch& a, hipStream_t stream) {
+template <PageKind kKind>
+void launch_decode_kind(const AttnLaunch& a, hipStream_t stream) {
   // One workgroup a CU, by asking for more LDS than two could share, except for e4m3 items of
   // near-equal length.  With all the unequal items of a batch resident at once, each gets the same
   // share of the memory's rate and the longest end alone; one a CU, they start longest first as
@@ -396,11 +439,11 @@ void launch_decode_dtype(const AttnLaunch& a, hipStream_t stream) {
   // which latency bounds, would gain from two: 433 rows of 372 keys (16q/16kv) 257 us with one, 233 with
   // two, 922 of up to 30 (32q/8kv) 86 and 51.  Not used: the line between these and the long unequal
   // ones, by length and by inequality, is not measured.
-  const unsigned pad = kFp8 && a.uniform ? 0 : kOneWorkgroupLds - (kFp8 ? 64u : 34u) * 1024;
+  const unsigned pad = kKind != kBf16Pages && a.uniform ? 0 : kOneWorkgroupLds - (kKind != kBf16Pages ? 64u : 34u) * 1024;
   const PlanPtrs pv = plan_ptrs(a.workspace, a.dims);
   const int32_t g = a.hq / a.kv.hkv;
   const uint32_t ginv = ((1u << 24) + (uint32_t)g - 1) / (uint32_t)g;
-  attn_decode_kernel<kFp8><<<(unsigned)a.dims.num_items, kDecodeWaves * 64, pad, stream>>>(
+  attn_decode_kernel<kKind><<<(unsigned)a.dims.num_items, kDecodeWaves * 64, pad, stream>>>(
       pv.items, pv.hdr, a.group_by_xcd ? (int32_t)a.dims.num_items : 0, a.kv.max_pages, a.kv.block_tables,
       static_cast<const uint16_t*>(a.q), a.hq, g, ginv, tile_tokens(g, kDecodeTileCols),
       static_cast<uint16_t*>(a.out), a.lse, a.kv.kpool, a.kv.vpool, a.kv.kscale, a.kv.vscale, a.kv.hkv,
@@ -409,8 +452,7 @@ void launch_decode_dtype(const AttnLaunch& a, hipStream_t stream) {
 
 hipError_t launch_attn_decode(const AttnLaunch& a, hipStream_t stream) {
   if (a.dims.num_items <= 0) return hipSuccess;
-  if (a.kv.fp8) launch_decode_dtype<true>(a, stream);
-  else launch_decode_dtype<false>(a, stream);
+  with_kind(a.kv.kind, [&](auto kind) { launch_decode_kind<decltype(kind)::value>(a, stream); });
   return hipGetLastError();
 }
 

@@ -18,7 +18,7 @@ namespace s2l {
 
 namespace {
 
-template <bool kFp8>
+template <PageKind kKind>
 __global__ __launch_bounds__(256) void kv_append_kernel(
     const int32_t* __restrict__ prefix_lens, const int32_t* __restrict__ chunk_lens,
     const int32_t* __restrict__ cu_chunk, const int32_t* __restrict__ block_tables, int32_t max_pages, int32_t hkv,
@@ -36,12 +36,27 @@ __global__ __launch_bounds__(256) void kv_append_kernel(
   if (pos < P || pos >= P + C) return;
   const int64_t page = block_tables[(int64_t)r * max_pages + lp];
   const int64_t src = ((int64_t)(row0 + pos - P) * hkv + h) * 128 + c * 8;
-  const int64_t dst = ((page * hkv + h) * 16 + slot) * 128 + c * 8;
+  const int64_t run = page * hkv + h;
+  const int64_t dst = (run * 16 + slot) * 128 + c * 8;
   const u32x4 kx = *reinterpret_cast<const u32x4*>(knew + src);
   const u32x4 vx = *reinterpret_cast<const u32x4*>(vnew + src);
-  if constexpr (!kFp8) {
+  if constexpr (kKind == kBf16Pages) {
     *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(kpool) + dst) = kx;
     *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(vpool) + dst) = vx;
+  } else if constexpr (kKind == kMxfp4Pages) {
+    // four lanes hold a block of 32 dims (a row's 16 lanes are all here or none)
+    uint32_t m = max_magnitude(kx) | max_magnitude(vx) << 16;
+    m = max_u16x2(m, lane_xor1(m));
+    m = max_u16x2(m, lane_xor2(m));
+    const uint32_t kb = mx_scale_byte(m & 0xFFFFu), vb = mx_scale_byte(m >> 16);
+    uint8_t* kr = static_cast<uint8_t*>(kpool) + run * kMxRunBytes;
+    uint8_t* vr = static_cast<uint8_t*>(vpool) + run * kMxRunBytes;
+    *reinterpret_cast<uint32_t*>(kr + slot * kMxCodeBytes + 4 * c) = mx_encode8(kx, kb);
+    *reinterpret_cast<uint32_t*>(vr + slot * kMxCodeBytes + 4 * c) = mx_encode8(vx, vb);
+    if ((c & 3) == 0) {
+      kr[kMxScalesAt + slot * kMxScaleBytes + (c >> 2)] = (uint8_t)kb;
+      vr[kMxScalesAt + slot * kMxScaleBytes + (c >> 2)] = (uint8_t)vb;
+    }
   } else {
     // code = e4m3(fp32(x) * fp32(1/scale[h])), RNE, saturated
     const float ki = __fdiv_rn(1.0f, kscale[h]);
@@ -83,6 +98,89 @@ __global__ __launch_bounds__(256) void kv_gather_kernel(
     const int64_t dst = (((row0 + pos) * hkv + h) * 128) * kEB + c * 16;
     *reinterpret_cast<u32x4*>(ko + dst) = *reinterpret_cast<const u32x4*>(kp + src);
     *reinterpret_cast<u32x4*>(vo + dst) = *reinterpret_cast<const u32x4*>(vp + src);
+  }
+}
+
+// Gather of MXFP4 rows: 16 dwords of codes and the dword of scales, row by row and head by head.
+__global__ __launch_bounds__(256) void kv_gather_mxfp4_kernel(
+    const void* __restrict__ kpool, const void* __restrict__ vpool, void* __restrict__ kout,
+    void* __restrict__ vout, const int32_t* __restrict__ prefix_lens, const int32_t* __restrict__ chunk_lens,
+    const int32_t* __restrict__ cu_out, const int32_t* __restrict__ block_tables, int32_t max_pages,
+    int32_t hkv, int32_t include_chunk) {
+  const int r = blockIdx.y;
+  const int n = prefix_lens[r] + (include_chunk ? chunk_lens[r] : 0);
+  const int lp = blockIdx.x;
+  if (lp * 16 >= n) return;
+  const int64_t page = block_tables[(int64_t)r * max_pages + lp];
+  const int64_t row0 = cu_out[r];
+  constexpr int kWords = (kMxCodeBytes + kMxScaleBytes) / 4;   // of a row of a head
+  const uint32_t* kp = static_cast<const uint32_t*>(kpool);
+  const uint32_t* vp = static_cast<const uint32_t*>(vpool);
+  uint32_t* ko = static_cast<uint32_t*>(kout);
+  uint32_t* vo = static_cast<uint32_t*>(vout);
+  for (int u = threadIdx.x; u < hkv * 16 * kWords; u += 256) {
+    const int w = u % kWords, h = u / kWords % hkv, slot = u / (kWords * hkv);
+    const int pos = lp * 16 + slot;
+    if (pos >= n) continue;
+    const int64_t src = (page * hkv + h) * (kMxRunBytes / 4) + (w < kMxCodeBytes / 4 ? slot * (kMxCodeBytes / 4) + w : kMxScalesAt / 4 + slot);
+    const int64_t dst = ((row0 + pos) * hkv + h) * kWords + w;
+    ko[dst] = kp[src];
+    vo[dst] = vp[src];
+  }
+}
+
+// Values: row cu_out[r] + i receives position begin + i of request r as bf16.  Workgroup (page of the
+// part, request); thread by thread eight dims of a row of a head, 16 bytes out, in the order of the
+// output rows.  Bound by writing them.
+template <PageKind kKind>
+__global__ __launch_bounds__(256) void kv_read_kernel(
+    const void* __restrict__ kpool, const void* __restrict__ vpool, const float* __restrict__ kscale,
+    const float* __restrict__ vscale, uint16_t* __restrict__ kout, uint16_t* __restrict__ vout,
+    const int32_t* __restrict__ prefix_lens, const int32_t* __restrict__ chunk_lens,
+    const int32_t* __restrict__ cu_out, const int32_t* __restrict__ block_tables, int32_t max_pages,
+    int32_t hkv, int32_t skip_prefix, int32_t with_chunk, int64_t out_rows) {
+  const int r = blockIdx.y;
+  const int P = prefix_lens[r], C = chunk_lens[r];
+  const int64_t row0 = cu_out[r];
+  const int begin = skip_prefix ? P : 0, end = with_chunk ? P + C : P;
+  const int lp = (begin >> 4) + (int)blockIdx.x;
+  if (lp * 16 >= end) return;
+  const int64_t page = block_tables[(int64_t)r * max_pages + lp];
+  for (int u = threadIdx.x; u < hkv * 256; u += 256) {
+    const int c = u & 15, h = (u >> 4) % hkv, slot = (u >> 4) / hkv;
+    const int pos = lp * 16 + slot;
+    const int64_t row = row0 + pos - begin;
+    if (pos < begin || pos >= end || row < 0 || row >= out_rows) continue;
+    const int64_t run = page * hkv + h;
+    u32x4 k, v;
+    if constexpr (kKind == kMxfp4Pages) {
+      const uint8_t* kr = static_cast<const uint8_t*>(kpool) + run * kMxRunBytes;
+      const uint8_t* vr = static_cast<const uint8_t*>(vpool) + run * kMxRunBytes;
+      const int at = slot * kMxCodeBytes + 4 * c, sc = kMxScalesAt + slot * kMxScaleBytes + (c >> 2);
+      k = fp4x8_to_bf16x8(*reinterpret_cast<const uint32_t*>(kr + at), mx_scale(kr[sc]));
+      v = fp4x8_to_bf16x8(*reinterpret_cast<const uint32_t*>(vr + at), mx_scale(vr[sc]));
+    } else if constexpr (kKind == kE4m3Pages) {
+      const int64_t at = (run * 16 + slot) * 128 + 8 * c;
+      auto value = [](const void* pool, int64_t at, float scale) {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(pool) + at);
+        u32x4 y;
+        for (int i = 0; i < 2; ++i) {
+          const u32x2 w = fp8x4_to_bf16x4(x[i]);
+          y[2 * i] = pack_bf16x2(bf16lo(w[0]) * scale, bf16hi(w[0]) * scale);
+          y[2 * i + 1] = pack_bf16x2(bf16lo(w[1]) * scale, bf16hi(w[1]) * scale);
+        }
+        return y;
+      };
+      k = value(kpool, at, kscale[h]);
+      v = value(vpool, at, vscale[h]);
+    } else {
+      const int64_t at = (run * 16 + slot) * 128 + 8 * c;
+      k = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(kpool) + at);
+      v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(vpool) + at);
+    }
+    const int64_t dst = (row * hkv + h) * 128 + 8 * c;
+    *reinterpret_cast<u32x4*>(kout + dst) = k;
+    *reinterpret_cast<u32x4*>(vout + dst) = v;
   }
 }
 
@@ -160,15 +258,13 @@ hipError_t launch_kv_append(const KvLaunch& a, const void* knew, const void* vne
                             hipStream_t stream) {
   if (a.num_reqs == 0 || max_pages_touched == 0) return hipSuccess;
   dim3 grid(max_pages_touched, a.hkv, a.num_reqs);
-  if (a.fp8) {
-    kv_append_kernel<true><<<grid, 256, 0, stream>>>(
-        a.prefix_lens, a.chunk_lens, a.cu_chunk, a.block_tables, a.max_pages, a.hkv,
-        static_cast<const uint16_t*>(knew), static_cast<const uint16_t*>(vnew), a.kpool, a.vpool, a.kscale, a.vscale);
-  } else {
-    kv_append_kernel<false><<<grid, 256, 0, stream>>>(
-        a.prefix_lens, a.chunk_lens, a.cu_chunk, a.block_tables, a.max_pages, a.hkv,
-        static_cast<const uint16_t*>(knew), static_cast<const uint16_t*>(vnew), a.kpool, a.vpool, nullptr, nullptr);
-  }
+  auto launch = [&](auto kind) {
+    constexpr PageKind kKind = decltype(kind)::value;
+    kv_append_kernel<kKind><<<grid, 256, 0, stream>>>(a.prefix_lens, a.chunk_lens, a.cu_chunk, a.block_tables, a.max_pages,
+                                                      a.hkv, static_cast<const uint16_t*>(knew),
+                                                      static_cast<const uint16_t*>(vnew), a.kpool, a.vpool, a.kscale, a.vscale);
+  };
+  with_kind(a.kind, launch);
   return hipGetLastError();
 }
 
@@ -176,13 +272,23 @@ hipError_t launch_kv_gather(const KvLaunch& a, int32_t include_chunk, const int3
                             void* vout, int32_t max_pages_read, hipStream_t stream) {
   if (a.num_reqs == 0 || max_pages_read == 0) return hipSuccess;
   dim3 grid(max_pages_read, a.num_reqs);
-  if (a.fp8) {
-    kv_gather_kernel<1><<<grid, 256, 0, stream>>>(a.kpool, a.vpool, kout, vout, a.prefix_lens, a.chunk_lens,
-                                                  cu_out, a.block_tables, a.max_pages, a.hkv, include_chunk);
-  } else {
-    kv_gather_kernel<2><<<grid, 256, 0, stream>>>(a.kpool, a.vpool, kout, vout, a.prefix_lens, a.chunk_lens,
-                                                  cu_out, a.block_tables, a.max_pages, a.hkv, include_chunk);
-  }
+  const auto kernel = a.kind == kMxfp4Pages ? kv_gather_mxfp4_kernel : a.kind == kE4m3Pages ? kv_gather_kernel<1> : kv_gather_kernel<2>;
+  kernel<<<grid, 256, 0, stream>>>(a.kpool, a.vpool, kout, vout, a.prefix_lens, a.chunk_lens, cu_out, a.block_tables,
+                                   a.max_pages, a.hkv, include_chunk);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_read(const KvLaunch& a, bool skip_prefix, bool with_chunk, const int32_t* cu_out, void* kout, void* vout,
+                          int64_t out_rows, int32_t max_pages_read, hipStream_t stream) {
+  if (a.num_reqs == 0 || max_pages_read == 0 || out_rows == 0) return hipSuccess;
+  dim3 grid(max_pages_read, a.num_reqs);
+  auto launch = [&](auto kind) {
+    constexpr PageKind kKind = decltype(kind)::value;
+    kv_read_kernel<kKind><<<grid, 256, 0, stream>>>(a.kpool, a.vpool, a.kscale, a.vscale, static_cast<uint16_t*>(kout),
+                                                    static_cast<uint16_t*>(vout), a.prefix_lens, a.chunk_lens, cu_out,
+                                                    a.block_tables, a.max_pages, a.hkv, skip_prefix, with_chunk, out_rows);
+  };
+  with_kind(a.kind, launch);
   return hipGetLastError();
 }
 

@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "linear_plan.h"
 #include "plan_rules.h"
 
@@ -21,13 +23,24 @@ struct KvLaunch {           // device pointers of one layer's cache and one batc
   int32_t hkv;
   int32_t num_reqs;
   int32_t num_pages;
-  bool fp8;
+  PageKind kind;
 };
+
+// f(std::integral_constant<PageKind, kind>): the instantiation that a cache's pages need.
+template <typename F>
+inline void with_kind(PageKind kind, F&& f) {
+  if (kind == kMxfp4Pages) f(std::integral_constant<PageKind, kMxfp4Pages>{});
+  else if (kind == kE4m3Pages) f(std::integral_constant<PageKind, kE4m3Pages>{});
+  else f(std::integral_constant<PageKind, kBf16Pages>{});
+}
 
 hipError_t launch_kv_append(const KvLaunch& a, const void* knew, const void* vnew, int32_t max_pages_touched,
                             hipStream_t stream);
 hipError_t launch_kv_gather(const KvLaunch& a, int32_t include_chunk, const int32_t* cu_out, void* kout,
                             void* vout, int32_t max_pages_read, hipStream_t stream);
+// Values of positions [P if skip_prefix, P + C if with_chunk else P) as bf16 rows, out_rows of them.
+hipError_t launch_kv_read(const KvLaunch& a, bool skip_prefix, bool with_chunk, const int32_t* cu_out, void* kout, void* vout,
+                          int64_t out_rows, int32_t max_pages_read, hipStream_t stream);
 // Counts used block-table entries outside [0, num_pages) into counts[0] and the largest
 // offending request + 1 into counts[1] (both cleared first).
 hipError_t launch_check_tables(const KvLaunch& a, int32_t max_pages_used, int32_t* counts, hipStream_t stream);
@@ -94,7 +107,7 @@ struct ReduceLaunch {
 };
 hipError_t launch_split_reduce(const ReduceLaunch& a, hipStream_t stream);
 
-struct RopeLaunch {          // rotation of rows, and their append (rope.hip)
+struct RopeLaunch {          // rotation of rows, normed or not, and their append (rope.hip)
   const uint16_t *q, *k, *v;
   uint16_t *q_out, *k_out;   // k_out without pools, v with them only
   int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride;   // elements
@@ -104,7 +117,10 @@ struct RopeLaunch {          // rotation of rows, and their append (rope.hip)
   uint64_t pair_axes[2];     // two bits a pair
   int32_t rot_dim, num_axes;
   float scale;
-  bool adjacent, fp8;
+  bool adjacent, norm, norm_fp32;
+  PageKind kind;
+  const void *q_weight, *k_weight;   // null: factors of 1
+  float eps, offset;
   const int32_t *prefix_lens, *cu_chunk, *block_tables;
   int32_t max_pages, num_reqs, hq, hkv, total_rows;
   void *k_pool, *v_pool;     // null: no append

@@ -21,6 +21,17 @@ namespace s2l {
 
 constexpr int kHeadDim = 128;
 constexpr int kPageSize = 16;
+// What the pools hold.  One (page, kv head) is a run of 16 rows: bf16 elements, e4m3 codes, or MXFP4:
+// 16 rows of E2M1 codes, two a byte, then of each row a scale byte for each 32 dims.
+enum PageKind : int { kBf16Pages = 0, kE4m3Pages = 1, kMxfp4Pages = 2 };
+constexpr int kMxBlock = 32;                                      // dims that share a scale
+constexpr int kMxCodeBytes = kHeadDim / 2;                        // of one row
+constexpr int kMxScaleBytes = kHeadDim / kMxBlock;
+constexpr int kMxScalesAt = kPageSize * kMxCodeBytes;             // in a run
+constexpr int kMxRunBytes = kMxScalesAt + kPageSize * kMxScaleBytes;
+S2L_HD constexpr int run_bytes(int kind) {
+  return kind == kMxfp4Pages ? kMxRunBytes : kPageSize * kHeadDim * (kind == kE4m3Pages ? 1 : 2);
+}
 constexpr int kMinTileCols = 128;   // packed (token, head) columns per work item: 4 waves x 32
 constexpr int kMaxTileCols = 256;   //   or 8 waves x 32
 constexpr int kDecodeTileCols = 16; // decode-shaped items: 16 columns, four waves over the keys

@@ -1,4 +1,4 @@
-// Argument marshalling of the per-step calls (append, plan, attention, merge, rotation, linear attention) for the Python
+// Argument marshalling of the per-step calls (append, plan, attention, merge, rotation, linear attention, read-back) for the Python
 // package, through the CPython API: a step of small sizes is bound by what the host does between
 // its launches, and building the argument structs through ctypes took 9 of the 14 us of a call.
 // Every pointer, length and stream is read from the objects on each call; nothing is kept.
@@ -27,14 +27,17 @@ struct Entry {
   decltype(&s2l_rope_qk) rope_qk;
   decltype(&s2l_rope_kv_append) rope_append;
   decltype(&s2l_linear_attn) linear;
+  decltype(&s2l_norm_rope_qk) norm_rope_qk;
+  decltype(&s2l_norm_rope_kv_append) norm_rope_append;
+  decltype(&s2l_kv_read) read;
 } lib;
 
 PyObject *tensor_type, *cache_type, *batch_type, *opts_type, *info_type, *stream_type, *bf16, *f32, *u8, *is_initialized, *get_device, *get_stream,
-    *rope_type, *state_type, *i32;
+    *rope_type, *state_type, *i32, *norm_type;
 PyObject *s_dtype, *s_data_ptr, *s_is_contiguous, *s_shape, *s_numel, *s_k_pages, *s_v_pages, *s_k_scale, *s_v_scale,
     *s_fp8, *s_prefix_host, *s_chunk_host, *s_tables_host, *s_prefix_lens, *s_chunk_lens, *s_cu_chunk, *s_block_tables,
     *s_cuda_stream, *s_stride, *s_get_device, *s_inv_freq, *s_positions, *s_pair_axis, *s_adjacent, *s_scale, *s_states, *s_log_decay,
-    *s_slot_in, *s_slot_out;
+    *s_slot_in, *s_slot_out, *s_mxfp4, *s_q_weight, *s_k_weight, *s_eps, *s_offset;
 
 // Owned reference, released at the end of the scope.
 struct Ref {
@@ -122,13 +125,18 @@ bool cache_arg(PyObject* o, s2l_kv_cache* c) {
   *c = s2l_kv_cache{};
   const Ref k(PyObject_GetAttr(o, s_k_pages)), fp8(PyObject_GetAttr(o, s_fp8));
   if (!k || !fp8 || (PyObject*)Py_TYPE(k.o) != tensor_type || (fp8.o != Py_True && fp8.o != Py_False)) return false;
-  const Ref shape(PyObject_GetAttr(k.o, s_shape));
-  if (!shape || !PyTuple_Check(shape.o) || PyTuple_GET_SIZE(shape.o) != 4) return false;
+  const Ref shape(PyObject_GetAttr(k.o, s_shape)), mx(PyObject_GetAttr(o, s_mxfp4));
+  if (!shape || !mx || !PyTuple_Check(shape.o) || PyTuple_GET_SIZE(shape.o) != (mx.o == Py_True ? 3 : 4)) return false;
   int32_t n[4];
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < (int)PyTuple_GET_SIZE(shape.o); ++i) {
     const long long x = PyLong_AsLongLong(PyTuple_GET_ITEM(shape.o, i));
     if (PyErr_Occurred() || x < 0 || x > INT32_MAX) return false;
     n[i] = (int32_t)x;
+  }
+  if (mx.o == Py_True) {
+    if (n[2] != S2L_MXFP4_RUN_BYTES || fp8.o == Py_True) return false;
+    n[2] = S2L_PAGE_SIZE;
+    n[3] = S2L_HEAD_DIM;
   }
   void *ks = nullptr, *vs = nullptr;
   if (!data_ptr(k.o, &c->k_pages) || !attr_data_ptr(o, s_v_pages, &c->v_pages)) return false;
@@ -139,7 +147,7 @@ bool cache_arg(PyObject* o, s2l_kv_cache* c) {
   c->num_kv_heads = n[1];
   c->page_size = n[2];
   c->head_dim = n[3];
-  c->dtype = fp8.o == Py_True ? S2L_KV_FP8_E4M3 : S2L_KV_BF16;
+  c->dtype = mx.o == Py_True ? S2L_KV_MXFP4 : fp8.o == Py_True ? S2L_KV_FP8_E4M3 : S2L_KV_BF16;
   return true;
 }
 
@@ -290,6 +298,35 @@ bool rope_arg(PyObject* o, int64_t tokens, long dev, s2l_rope* r) {
   return true;
 }
 
+// A QKNorm's weight: None, or a contiguous device vector of 128 of the type that `dtype` names, which the
+// first weight sets.
+bool weight_arg(PyObject* o, PyObject* name, long dev, int32_t* dtype, const void** w) {
+  const Ref t(PyObject_GetAttr(o, name));
+  *w = nullptr;
+  if (!t || t.o == Py_None) return t.o == Py_None;
+  void* p;
+  int64_t n, s;
+  const int32_t type = tensor(t.o, f32, &p) ? S2L_NORM_FP32 : tensor(t.o, bf16, &p) ? S2L_NORM_BF16 : -1;
+  if (type < 0 || (*dtype >= 0 && type != *dtype) || !layout(t.o, 1, &n, &s) || n != S2L_HEAD_DIM || !on_device(t.o, dev)) return false;
+  *dtype = type;
+  *w = p;
+  return true;
+}
+
+bool norm_arg(PyObject* o, long dev, s2l_qk_norm* n) {
+  if ((PyObject*)Py_TYPE(o) != norm_type) return false;
+  *n = s2l_qk_norm{};
+  int32_t dtype = -1;
+  const Ref eps(PyObject_GetAttr(o, s_eps)), offset(PyObject_GetAttr(o, s_offset));
+  if (!eps || !offset || !PyFloat_CheckExact(eps.o) || !PyFloat_CheckExact(offset.o) ||
+      !weight_arg(o, s_q_weight, dev, &dtype, &n->q_weight) || !weight_arg(o, s_k_weight, dev, &dtype, &n->k_weight))
+    return false;
+  n->eps = (float)PyFloat_AS_DOUBLE(eps.o);
+  n->offset = (float)PyFloat_AS_DOUBLE(offset.o);
+  n->weight_dtype = dtype < 0 ? S2L_NORM_BF16 : dtype;
+  return true;
+}
+
 PyObject* general() {   // not the plain form: whatever was raised on the way does not count
   PyErr_Clear();
   Py_RETURN_NONE;
@@ -382,42 +419,75 @@ PyObject* reduce(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return call([&] { return lib.reduce(&batch.c, hq, out, static_cast<float*>(lse), info.p, ws, bytes, stream); });
 }
 
-// (batch, rope, q, q_out, k, k_out, stream)
-PyObject* rope_qk(PyObject*, PyObject* const* a, Py_ssize_t n) {
+// (batch, rope, q, q_out, k, k_out, stream), with a norm after the batch for norm_rope_qk
+PyObject* rotate(PyObject* const* a, Py_ssize_t n, bool normed) {
   BatchArg batch;
   s2l_rope rope;
+  s2l_qk_norm norm;
   Rows q, q_out, k, k_out;
   int64_t tokens;
   long dev;
   void* stream;
-  if (n != 7 || !batch_on_device(a[0], &batch, &tokens, &dev) || !rope_arg(a[1], tokens, dev, &rope) || !q.take(a[2], tokens, dev) ||
-      !q_out.take(a[3], tokens, dev) || q.heads != q_out.heads || !stream_arg(a[6], &stream))
+  if (n != 7 + normed || !batch_on_device(a[0], &batch, &tokens, &dev) || (normed && !norm_arg(a[1], dev, &norm))) return general();
+  a += normed;
+  if (!rope_arg(a[1], tokens, dev, &rope) || !q.take(a[2], tokens, dev) || !q_out.take(a[3], tokens, dev) || q.heads != q_out.heads ||
+      !stream_arg(a[6], &stream))
     return general();
   if (a[4] != Py_None && (!k.take(a[4], tokens, dev) || !k_out.take(a[5], tokens, dev) || k.heads != k_out.heads)) return general();
   return call([&] {
-    return lib.rope_qk(&batch.c, &rope, q.p, q.stride, q.heads, q_out.p, q_out.stride, k.p, k.stride, k.heads, k_out.p, k_out.stride,
-                       stream);
+    return normed ? lib.norm_rope_qk(&batch.c, &norm, &rope, q.p, q.stride, q.heads, q_out.p, q_out.stride, k.p, k.stride, k.heads,
+                                     k_out.p, k_out.stride, stream)
+                  : lib.rope_qk(&batch.c, &rope, q.p, q.stride, q.heads, q_out.p, q_out.stride, k.p, k.stride, k.heads, k_out.p,
+                                k_out.stride, stream);
   });
 }
+PyObject* rope_qk(PyObject*, PyObject* const* a, Py_ssize_t n) { return rotate(a, n, false); }
+PyObject* norm_rope_qk(PyObject*, PyObject* const* a, Py_ssize_t n) { return rotate(a, n, true); }
 
-// (cache, batch, rope, q, q_out, k, v, stream)
-PyObject* rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+// (cache, batch, rope, q, q_out, k, v, stream), with a norm after the batch for norm_rope_append
+PyObject* rotate_append(PyObject* const* a, Py_ssize_t n, bool normed) {
   s2l_kv_cache cache;
   BatchArg batch;
   s2l_rope rope;
+  s2l_qk_norm norm;
   Rows q, q_out, k, v;
   int64_t tokens;
   long dev;
   void* stream;
-  if (n != 8 || !cache_arg(a[0], &cache) || !batch_on_device(a[1], &batch, &tokens, &dev) || !cache_on_device(a[0], cache, dev) ||
-      !rope_arg(a[2], tokens, dev, &rope) ||
-      !k.take(a[5], tokens, dev) || !v.take(a[6], tokens, dev) || k.heads != cache.num_kv_heads || v.heads != k.heads ||
-      !stream_arg(a[7], &stream))
+  if (n != 8 + normed || !cache_arg(a[0], &cache) || !batch_on_device(a[1], &batch, &tokens, &dev) ||
+      !cache_on_device(a[0], cache, dev) || (normed && !norm_arg(a[2], dev, &norm)))
+    return general();
+  a += normed;
+  if (!rope_arg(a[2], tokens, dev, &rope) || !k.take(a[5], tokens, dev) || !v.take(a[6], tokens, dev) ||
+      k.heads != cache.num_kv_heads || v.heads != k.heads || !stream_arg(a[7], &stream))
     return general();
   if (a[3] != Py_None && (!q.take(a[3], tokens, dev) || !q_out.take(a[4], tokens, dev) || q.heads != q_out.heads)) return general();
   return call([&] {
-    return lib.rope_append(&cache, &batch.c, &rope, q.p, q.stride, q.heads, q_out.p, q_out.stride, k.p, k.stride, v.p, v.stride, stream);
+    return normed ? lib.norm_rope_append(&cache, &batch.c, &norm, &rope, q.p, q.stride, q.heads, q_out.p, q_out.stride, k.p, k.stride,
+                                         v.p, v.stride, stream)
+                  : lib.rope_append(&cache, &batch.c, &rope, q.p, q.stride, q.heads, q_out.p, q_out.stride, k.p, k.stride, v.p,
+                                    v.stride, stream);
   });
+}
+PyObject* rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) { return rotate_append(a, n, false); }
+PyObject* norm_rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) { return rotate_append(a, n, true); }
+
+// (cache, batch, part, cu_out, k_out, v_out, stream)
+PyObject* read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  s2l_kv_cache cache;
+  BatchArg batch;
+  int32_t part;
+  int64_t tokens, rows[3], more[3], s[3];
+  long dev;
+  void *cu, *k, *v, *stream;
+  size_t offsets;
+  if (n != 7 || !cache_arg(a[0], &cache) || !batch_on_device(a[1], &batch, &tokens, &dev) || !cache_on_device(a[0], cache, dev) ||
+      !int_arg(a[2], &part) || !tensor(a[3], i32, &cu) || !numel(a[3], &offsets) || !on_device(a[3], dev) || !layout(a[3], 1, rows, s) ||
+      offsets < (size_t)batch.c.num_reqs || !tensor(a[4], bf16, &k) || !on_device(a[4], dev) || !layout(a[4], 3, rows, s) ||
+      !tensor(a[5], bf16, &v) || !on_device(a[5], dev) || !layout(a[5], 3, more, s) || rows[0] != more[0] ||
+      rows[1] != cache.num_kv_heads || more[1] != rows[1] || rows[2] != S2L_HEAD_DIM || more[2] != S2L_HEAD_DIM || !stream_arg(a[6], &stream))
+    return general();
+  return call([&] { return lib.read(&cache, &batch.c, part, static_cast<const int32_t*>(cu), k, v, rows[0], stream); });
 }
 
 // (state, batch, q, k, v, scale, out, workspace, stream)
@@ -449,16 +519,16 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // (types and dtypes and torch functions as a tuple, entry point addresses as a tuple)
 PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  void* f[10];
+  void* f[13];
   PyObject** o[] = {&tensor_type, &cache_type, &batch_type, &opts_type, &info_type, &stream_type,
-                    &bf16, &f32, &u8, &is_initialized, &get_device, &get_stream, &rope_type, &state_type, &i32};
-  if (n != 2 || !PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) != 15 || !PyTuple_Check(a[1]) || PyTuple_GET_SIZE(a[1]) != 10) {
+                    &bf16, &f32, &u8, &is_initialized, &get_device, &get_stream, &rope_type, &state_type, &i32, &norm_type};
+  if (n != 2 || !PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) != 16 || !PyTuple_Check(a[1]) || PyTuple_GET_SIZE(a[1]) != 13) {
     PyErr_SetString(PyExc_TypeError, "setup(objects, addresses)");
     return nullptr;
   }
-  for (int i = 0; i < 10; ++i)
+  for (int i = 0; i < 13; ++i)
     if (!to_ptr(PyTuple_GET_ITEM(a[1], i), &f[i])) return nullptr;
-  for (int i = 0; i < 15; ++i) {
+  for (int i = 0; i < 16; ++i) {
     Py_INCREF(PyTuple_GET_ITEM(a[0], i));
     Py_XSETREF(*o[i], PyTuple_GET_ITEM(a[0], i));
   }
@@ -470,12 +540,15 @@ PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
   lib.rope_qk = reinterpret_cast<decltype(lib.rope_qk)>(f[7]);
   lib.rope_append = reinterpret_cast<decltype(lib.rope_append)>(f[8]);
   lib.linear = reinterpret_cast<decltype(lib.linear)>(f[9]);
+  lib.norm_rope_qk = reinterpret_cast<decltype(lib.norm_rope_qk)>(f[10]);
+  lib.norm_rope_append = reinterpret_cast<decltype(lib.norm_rope_append)>(f[11]);
+  lib.read = reinterpret_cast<decltype(lib.read)>(f[12]);
   Py_RETURN_NONE;
 }
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(setup), FAST(append), FAST(plan), FAST(attn), FAST(fused), FAST(reduce), FAST(rope_qk),
-                         FAST(rope_append), FAST(linear), {nullptr, nullptr, 0, nullptr}};
+                         FAST(rope_append), FAST(linear), FAST(norm_rope_qk), FAST(norm_rope_append), FAST(read), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Argument marshalling of the per-step calls.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 
@@ -492,7 +565,8 @@ PyMODINIT_FUNC PyInit__binding(void) {
                {&s_cu_chunk, "cu_chunk"}, {&s_block_tables, "block_tables"}, {&s_cuda_stream, "cuda_stream"},
                {&s_stride, "stride"}, {&s_get_device, "get_device"}, {&s_inv_freq, "inv_freq"}, {&s_positions, "positions"},
                {&s_pair_axis, "pair_axis"}, {&s_adjacent, "adjacent"}, {&s_scale, "scale"}, {&s_states, "states"},
-               {&s_log_decay, "log_decay"}, {&s_slot_in, "slot_in"}, {&s_slot_out, "slot_out"}};
+               {&s_log_decay, "log_decay"}, {&s_slot_in, "slot_in"}, {&s_slot_out, "slot_out"}, {&s_mxfp4, "mxfp4"},
+               {&s_q_weight, "q_weight"}, {&s_k_weight, "k_weight"}, {&s_eps, "eps"}, {&s_offset, "offset"}};
   for (const auto& n : names)
     if (!(*n.o = PyUnicode_InternFromString(n.s))) return nullptr;
   return PyModule_Create(&module);

@@ -70,7 +70,41 @@ __device__ inline u32x2 encode8(const u32x4& x, float inv) {
                f32x4_to_fp8x4(bf16lo(x[2]) * inv, bf16hi(x[2]) * inv, bf16lo(x[3]) * inv, bf16hi(x[3]) * inv)};
 }
 
-template <bool kAdjacent, bool kAppend, bool kFp8, int kHeads>
+// A head's norm: its 16 elements a lane times 1 / sqrt(mean square + eps) and the weights, fp32.  The sum runs over
+// the head's eight lanes in a fixed order.
+__device__ inline void norm16(float* x, float* y, const float* wx, const float* wy, float eps) {
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s = __builtin_fmaf(x[i], x[i], s);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s = __builtin_fmaf(y[i], y[i], s);
+  s += u2f(lane_xor1(f2u(s)));
+  s += u2f(lane_xor2(f2u(s)));
+  s += u2f(lane_of_other_four(f2u(s)));
+  const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(s, 1.0f / 128.0f, eps));
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = x[i] * r * wx[i], y[i] = y[i] * r * wy[i];
+}
+// Eight of a head's weights from dim `d` on, with the offset.
+__device__ inline void load_weights(const void* weight, bool fp32, int d, float offset, float* w) {
+  if (weight == nullptr) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = 1.f;
+    return;
+  }
+  if (fp32) {
+    const f32x4_any* p = reinterpret_cast<const f32x4_any*>(static_cast<const float*>(weight) + d);
+    const f32x4 a = p[0], b = p[1];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = (i < 4 ? a[i & 3] : b[i & 3]) + offset;
+  } else {
+    unpack8(*reinterpret_cast<const u32x4_any*>(static_cast<const uint16_t*>(weight) + d), w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] += offset;
+  }
+}
+
+template <bool kAdjacent, bool kAppend, PageKind kKind, bool kNorm, int kHeads>
 __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a) {
   const int lane = threadIdx.x & 63, unit = lane & 7;
   const int heads = a.hq + a.hkv * (kAppend ? 2 : 1);
@@ -102,6 +136,18 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a) {
     xb[j] = *reinterpret_cast<const u32x4_any*>(src + ob);
   }
 
+  float wa[kNorm ? kHeads : 1][8], wb[kNorm ? kHeads : 1][8];
+  if constexpr (kNorm) {
+#pragma unroll
+    for (int j = 0; j < kHeads; ++j) {
+      const int h = head0 + 8 * j;
+      if (h >= a.hq + a.hkv) continue;   // past the heads, or values
+      const void* weight = h < a.hq ? a.q_weight : a.k_weight;
+      load_weights(weight, a.norm_fp32, oa, a.offset, wa[j]);
+      load_weights(weight, a.norm_fp32, ob, a.offset, wb[j]);
+    }
+  }
+
   float cs[8], sn[8];
   if (turns) {
     double pos[S2L_ROPE_MAX_AXES];
@@ -131,19 +177,25 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a) {
   for (int j = 0; j < kHeads; ++j) {
     const int h = head0 + 8 * j;
     if (h >= heads) continue;
-    if (turns && (!kAppend || h < a.hq + a.hkv)) {
+    const bool rotates = turns && (!kAppend || h < a.hq + a.hkv);
+    if (rotates || (kNorm && h < a.hq + a.hkv)) {
       float x[8], y[8];
       unpack8(xa[j], x);
       unpack8(xb[j], y);
-      float u[8], w[8];
+      if constexpr (kNorm) norm16(x, y, wa[j], wb[j], a.eps);
+      if (rotates) {
+        float u[8], w[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if constexpr (!kAdjacent) turn(x[i], y[i], cs[i], sn[i], &u[i], &w[i]);
-        else if (i < 4) turn(x[2 * i], x[2 * i + 1], cs[i], sn[i], &u[2 * i], &u[2 * i + 1]);
-        else turn(y[2 * i - 8], y[2 * i - 7], cs[i], sn[i], &w[2 * i - 8], &w[2 * i - 7]);
+        for (int i = 0; i < 8; ++i) {
+          if constexpr (!kAdjacent) turn(x[i], y[i], cs[i], sn[i], &u[i], &w[i]);
+          else if (i < 4) turn(x[2 * i], x[2 * i + 1], cs[i], sn[i], &u[2 * i], &u[2 * i + 1]);
+          else turn(y[2 * i - 8], y[2 * i - 7], cs[i], sn[i], &w[2 * i - 8], &w[2 * i - 7]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = u[i], y[i] = w[i];
       }
-      xa[j] = pack8(u);
-      xb[j] = pack8(w);
+      xa[j] = pack8(x);
+      xb[j] = pack8(y);
     }
     if (h < a.hq) {
       uint16_t* dst = a.q_out + row * a.q_out_stride + h * 128;
@@ -158,7 +210,29 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a) {
       const int g = h - a.hq - (is_v ? a.hkv : 0);
       const int64_t dst = (slot_row + g * 16) * 128;
       void* pool = is_v ? a.v_pool : a.k_pool;
-      if constexpr (kFp8) {
+      if constexpr (kKind == kMxfp4Pages) {
+        // the head's 16 chunks of eight dims lie over its eight lanes as they were paired: each block's
+        // largest magnitude from its four, by a 16-bit field a block
+        uint32_t m[2] = {0, 0};
+        const uint32_t ma = max_magnitude(xa[j]), mb = max_magnitude(xb[j]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t fa = oa >> 6 == i ? ma << ((oa >> 1) & 16) : 0, fb = ob >> 6 == i ? mb << ((ob >> 1) & 16) : 0;
+          m[i] = max_u16x2(fa, fb);
+          m[i] = max_u16x2(m[i], lane_xor1(m[i]));
+          m[i] = max_u16x2(m[i], lane_xor2(m[i]));
+          m[i] = max_u16x2(m[i], lane_of_other_four(m[i]));
+        }
+        uint32_t bytes = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bytes |= mx_scale_byte(m[i >> 1] >> (16 * (i & 1)) & 0xFFFFu) << (8 * i);
+        const int slot = (int)(slot_row & 15);
+        uint8_t* run = static_cast<uint8_t*>(pool) + ((slot_row >> 4) + g) * kMxRunBytes;
+        uint8_t* codes = run + slot * kMxCodeBytes;
+        *reinterpret_cast<uint32_t*>(codes + oa / 2) = mx_encode8(xa[j], bytes >> (oa / kMxBlock * 8) & 255u);
+        *reinterpret_cast<uint32_t*>(codes + ob / 2) = mx_encode8(xb[j], bytes >> (ob / kMxBlock * 8) & 255u);
+        if (unit == 0) *reinterpret_cast<uint32_t*>(run + kMxScalesAt + slot * kMxScaleBytes) = bytes;
+      } else if constexpr (kKind == kE4m3Pages) {
         const float inv = __fdiv_rn(1.0f, (is_v ? a.v_scale : a.k_scale)[g]);
         *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(pool) + dst + oa) = encode8(xa[j], inv);
         *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(pool) + dst + ob) = encode8(xb[j], inv);
@@ -174,31 +248,34 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a) {
 // hide more.  One head a lane and two, us in a graph: 32 + 8 + 8 heads, 512 rows 4.6 and 4.8, 1024 (6144 waves) 7.9 and
 // 7.9, 1365 (8190) 9.6 and 8.9, 4096 24.0 and 21.8; 64 + 8 + 8 into e4m3 pages, 600 (6000) 8.3 and 8.1, 1000 11.4 and
 // 10.1; 32 + 32 without pages, 768 (6144) 8.4 and 8.4, 1024 10.1 and 10.1.
-template <bool kAdjacent, bool kAppend, bool kFp8>
+template <bool kAdjacent, bool kAppend, PageKind kKind, bool kNorm>
 void launch(const RopeLaunch& a, hipStream_t stream) {
   constexpr int64_t kFewWaves = 6144;
   const int heads = a.hq + a.hkv * (kAppend ? 2 : 1);
   const int64_t four_rows = ((int64_t)a.total_rows + 3) / 4, groups = (heads + 7) / 8;
   if (a.total_rows * groups <= kFewWaves)
-    rope_kernel<kAdjacent, kAppend, kFp8, 1><<<dim3((uint32_t)(four_rows * groups)), 256, 0, stream>>>(a);
+    rope_kernel<kAdjacent, kAppend, kKind, kNorm, 1><<<dim3((uint32_t)(four_rows * groups)), 256, 0, stream>>>(a);
   else
-    rope_kernel<kAdjacent, kAppend, kFp8, 2><<<dim3((uint32_t)(four_rows * ((groups + 1) / 2))), 256, 0, stream>>>(a);
+    rope_kernel<kAdjacent, kAppend, kKind, kNorm, 2><<<dim3((uint32_t)(four_rows * ((groups + 1) / 2))), 256, 0, stream>>>(a);
+}
+
+template <bool kAppend, PageKind kKind>
+void launch_kind(const RopeLaunch& a, hipStream_t stream) {
+  if (a.norm) {
+    if (a.adjacent) launch<true, kAppend, kKind, true>(a, stream);
+    else launch<false, kAppend, kKind, true>(a, stream);
+  } else {
+    if (a.adjacent) launch<true, kAppend, kKind, false>(a, stream);
+    else launch<false, kAppend, kKind, false>(a, stream);
+  }
 }
 
 }  // namespace
 
 hipError_t launch_rope(const RopeLaunch& a, hipStream_t stream) {
   if (a.total_rows == 0 || a.hq + a.hkv == 0) return hipSuccess;
-  if (a.k_pool == nullptr) {
-    if (a.adjacent) launch<true, false, false>(a, stream);
-    else launch<false, false, false>(a, stream);
-  } else if (a.fp8) {
-    if (a.adjacent) launch<true, true, true>(a, stream);
-    else launch<false, true, true>(a, stream);
-  } else {
-    if (a.adjacent) launch<true, true, false>(a, stream);
-    else launch<false, true, false>(a, stream);
-  }
+  if (a.k_pool == nullptr) launch_kind<false, kBf16Pages>(a, stream);
+  else with_kind(a.kind, [&](auto kind) { launch_kind<true, decltype(kind)::value>(a, stream); });
   return hipGetLastError();
 }
 

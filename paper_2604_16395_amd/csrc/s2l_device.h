@@ -12,6 +12,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 __device__ inline uint32_t f2u(float x) { return __builtin_bit_cast(uint32_t, x); }
@@ -43,6 +44,56 @@ __device__ inline uint32_t f32x4_to_fp8x4(float a, float b, float c, float d) {
   w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(sat448(c), sat448(d), (int)w, true);
   return w;
 }
+
+// MXFP4: 32 dims share a power of two, 2^(b - 127) for the stored byte b; b = 255 makes NaN of them.
+// Its bits as an fp32 number's exponent are the scale operand of the conversions (2^-127, byte 0, is
+// taken as such).
+__device__ inline float mx_scale(uint32_t b) { return u2f(b << 23); }
+
+// Eight E2M1 codes (one dword, low half of a byte first) times the scale -> eight bf16 (exact).
+__device__ inline u32x4 fp4x8_to_bf16x8(uint32_t w, float scale) {
+  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3))};
+}
+
+// A pair of bf16 divided by the scale -> two E2M1 codes (RNE, saturating at 6) in byte kByte of w.  The pair
+// is passed by value: a bit cast of a vector's element, where that is an lvalue, reads its first one.
+template <int kByte>
+__device__ inline uint32_t bf16x2_to_fp4x2(uint32_t w, uint32_t pair, float scale) {
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, pair), scale, kByte);
+}
+__device__ inline uint32_t bf16x8_to_fp4x8(const u32x4& x, float scale) {
+  return bf16x2_to_fp4x2<3>(bf16x2_to_fp4x2<2>(bf16x2_to_fp4x2<1>(bf16x2_to_fp4x2<0>(0u, x[0], scale), x[1], scale), x[2], scale),
+                            x[3], scale);
+}
+
+// Magnitudes as integers: bf16 without its sign orders like the number, infinity and NaN above all.
+__device__ inline uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+// The largest magnitude of eight bf16, in the lower half.
+__device__ inline uint32_t max_magnitude(const u32x4& x) {
+  constexpr uint32_t kAbs = 0x7FFF7FFFu;
+  const uint32_t m = max_u16x2(max_u16x2(x[0] & kAbs, x[1] & kAbs), max_u16x2(x[2] & kAbs, x[3] & kAbs));
+  return max_u16x2(m, m >> 16) & 0xFFFFu;
+}
+// The scale byte of a block by its largest magnitude: floor(log2) is the exponent field less 127, E2M1's
+// largest binade starts at 2^2, and bytes below 2 would make values that bf16 holds as subnormals only.
+__device__ inline uint32_t mx_scale_byte(uint32_t magnitude) {
+  const int e = (int)(magnitude >> 7);
+  return e == 255 ? 255u : (uint32_t)(e < 4 ? 2 : e - 2);
+}
+// The codes of eight dims of such a block: 0 where it is NaN.
+__device__ inline uint32_t mx_encode8(const u32x4& x, uint32_t byte) {
+  return byte == 255u ? 0u : bf16x8_to_fp4x8(x, mx_scale(byte));
+}
+
+// x of lane l ^ 1, l ^ 2, and of the lane opposite in its eight (for a value that is equal in each four).
+__device__ inline uint32_t lane_xor1(uint32_t x) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xF, 0xF, true); }
+__device__ inline uint32_t lane_xor2(uint32_t x) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xF, 0xF, true); }
+__device__ inline uint32_t lane_of_other_four(uint32_t x) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x141, 0xF, 0xF, true); }
 
 // acc + lo + hi of a packed bf16 pair, in fp32 (v_dot2_f32_bf16 with (1, 1)).
 __device__ inline float sum_bf16x2(uint32_t w, float acc) {
