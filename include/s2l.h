@@ -87,7 +87,8 @@ typedef enum s2l_kv_dtype {
  * kept where bf16 has normal values: of a block with largest magnitude a, exponent
  * e = max(floor(log2 a) - 2, -125), code = e2m1(x 2^-e), round to nearest even, saturating to +-6; a
  * block that holds a NaN or an infinity becomes NaN throughout (byte 255, codes 0).  The cached value
- * is decode(code) 2^e.  Attention takes any byte but 253 and 254, whose values pass bf16's range.
+ * is decode(code) 2^e.  Bytes 253 and 254, whose values pass bf16's range, are never written; attention
+ * takes them for NaN in V.
  */
 typedef struct s2l_kv_cache {
   void* k_pages;          /* device; bf16 elements, uint8 codes or MXFP4 runs               */
@@ -453,7 +454,9 @@ s2l_status s2l_attn_plan(const s2l_batch* batch, int32_t num_q_heads, int32_t nu
  * see its key; of an MXFP4 cache a NaN of V reaches no other row.  Precision: the
  * weights e^{s_j} / sum are applied as bf16 values normalised by their own sum, so out is
  * within about 2^-7 sum_j w_j |V_j - out| + 2^-8 |out| of the exact result; lse is the
- * log of the sum of those bf16 weights (within about 2^-8 of the exact value).
+ * log of the sum of those bf16 weights (within about 2^-8 of the exact value).  Over an MXFP4 cache tiles of 128
+ * and 256 columns take each q within 2^-13 of the largest magnitude among its 32 dims (32 b .. 32 b + 31 of a
+ * row), which moves s_j by at most 2^-13 softmax_scale sum |that magnitude K|; softmax_scale |q| < 2^100.
  *   q   : device bf16 [T][Hq][128] (post-RoPE).     out : device bf16 [T][Hq][128].
  *   lse : device fp32 [T][Hq] or NULL.               softmax_scale > 0 (e.g. 1/sqrt(128)).
  *   plan: the s2l_plan_info returned by s2l_attn_plan for this batch and head counts.

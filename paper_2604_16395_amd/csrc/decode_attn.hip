@@ -57,6 +57,7 @@ constexpr int kVRow = kHeadDim * 2;             // bf16 key row in LDS
 // flight), 8 KiB of K and V each way per tile either way, so that two workgroups fit a CU.
 template <PageKind kKind>
 constexpr int kTilePages = kKind == kBf16Pages ? 2 : 4;
+constexpr int kDNoNan = 0x7FFFFFFF;
 constexpr float kDLn2 = 0.6931471805599453f;
 constexpr float kDOverflow = 18446744073709551616.0f;   // 2^64
 constexpr int32_t kDRsrcWord3 = 0x00020000;
@@ -158,9 +159,8 @@ __global__ __launch_bounds__(kDecodeWaves * 64, 2) void attn_decode_kernel(
   };
   int32_t pg0 = load_pages(0);   // before the Q loads, so that the first tile does not wait for them
   int32_t pg1 = load_pages(1);
-  if constexpr (kMx) {
-    if (threadIdx.x < kMxScaleBytes) s_nan[threadIdx.x] = 0x7FFFFFFF;
-    __syncthreads();
+  if constexpr (kMx) {   // the merge's first barrier comes before its use
+    if (threadIdx.x < kMxScaleBytes) s_nan[threadIdx.x] = kDNoNan;
   }
 
   // Q^T (B operand) of k-step ks: lane (j, q) holds eight dims of Q[column j], the same ones that
@@ -188,14 +188,15 @@ __global__ __launch_bounds__(kDecodeWaves * 64, 2) void attn_decode_kernel(
       // uniform by construction; readfirstlane lets the compiler see it (a descriptor it
       // must treat as per-lane costs a loop around every load)
       const int keys = k < my_n ? clamp16i(hi - (key0 + 16 * b)) : 0;
-      const int bytes = __builtin_amdgcn_readfirstlane(kMx ? kRun : keys * kKeyBytes);
+      // MXFP4: a page that has a key below `hi` whole (see stage_v)
+      const int bytes = __builtin_amdgcn_readfirstlane(kMx ? (keys > 0 ? kRun : 0) : keys * kKeyBytes);
       const auto kr = page_rsrc(kpb + page * page_stride, bytes);
       const auto vr = page_rsrc(vpb + page * page_stride, bytes);
-      if constexpr (kMx) {   // K: key j, block q.  V: key l / 4, block l % 4.  Keys at or past `hi`: past the run
-        const int ko = j < keys ? j : kRun, vo = lane >> 2 < keys ? lane >> 2 : kRun;
-        t.k[b][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kr, ko * kMxCodeBytes + 16 * qg, 0, 0));
+      if constexpr (kMx) {   // K: key j, block q.  V: key l / 4, block l % 4
+        const int vo = lane >> 2;
+        t.k[b][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kr, j * kMxCodeBytes + 16 * qg, 0, 0));
         t.v[b][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vr, vo * kMxCodeBytes + 16 * (lane & 3), 0, 0));
-        t.ks[b] = __builtin_amdgcn_raw_buffer_load_b8(kr, kMxScalesAt + ko * kMxScaleBytes + qg, 0, 0);
+        t.ks[b] = __builtin_amdgcn_raw_buffer_load_b8(kr, kMxScalesAt + j * kMxScaleBytes + qg, 0, 0);
         t.vs[b] = __builtin_amdgcn_raw_buffer_load_b8(vr, kMxScalesAt + vo * kMxScaleBytes + (lane & 3), 0, 0);
         continue;
       }
@@ -214,19 +215,22 @@ __global__ __launch_bounds__(kDecodeWaves * 64, 2) void attn_decode_kernel(
     }
   };
   // V rows of a tile from registers into this wave's LDS (key-major, permuted chunks).
-  // A NaN block of MXFP4 V goes in as zeros, and its key into s_nan: 0 times NaN would reach the columns
-  // that do not see the key.
+  // A block of MXFP4 V that is NaN (or past bf16's range) goes in with values of 2^-125 and less, and its key
+  // into nan_key: 0 times NaN would reach the columns that do not see the key.  So what keys at or past `hi`
+  // hold has no effect: no column sees them.
+  int32_t nan_key = kDNoNan;
   auto stage_v = [&](int k, const TileRegs<kKind>& t) {
     if constexpr (kMx) {
 #pragma unroll
       for (int b = 0; b < kPages; ++b) {
         const int row = 16 * b + (lane >> 2), c0 = 4 * (lane & 3), sw = 2 * (row & 7);
-        const bool bad = t.vs[b] == 255u;
-        if (__builtin_amdgcn_ballot_w64(bad) != 0 && bad) atomicMin(&s_nan[lane & 3], lo + (wave + kDecodeWaves * k) * kDTile + row);
+        const bool bad = t.vs[b] > 252u;
+        const int key = lo + (wave + kDecodeWaves * k) * kDTile + row;
+        nan_key = bad && key < nan_key ? key : nan_key;
         const float scale = mx_scale(bad ? 0u : t.vs[b]);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<u32x4*>(vbuf + row * kVRow + 16 * ((c0 + i) ^ sw)) = fp4x8_to_bf16x8(bad ? 0u : t.v[b][0][i], scale);
+          *reinterpret_cast<u32x4*>(vbuf + row * kVRow + 16 * ((c0 + i) ^ sw)) = fp4x8_to_bf16x8(t.v[b][0][i], scale);
       }
       return;
     }
@@ -378,6 +382,9 @@ __global__ __launch_bounds__(kDecodeWaves * 64, 2) void attn_decode_kernel(
 #pragma unroll
   for (int db = 0; db < 8; ++db) *reinterpret_cast<f32x4*>(xo + ((wave * 8 + db) * 64 + lane) * 4) = o[db];
   *reinterpret_cast<f32x2*>(xml + (wave * 64 + lane) * 2) = f32x2{m_col, l_col};
+  if constexpr (kMx) {
+    if (nan_key != kDNoNan) atomicMin(&s_nan[lane & 3], nan_key);
+  }
   __syncthreads();
   float mw[kDecodeWaves], lw[kDecodeWaves], mstar = -INFINITY;
 #pragma unroll

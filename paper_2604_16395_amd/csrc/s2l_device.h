@@ -13,10 +13,16 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x6 __attribute__((ext_vector_type(6)));
+typedef _Float16 f16x32 __attribute__((ext_vector_type(32)));
+typedef float f32x32 __attribute__((ext_vector_type(32)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 __device__ inline uint32_t f2u(float x) { return __builtin_bit_cast(uint32_t, x); }
 __device__ inline float u2f(uint32_t x) { return __builtin_bit_cast(float, x); }
+
+__device__ inline float bf16lo(uint32_t w) { return u2f(w << 16); }
+__device__ inline float bf16hi(uint32_t w) { return u2f(w & 0xFFFF0000u); }
 
 // Two fp32 -> packed bf16 pair, round to nearest even (v_cvt_pk_bf16_f32).
 __device__ inline uint32_t pack_bf16x2(float a, float b) {
@@ -90,6 +96,49 @@ __device__ inline uint32_t mx_encode8(const u32x4& x, uint32_t byte) {
   return byte == 255u ? 0u : bf16x8_to_fp4x8(x, mx_scale(byte));
 }
 
+// Queries against MXFP4 keys on the f8f6f4 MFMA, which takes the keys' codes and scales as they are stored and,
+// against E2M3 values, runs at twice the rate of bf16.  Queries enter times a factor (the softmax's, so that the
+// products are the exponents of the probabilities), as the sum of three E2M3 values with one power of two for
+// each 32 dims, as the keys have it:
+//   factor q = 2^(s - 127) (t0 + t1 / 8 + t2 / 256 + rest),
+// each value the nearest to what the ones before leave (at most 7.5).  The block's largest goes to [4, 8), so t0
+// leaves at most 1/4 (1/2 from 7.75 on), t1 2^-7 (2^-6), t2 2^-12 (2^-11); what t0 leaves is rounded to f16 on the
+// way, 2^-14 (2^-13) at most.  So |rest| <= 2^-13 of the block's largest: 14 bits below it, where bf16 has 8.
+struct QueryTerms {
+  u32x6 t[3];
+  uint32_t scales;     // of t0 .. t2, a byte each: 255 (NaN) where a query is not finite
+};
+__device__ inline QueryTerms split_queries(const u32x4& a, const u32x4& b, const u32x4& c, const u32x4& d, float factor) {
+  const uint32_t m = max_u16x2(max_u16x2(max_magnitude(a), max_magnitude(b)), max_u16x2(max_magnitude(c), max_magnitude(d)));
+  // the exponent of (largest x factor), each taken as a number in [1, 2) and a power of two: no overflow on the way
+  const uint32_t f = f2u(factor);
+  const float top = u2f((m << 16 & 0x7FFFFFu) | 0x3F800000u) * u2f((f & 0x7FFFFFu) | 0x3F800000u);
+  const int e = (int)(m >> 7) + (int)(f >> 23) - 127 + (top >= 2.f) - 2;
+  const int s = e < 9 ? 9 : e > 254 ? 254 : e;   // below: all of it leaves scores of 2^-100 and less
+  const float scale = u2f((f & 0x7FFFFFu) | 0x3F800000u);
+  const int shift = (int)(f >> 23) - s;          // factor q 2^(127 - s) = scale (q 2^shift)
+  float y[32];
+  f16x32 left;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const uint32_t w = i < 4 ? a[i & 3] : i < 8 ? b[i & 3] : i < 12 ? c[i & 3] : d[i & 3];
+    y[2 * i] = __builtin_ldexpf(bf16lo(w), shift) * scale;
+    y[2 * i + 1] = __builtin_ldexpf(bf16hi(w), shift) * scale;
+  }
+#pragma unroll
+  for (int i = 0; i < 32; ++i) left[i] = (_Float16)y[i];
+  QueryTerms r;
+  r.scales = m >= 0x7F80u ? 0xFFFFFFFFu : (uint32_t)(s | (s - 3) << 8 | (s - 8) << 16);
+  r.t[0] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_f16(left, 1.f);
+  const f32x32 t0 = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(r.t[0], 1.f);
+#pragma unroll
+  for (int i = 0; i < 32; ++i) left[i] = (_Float16)(y[i] - t0[i]);
+  r.t[1] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_f16(left, 0.125f);
+  left -= __builtin_amdgcn_cvt_scalef32_pk32_f16_fp6(r.t[1], 0.125f);
+  r.t[2] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_f16(left, 0.00390625f);
+  return r;
+}
+
 // x of lane l ^ 1, l ^ 2, and of the lane opposite in its eight (for a value that is equal in each four).
 __device__ inline uint32_t lane_xor1(uint32_t x) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xF, 0xF, true); }
 __device__ inline uint32_t lane_xor2(uint32_t x) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xF, 0xF, true); }
@@ -100,9 +149,6 @@ __device__ inline float sum_bf16x2(uint32_t w, float acc) {
   return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, 0x3F803F80u), acc,
                                          false);
 }
-
-__device__ inline float bf16lo(uint32_t w) { return u2f(w << 16); }
-__device__ inline float bf16hi(uint32_t w) { return u2f(w & 0xFFFF0000u); }
 
 // Combination over the lane pair (l, l ^ 32) with v_permlane32_swap, written as one
 // assembly block: the compiler treats the two results of permlane32_swap(x, x) as equal and

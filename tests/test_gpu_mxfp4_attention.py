@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2604_16395_amd as s2l
+import workloads
 from oracle import mxfp4
 from oracle.paged_kv import bf16_bits_to_f32
 from tests.gpu_util import DEV, LOG2E, SCALE, assert_attention_close, bf16_to_f64, plant_dots_for, to_bf16
@@ -100,6 +101,91 @@ def test_scores_that_rise_past_the_reference(layout, split):
     assert score[64:].max() - score[:64].max() > 64
     out, lse = s.attention(opts_of(layout, split))
     assert_attention_close(case, out, lse, s.oracle(), what=f"{layout}")
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+def test_queries_far_below_their_block(layout):
+    """Dims with queries 2000 times the others, over which all keys are zero: the scores come from the small ones.
+    Tiles of 128 and 256 columns take a query within 2^-13 of its block's largest, so a score is off by at most
+    d = 2^-13 scale sum_blocks largest sum |K|, a weight by e^(2 d) - 1 of itself; those of 16 columns take it whole."""
+    hq, hkv = 8, 2
+    case = mx_case("outliers", [400], [2], hq, hkv, seed=69, sigma=1.0)
+    q, k = bf16_bits_to_f32(case.q_bits).reshape(2, hq, 4, 32), bf16_bits_to_f32(case.k_full_bits)
+    q[:, :, :3, 5] = 2000 * np.sign(q[:, :, :3, 5])
+    k[:, :, [5, 37, 69]] = 0
+    case.q_bits, case.k_full_bits = workloads.bf16_bits(q.reshape(2, hq, 128)), quantised_bits(workloads.bf16_bits(k))
+    s = MxSetup(case)
+    s.append()
+    out, lse = s.attention(opts_of(layout))
+    o, l, a, b = s.oracle()
+    kept = np.abs(bf16_bits_to_f32(case.k_full_bits).astype(np.float64)).reshape(-1, hkv, 4, 32).sum(-1)      # [keys][hkv][4]
+    top = np.abs(q.astype(np.float64)).max(-1).reshape(2, hkv, hq // hkv, 4)
+    d = 0 if layout[0] == 16 else 2.0 ** -13 * SCALE * np.einsum("tgjb,kgb->tgjk", top, kept).max(-1).reshape(2, hq)
+    u = 2.0 ** -8
+    err = np.abs(bf16_to_f64(out) - o)
+    assert (err <= u * np.abs(o) + (2.02 * u + np.expm1(2 * np.asarray(d))[..., None]) * b + 2.0 ** -16 * a + 1e-6).all()
+    assert (np.abs(lse.cpu().numpy() - l) <= u + d + 1e-4 * (1 + np.abs(l))).all()
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("layout", LAYOUTS)
+def test_a_query_that_is_not_finite(layout, bad):
+    """Its own row is NaN; the others of its tile keep their bits."""
+    case = mx_case("bad_q", [300], [4], 4, 2, seed=70)
+    s = MxSetup(case)
+    s.append()
+    ref, ref_lse = s.attention(opts_of(layout))
+    s.q[2, 1, 77] = bad
+    out, lse = s.attention(opts_of(layout))
+    assert torch.isnan(out[2, 1]).all() and torch.isnan(lse[2, 1])
+    out[2, 1], lse[2, 1] = ref[2, 1], ref_lse[2, 1]
+    assert torch.equal(out.view(torch.int16), ref.view(torch.int16)) and torch.equal(lse, ref_lse)
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-4, 0.7, 1.9, 1.0e3])
+@pytest.mark.parametrize("layout", [(128, 1), (256, 1)])
+def test_other_softmax_scales(layout, scale):
+    """Factors of every mantissa and size, with queries of sizes from 2^-100 to 2 (scores up to thousands)."""
+    case = mx_case("scales", [130], [3], 2, 2, seed=71)
+    q = bf16_bits_to_f32(case.q_bits)
+    q[0] *= np.float32(2.0 ** -100)
+    q[1] *= np.float32(4 / max(scale, 1e-3) / 8)
+    case.q_bits = workloads.bf16_bits(q)
+    s = MxSetup(case)
+    s.append()
+    out, lse = s.attention(opts_of(layout), scale=scale)
+    o, l, a, b = s.oracle(scale=scale)
+    keys = np.abs(bf16_bits_to_f32(case.k_full_bits).astype(np.float64)).reshape(-1, 2, 4, 32).sum(-1)
+    top = np.abs(bf16_bits_to_f32(case.q_bits).astype(np.float64)).reshape(3, 2, 4, 32).max(-1)
+    # the queries' terms, and fp32 sums of products up to the largest score
+    d = (2.0 ** -13 + 2.0 ** -18) * scale * np.einsum("tgb,kgb->tgk", top, keys).max(-1)
+    u = 2.0 ** -8
+    err = np.abs(bf16_to_f64(out) - o)
+    assert (err <= u * np.abs(o) + (2.02 * u + np.expm1(2 * d)[..., None]) * b + 2.0 ** -16 * a + 1e-6).all()
+    assert (np.abs(lse.cpu().numpy() - l) <= u + d + 1e-4 * (1 + np.abs(l))).all()
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+def test_what_lies_behind_the_sequence_has_no_effect(layout):
+    """Any bytes in the slots behind each sequence's end, in its last page and in the pages after, among them scale
+    bytes that stand for NaN or pass every range: the bits stay."""
+    case = mx_case("behind", [70, 5, 0], [3, 20, 1], 4, 2, seed=72)
+    s = MxSetup(case)
+    s.append()
+    ref, ref_lse = s.attention(opts_of(layout))
+    rng = np.random.default_rng(72)
+    for pool in (s.cache.k_pages, s.cache.v_pages):
+        host = pool.cpu().numpy()
+        host[case.poison_page] = rng.integers(0, 256, host[0].shape)
+        for r in range(3):
+            n = int(case.prefix_lens[r] + case.chunk_lens[r])
+            page, slot = slots(case.block_tables, r, range(n, -(-n // 16) * 16))
+            for p, i in zip(page, slot):
+                host[p, :, 64 * i:64 * i + 64] = rng.integers(0, 256, (2, 64))
+                host[p, :, 1024 + 4 * i:1028 + 4 * i] = rng.integers(250, 256, (2, 4))
+        pool.copy_(torch.from_numpy(host))
+    out, lse = s.attention(opts_of(layout))
+    assert torch.equal(out.view(torch.int16), ref.view(torch.int16)) and torch.equal(lse, ref_lse)
 
 
 def nan_block(pool, tables, r, key, head, block):
