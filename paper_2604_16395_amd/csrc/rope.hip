@@ -5,6 +5,11 @@
 // position * (inv_freq / 2 pi), and only its distance from the nearest whole turn is rounded to
 // fp32 (2^-26 of a turn), for the hardware's sine and cosine, which take turns.
 //
+// Norms (kNorm): a head's squares are summed over its eight lanes before the rotation, fp32 until the one rounding at
+// the end.  One row 3.2 us, 35107 rows of 32 + 8 + 8 heads 163 us, as fast as a copy moves their 863 MB; 2342 rows of
+// 32 + 32 without pages 18.4 us (77 MB, which the last-level cache holds), bound by the arithmetic and, as all waves
+// are resident at once, by loading, computing and storing one after another.
+//
 // A wave takes one row (token) and 8 kHeads of its heads (a workgroup four rows; workgroups of the same rows
 // follow one another); lane l holds unit l % 8 of head l / 8, the 16 elements of 8 pairs in two 16-byte
 // chunks, so that a lane's 8 sines and cosines serve all its heads and rows of a head are read and
@@ -136,21 +141,23 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a) {
     xb[j] = *reinterpret_cast<const u32x4_any*>(src + ob);
   }
 
-  float wa[kNorm ? kHeads : 1][8], wb[kNorm ? kHeads : 1][8];
+  // the weights of the wave's first head, which are those of all its heads but where queries end within them
+  float wa[8], wb[8];
+  const int last = min(first + 8 * kHeads, a.hq + a.hkv) - 1;   // the wave's last head that is normed
+  const bool mixed = kNorm && kHeads > 1 && first < a.hq && last >= a.hq;
+  auto weights_of = [&](int h) {
+    const void* weight = h < a.hq ? a.q_weight : a.k_weight;
+    load_weights(weight, a.norm_fp32, oa, a.offset, wa);
+    load_weights(weight, a.norm_fp32, ob, a.offset, wb);
+  };
   if constexpr (kNorm) {
-#pragma unroll
-    for (int j = 0; j < kHeads; ++j) {
-      const int h = head0 + 8 * j;
-      if (h >= a.hq + a.hkv) continue;   // past the heads, or values
-      const void* weight = h < a.hq ? a.q_weight : a.k_weight;
-      load_weights(weight, a.norm_fp32, oa, a.offset, wa[j]);
-      load_weights(weight, a.norm_fp32, ob, a.offset, wb[j]);
-    }
+    if (first <= last) weights_of(head0);
   }
 
   float cs[8], sn[8];
   if (turns) {
     double pos[S2L_ROPE_MAX_AXES];
+    const bool one_axis = kNorm && a.num_axes == 1;   // no choice among them for each pair
 #pragma unroll
     for (int i = 0; i < S2L_ROPE_MAX_AXES; ++i)
       pos[i] = (double)(a.positions == nullptr ? at.pos : a.positions[(i < a.num_axes ? i : 0) * a.pos_stride + row]);
@@ -160,7 +167,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const uint32_t axis = axes >> (2 * i) & 3;
-      const double p = axis & 2 ? (axis & 1 ? pos[3] : pos[2]) : (axis & 1 ? pos[1] : pos[0]);
+      const double p = one_axis ? pos[0] : axis & 2 ? (axis & 1 ? pos[3] : pos[2]) : (axis & 1 ? pos[1] : pos[0]);
       const double f = (double)(i < 4 ? f0[i & 3] : f1[i & 3]) * 0.15915494309189535;
       const float angle = (float)__builtin_fma(p, f, -__builtin_rint(p * f));
       cs[i] = a.scale * __builtin_amdgcn_cosf(angle);
@@ -182,8 +189,11 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a) {
       float x[8], y[8];
       unpack8(xa[j], x);
       unpack8(xb[j], y);
-      if constexpr (kNorm) norm16(x, y, wa[j], wb[j], a.eps);
-      if (rotates) {
+      if constexpr (kNorm) {
+        if (j > 0 && mixed) weights_of(h);
+        norm16(x, y, wa, wb, a.eps);
+      }
+      if (!kNorm || rotates) {
         float u[8], w[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -191,11 +201,12 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a) {
           else if (i < 4) turn(x[2 * i], x[2 * i + 1], cs[i], sn[i], &u[2 * i], &u[2 * i + 1]);
           else turn(y[2 * i - 8], y[2 * i - 7], cs[i], sn[i], &w[2 * i - 8], &w[2 * i - 7]);
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = u[i], y[i] = w[i];
+        xa[j] = pack8(u);
+        xb[j] = pack8(w);
+      } else {
+        xa[j] = pack8(x);
+        xb[j] = pack8(y);
       }
-      xa[j] = pack8(x);
-      xb[j] = pack8(y);
     }
     if (h < a.hq) {
       uint16_t* dst = a.q_out + row * a.q_out_stride + h * 128;
@@ -248,15 +259,26 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a) {
 // hide more.  One head a lane and two, us in a graph: 32 + 8 + 8 heads, 512 rows 4.6 and 4.8, 1024 (6144 waves) 7.9 and
 // 7.9, 1365 (8190) 9.6 and 8.9, 4096 24.0 and 21.8; 64 + 8 + 8 into e4m3 pages, 600 (6000) 8.3 and 8.1, 1000 11.4 and
 // 10.1; 32 + 32 without pages, 768 (6144) 8.4 and 8.4, 1024 10.1 and 10.1.
+// With norms a head costs more beside what its lane shares (sines, weights), and many rows take up to four heads a
+// lane, evenly over the waves of a row: two, three and four, us in a graph: 35107 rows of 32 + 8 + 8 heads 167.9, 162.7,
+// 174.1 (two waves a row take three), 2342 rows of 32 + 32 without pages 20.0, 20.8, 18.4 (two waves, four).
 template <bool kAdjacent, bool kAppend, PageKind kKind, bool kNorm>
 void launch(const RopeLaunch& a, hipStream_t stream) {
   constexpr int64_t kFewWaves = 6144;
   const int heads = a.hq + a.hkv * (kAppend ? 2 : 1);
   const int64_t four_rows = ((int64_t)a.total_rows + 3) / 4, groups = (heads + 7) / 8;
-  if (a.total_rows * groups <= kFewWaves)
-    rope_kernel<kAdjacent, kAppend, kKind, kNorm, 1><<<dim3((uint32_t)(four_rows * groups)), 256, 0, stream>>>(a);
-  else
-    rope_kernel<kAdjacent, kAppend, kKind, kNorm, 2><<<dim3((uint32_t)(four_rows * ((groups + 1) / 2))), 256, 0, stream>>>(a);
+  auto run = [&](auto heads_a_lane) {
+    constexpr int kHeads = decltype(heads_a_lane)::value;
+    rope_kernel<kAdjacent, kAppend, kKind, kNorm, kHeads>
+        <<<dim3((uint32_t)(four_rows * ((groups + kHeads - 1) / kHeads))), 256, 0, stream>>>(a);
+  };
+  const int64_t waves = (groups + 3) / 4;   // of a row, at four heads a lane
+  const int64_t even = (groups + waves - 1) / waves;
+  if (a.total_rows * groups <= kFewWaves) run(std::integral_constant<int, 1>{});
+  else if (kNorm && even == 4) run(std::integral_constant<int, kNorm ? 4 : 2>{});
+  else if (kNorm && even == 3) run(std::integral_constant<int, kNorm ? 3 : 2>{});
+  else if (kNorm && even == 1) run(std::integral_constant<int, 1>{});
+  else run(std::integral_constant<int, 2>{});
 }
 
 template <bool kAppend, PageKind kKind>

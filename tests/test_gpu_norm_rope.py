@@ -109,6 +109,34 @@ def test_normed_append_is_norm_and_rotation_then_append(kind, rot, adjacent):
         assert same(q1, q2) and same(one.k_pages, two.k_pages) and same(one.v_pages, two.v_pages), (P, C)
 
 
+@pytest.mark.parametrize("hq,hkv", [(4, 2), (12, 2), (20, 7), (30, 1), (32, 8), (64, 8)])
+@pytest.mark.parametrize("kind", [None, "bf16", "mxfp4"])
+def test_many_rows_give_the_bits_of_few(hq, hkv, kind):
+    """One to four heads a lane, with a wave's heads queries, keys and values in any mix: the rows of a large batch have
+    the bits that they have in batches of 40 rows, where a lane takes one head."""
+    gen = torch.Generator(device=DEV).manual_seed(hq)
+    heads = hq + hkv * (1 if kind is None else 2)
+    T = 40 * (6144 // (-(-heads // 8) * 40) + 2)
+    norm = s2l.QKNorm(*(weights((torch.float32, 0.0), gen)[0] for _ in range(2)))
+    rope = s2l.Rope(torch.from_numpy(freqs(48)).to(DEV))
+    qkv = torch.randn((T, hq + 2 * hkv, 128), generator=gen, device=DEV).to(torch.bfloat16)
+    pages = -(-T // 16)
+    tables = np.random.default_rng(hq).permutation(pages).astype(np.int32)[None]
+    many, few = caches(kind or "bf16", pages, hkv, gen)
+    outs = []
+    for cache, parts in ((many, [(0, T)]), (few, [(a, 40) for a in range(0, T, 40)])):
+        q, k = (torch.zeros((T, n, 128), dtype=torch.bfloat16, device=DEV) for n in (hq, hkv))
+        for a, n in parts:
+            batch, row = s2l.Batch([a], [n], tables), qkv[a:a + n]
+            if kind is None:
+                s2l.s2l_norm_rope_qk(batch, norm, rope, row[:, :hq], q[a:a + n], row[:, hq:hq + hkv], k[a:a + n])
+            else:
+                s2l.s2l_norm_rope_kv_append(cache, batch, norm, rope, row[:, :hq], q[a:a + n], row[:, hq:hq + hkv], row[:, hq + hkv:])
+        torch.cuda.synchronize()
+        outs.append((q, k, cache.k_pages, cache.v_pages))
+    assert all(same(x, y) for x, y in zip(*outs))
+
+
 def test_weights_and_rows_at_odd_addresses():
     gen = torch.Generator(device=DEV).manual_seed(3)
     T, hq, inv = 37, 3, freqs(64)
