@@ -43,20 +43,6 @@ __global__ __launch_bounds__(256) void kv_append_kernel(
   if constexpr (kKind == kBf16Pages) {
     *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(kpool) + dst) = kx;
     *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(vpool) + dst) = vx;
-  } else if constexpr (kKind == kMxfp4Pages) {
-    // four lanes hold a block of 32 dims (a row's 16 lanes are all here or none)
-    uint32_t m = max_magnitude(kx) | max_magnitude(vx) << 16;
-    m = max_u16x2(m, lane_xor1(m));
-    m = max_u16x2(m, lane_xor2(m));
-    const uint32_t kb = mx_scale_byte(m & 0xFFFFu), vb = mx_scale_byte(m >> 16);
-    uint8_t* kr = static_cast<uint8_t*>(kpool) + run * kMxRunBytes;
-    uint8_t* vr = static_cast<uint8_t*>(vpool) + run * kMxRunBytes;
-    *reinterpret_cast<uint32_t*>(kr + slot * kMxCodeBytes + 4 * c) = mx_encode8(kx, kb);
-    *reinterpret_cast<uint32_t*>(vr + slot * kMxCodeBytes + 4 * c) = mx_encode8(vx, vb);
-    if ((c & 3) == 0) {
-      kr[kMxScalesAt + slot * kMxScaleBytes + (c >> 2)] = (uint8_t)kb;
-      vr[kMxScalesAt + slot * kMxScaleBytes + (c >> 2)] = (uint8_t)vb;
-    }
   } else {
     // code = e4m3(fp32(x) * fp32(1/scale[h])), RNE, saturated
     const float ki = __fdiv_rn(1.0f, kscale[h]);
@@ -69,6 +55,54 @@ __global__ __launch_bounds__(256) void kv_append_kernel(
     *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(kpool) + dst) = kq;
     *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(vpool) + dst) = vq;
   }
+}
+
+// MXFP4: the same for kMxHeads heads of a page, whose rows a thread loads before it encodes the first.  Four lanes
+// hold a block of 32 dims (a row's 16 lanes are all there or none): its largest magnitude sets the scale.  One row 2.4 us
+// (2.6 with a workgroup a head, 3.0 with four heads a workgroup), 35107 rows of 8 heads, 182 MB, 37 us (40 and 40).
+constexpr int kMxHeads = 2;
+__global__ __launch_bounds__(256) void kv_append_mxfp4_kernel(
+    const int32_t* __restrict__ prefix_lens, const int32_t* __restrict__ chunk_lens,
+    const int32_t* __restrict__ cu_chunk, const int32_t* __restrict__ block_tables, int32_t max_pages, int32_t hkv,
+    const uint16_t* __restrict__ knew, const uint16_t* __restrict__ vnew, uint8_t* __restrict__ kpool,
+    uint8_t* __restrict__ vpool) {
+  const int r = blockIdx.z, h0 = blockIdx.y * kMxHeads;
+  const int P = prefix_lens[r], C = chunk_lens[r], row0 = cu_chunk[r];
+  __asm__ volatile("" ::"s"(P), "s"(C), "s"(row0), "s"(kpool), "s"(vpool));
+  if (C <= 0) return;
+  const int lp = (P >> 4) + (int)blockIdx.x;
+  if (lp > ((P + C - 1) >> 4)) return;
+  const int slot = threadIdx.x >> 4, c = threadIdx.x & 15;
+  const int pos = lp * 16 + slot;
+  if (pos < P || pos >= P + C) return;
+  const int64_t page = block_tables[(int64_t)r * max_pages + lp];
+  const int64_t src = ((int64_t)(row0 + pos - P) * hkv + h0) * 128 + c * 8;
+  const int heads = hkv - h0 < kMxHeads ? hkv - h0 : kMxHeads;
+  u32x4 kx[kMxHeads], vx[kMxHeads];
+#pragma unroll
+  for (int j = 0; j < kMxHeads; ++j)
+    if (j < heads) {
+      kx[j] = *reinterpret_cast<const u32x4*>(knew + src + j * 128);
+      vx[j] = *reinterpret_cast<const u32x4*>(vnew + src + j * 128);
+    }
+  const int64_t run = (page * hkv + h0) * kMxRunBytes;
+  const int codes = slot * kMxCodeBytes + 4 * c, scale = kMxScalesAt + slot * kMxScaleBytes + (c >> 2);
+#pragma unroll
+  for (int j = 0; j < kMxHeads; ++j)
+    if (j < heads) {
+      uint32_t m = max_magnitude(kx[j]) | max_magnitude(vx[j]) << 16;
+      m = max_u16x2(m, lane_xor1(m));
+      m = max_u16x2(m, lane_xor2(m));
+      const uint32_t kb = mx_scale_byte(m & 0xFFFFu), vb = mx_scale_byte(m >> 16);
+      uint8_t* kr = kpool + run + j * kMxRunBytes;
+      uint8_t* vr = vpool + run + j * kMxRunBytes;
+      *reinterpret_cast<uint32_t*>(kr + codes) = mx_encode8(kx[j], kb);
+      *reinterpret_cast<uint32_t*>(vr + codes) = mx_encode8(vx[j], vb);
+      if ((c & 3) == 0) {
+        kr[scale] = (uint8_t)kb;
+        vr[scale] = (uint8_t)vb;
+      }
+    }
 }
 
 // Gather: rows cu_out[r] + p (p < n_r) <- stored elements of position p.  kEB = element bytes.
@@ -129,9 +163,54 @@ __global__ __launch_bounds__(256) void kv_gather_mxfp4_kernel(
   }
 }
 
-// Values: row cu_out[r] + i receives position begin + i of request r as bf16.  Workgroup (page of the
-// part, request); thread by thread eight dims of a row of a head, 16 bytes out, in the order of the
-// output rows.  Bound by writing them.
+// Values: row cu_out[r] + i receives position begin + i of request r as bf16.  Workgroup (page of the part, request);
+// a thread's unit is eight dims of a row of a head, 16 bytes out, in the order of the output rows; it loads
+// kReadUnits of them, K and V, before it stores the first, and stores past the caches: the output is four times what
+// is read.  Bound by the memory, mostly written: 88219 MXFP4 rows of 8 heads, 457 MB, 103 us (a copy that moves as
+// much takes 84); 110 with one unit at a time, 107 with a page's units in turns by one workgroup.
+template <PageKind kKind>
+struct ReadUnit {   // as loaded: widened when it is stored
+  uint32_t x[kKind == kBf16Pages ? 4 : kKind == kE4m3Pages ? 2 : 1];
+  float scale;
+};
+template <PageKind kKind>
+__device__ inline ReadUnit<kKind> read_unit(const void* pool, const float* scale, int64_t run, int h, int slot, int c) {
+  ReadUnit<kKind> u;
+  if constexpr (kKind == kMxfp4Pages) {
+    const uint8_t* p = static_cast<const uint8_t*>(pool) + run * kMxRunBytes;
+    u.x[0] = *reinterpret_cast<const uint32_t*>(p + slot * kMxCodeBytes + 4 * c);
+    u.scale = mx_scale(p[kMxScalesAt + slot * kMxScaleBytes + (c >> 2)]);
+  } else if constexpr (kKind == kE4m3Pages) {
+    const u32x2 x = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(pool) + (run * 16 + slot) * 128 + 8 * c);
+    u.x[0] = x[0], u.x[1] = x[1];
+    u.scale = scale[h];
+  } else {
+    const u32x4 x = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(pool) + (run * 16 + slot) * 128 + 8 * c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u.x[i] = x[i];
+    u.scale = 1.f;
+  }
+  return u;
+}
+template <PageKind kKind>
+__device__ inline u32x4 unit_values(const ReadUnit<kKind>& u) {
+  if constexpr (kKind == kMxfp4Pages) {
+    return fp4x8_to_bf16x8(u.x[0], u.scale);
+  } else if constexpr (kKind == kE4m3Pages) {
+    u32x4 y;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const u32x2 w = fp8x4_to_bf16x4(u.x[i]);
+      y[2 * i] = pack_bf16x2(bf16lo(w[0]) * u.scale, bf16hi(w[0]) * u.scale);
+      y[2 * i + 1] = pack_bf16x2(bf16lo(w[1]) * u.scale, bf16hi(w[1]) * u.scale);
+    }
+    return y;
+  } else {
+    return u32x4{u.x[0], u.x[1], u.x[2], u.x[3]};
+  }
+}
+
+constexpr int kReadUnits = 2;
 template <PageKind kKind>
 __global__ __launch_bounds__(256) void kv_read_kernel(
     const void* __restrict__ kpool, const void* __restrict__ vpool, const float* __restrict__ kscale,
@@ -146,41 +225,34 @@ __global__ __launch_bounds__(256) void kv_read_kernel(
   const int lp = (begin >> 4) + (int)blockIdx.x;
   if (lp * 16 >= end) return;
   const int64_t page = block_tables[(int64_t)r * max_pages + lp];
-  for (int u = threadIdx.x; u < hkv * 256; u += 256) {
-    const int c = u & 15, h = (u >> 4) % hkv, slot = (u >> 4) / hkv;
-    const int pos = lp * 16 + slot;
-    const int64_t row = row0 + pos - begin;
-    if (pos < begin || pos >= end || row < 0 || row >= out_rows) continue;
-    const int64_t run = page * hkv + h;
-    u32x4 k, v;
-    if constexpr (kKind == kMxfp4Pages) {
-      const uint8_t* kr = static_cast<const uint8_t*>(kpool) + run * kMxRunBytes;
-      const uint8_t* vr = static_cast<const uint8_t*>(vpool) + run * kMxRunBytes;
-      const int at = slot * kMxCodeBytes + 4 * c, sc = kMxScalesAt + slot * kMxScaleBytes + (c >> 2);
-      k = fp4x8_to_bf16x8(*reinterpret_cast<const uint32_t*>(kr + at), mx_scale(kr[sc]));
-      v = fp4x8_to_bf16x8(*reinterpret_cast<const uint32_t*>(vr + at), mx_scale(vr[sc]));
-    } else if constexpr (kKind == kE4m3Pages) {
-      const int64_t at = (run * 16 + slot) * 128 + 8 * c;
-      auto value = [](const void* pool, int64_t at, float scale) {
-        const u32x2 x = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(pool) + at);
-        u32x4 y;
-        for (int i = 0; i < 2; ++i) {
-          const u32x2 w = fp8x4_to_bf16x4(x[i]);
-          y[2 * i] = pack_bf16x2(bf16lo(w[0]) * scale, bf16hi(w[0]) * scale);
-          y[2 * i + 1] = pack_bf16x2(bf16lo(w[1]) * scale, bf16hi(w[1]) * scale);
-        }
-        return y;
-      };
-      k = value(kpool, at, kscale[h]);
-      v = value(vpool, at, vscale[h]);
-    } else {
-      const int64_t at = (run * 16 + slot) * 128 + 8 * c;
-      k = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(kpool) + at);
-      v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(vpool) + at);
+  // the slots that have a row: positions of the part whose rows are within the output
+  const int64_t base = row0 + lp * 16 - begin;   // the row of slot 0
+  auto clamp = [](int64_t x) { return (int)(x < 0 ? 0 : x > 16 ? 16 : x); };
+  const int first = max(clamp(begin - lp * 16), clamp(-base));
+  const int past = min(clamp(end - lp * 16), clamp(out_rows - base));
+  const int units = (past - first) * hkv * 16;
+  const int64_t dst = (base + first) * hkv * 128;
+  // gridDim.z workgroups take the page's units in one turn each
+  for (int u0 = threadIdx.x + (int)blockIdx.z * (256 * kReadUnits); u0 < units; u0 += 256 * kReadUnits * (int)gridDim.z) {
+    ReadUnit<kKind> k[kReadUnits], v[kReadUnits];
+#pragma unroll
+    for (int j = 0; j < kReadUnits; ++j) {
+      const int u = u0 + 256 * j;
+      if (u < units) {
+        const int c = u & 15, h = (u >> 4) % hkv, slot = first + (u >> 4) / hkv;
+        const int64_t run = page * hkv + h;
+        k[j] = read_unit<kKind>(kpool, kscale, run, h, slot, c);
+        v[j] = read_unit<kKind>(vpool, vscale, run, h, slot, c);
+      }
     }
-    const int64_t dst = (row * hkv + h) * 128 + 8 * c;
-    *reinterpret_cast<u32x4*>(kout + dst) = k;
-    *reinterpret_cast<u32x4*>(vout + dst) = v;
+#pragma unroll
+    for (int j = 0; j < kReadUnits; ++j) {
+      const int u = u0 + 256 * j;
+      if (u < units) {
+        __builtin_nontemporal_store(unit_values<kKind>(k[j]), reinterpret_cast<u32x4*>(kout + dst + (int64_t)u * 8));
+        __builtin_nontemporal_store(unit_values<kKind>(v[j]), reinterpret_cast<u32x4*>(vout + dst + (int64_t)u * 8));
+      }
+    }
   }
 }
 
@@ -258,13 +330,21 @@ hipError_t launch_kv_append(const KvLaunch& a, const void* knew, const void* vne
                             hipStream_t stream) {
   if (a.num_reqs == 0 || max_pages_touched == 0) return hipSuccess;
   dim3 grid(max_pages_touched, a.hkv, a.num_reqs);
+  if (a.kind == kMxfp4Pages) {
+    grid.y = (a.hkv + kMxHeads - 1) / kMxHeads;
+    kv_append_mxfp4_kernel<<<grid, 256, 0, stream>>>(a.prefix_lens, a.chunk_lens, a.cu_chunk, a.block_tables, a.max_pages, a.hkv,
+                                                     static_cast<const uint16_t*>(knew), static_cast<const uint16_t*>(vnew),
+                                                     static_cast<uint8_t*>(a.kpool), static_cast<uint8_t*>(a.vpool));
+    return hipGetLastError();
+  }
   auto launch = [&](auto kind) {
     constexpr PageKind kKind = decltype(kind)::value;
     kv_append_kernel<kKind><<<grid, 256, 0, stream>>>(a.prefix_lens, a.chunk_lens, a.cu_chunk, a.block_tables, a.max_pages,
                                                       a.hkv, static_cast<const uint16_t*>(knew),
                                                       static_cast<const uint16_t*>(vnew), a.kpool, a.vpool, a.kscale, a.vscale);
   };
-  with_kind(a.kind, launch);
+  if (a.kind == kE4m3Pages) launch(std::integral_constant<PageKind, kE4m3Pages>{});
+  else launch(std::integral_constant<PageKind, kBf16Pages>{});
   return hipGetLastError();
 }
 
@@ -281,7 +361,7 @@ hipError_t launch_kv_gather(const KvLaunch& a, int32_t include_chunk, const int3
 hipError_t launch_kv_read(const KvLaunch& a, bool skip_prefix, bool with_chunk, const int32_t* cu_out, void* kout, void* vout,
                           int64_t out_rows, int32_t max_pages_read, hipStream_t stream) {
   if (a.num_reqs == 0 || max_pages_read == 0 || out_rows == 0) return hipSuccess;
-  dim3 grid(max_pages_read, a.num_reqs);
+  dim3 grid(max_pages_read, a.num_reqs, (a.hkv + kReadUnits - 1) / kReadUnits);
   auto launch = [&](auto kind) {
     constexpr PageKind kKind = decltype(kind)::value;
     kv_read_kernel<kKind><<<grid, 256, 0, stream>>>(a.kpool, a.vpool, a.kscale, a.vscale, static_cast<uint16_t*>(kout),
