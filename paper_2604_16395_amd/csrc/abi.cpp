@@ -558,6 +558,11 @@ s2l_status attn_launch(const s2l_kv_cache* cache, const s2l_batch* batch, const 
   a.tile_cols = plan->tile_cols;
   a.key_halves = plan->key_halves;
   a.uniform = (plan->flags & S2L_PLAN_UNIFORM) != 0;
+  a.binned = (plan->flags & S2L_PLAN_BINNED) != 0;
+  a.longest_keys = 0;
+  for (int32_t r = 0; r < batch->num_reqs; ++r)
+    a.longest_keys = std::max(a.longest_keys, batch->prefix_lens_host[r] + batch->chunk_lens_host[r]);
+  if (plan->split_keys > 0) a.longest_keys = std::min(a.longest_keys, plan->split_keys);
   a.group_by_xcd = (plan->flags & (S2L_PLAN_UNIFORM | S2L_PLAN_BINNED)) != 0;
   a.knew = k_new;
   a.vnew = v_new;

@@ -446,7 +446,16 @@ void launch_decode_kind(const AttnLaunch& a, hipStream_t stream) {
   // which latency bounds, would gain from two: 433 rows of 372 keys (16q/16kv) 257 us with one, 233 with
   // two, 922 of up to 30 (32q/8kv) 86 and 51.  Not used: the line between these and the long unequal
   // ones, by length and by inequality, is not measured.
-  const unsigned pad = kKind != kBf16Pages && a.uniform ? 0 : kOneWorkgroupLds - (kKind != kBf16Pages ? 64u : 34u) * 1024;
+  // MXFP4, whose ranges are four times as many keys for the same bytes: two a CU, but for long binned items that are
+  // one to three rounds of the CUs, where the short ones that double up hold the longest back.  Two against one a CU,
+  // 158 batches of 16 to 400 rows (64q/8kv, 32q/8kv, 16q/2kv, 8q/1kv) of 700 to 48000 keys: equal items and one round
+  // of any the same to 3%, 128 to 400 rows of up to 700 keys 0.63 to 0.78 of the time, of up to 6000 0.88 to 0.94; 48 rows of
+  // 8 heads binned (384 items) up to 1500 keys 0.95, 3000 1.10, 24000 1.15; 64 rows (512) 1000 0.80, 2000 0.91, 4000 1.02,
+  // 16000 1.18; 128 rows (1024) 12000 0.99, 24000 1.02.
+  constexpr int kLongKeys = 2048, kFewItems = 3 * 256;
+  const bool two = kKind == kMxfp4Pages ? a.uniform || !a.binned || a.longest_keys <= kLongKeys || a.dims.num_items > kFewItems
+                                        : kKind == kE4m3Pages && a.uniform;
+  const unsigned pad = two ? 0 : kOneWorkgroupLds - (kKind != kBf16Pages ? 64u : 34u) * 1024;
   const PlanPtrs pv = plan_ptrs(a.workspace, a.dims);
   const int32_t g = a.hq / a.kv.hkv;
   const uint32_t ginv = ((1u << 24) + (uint32_t)g - 1) / (uint32_t)g;

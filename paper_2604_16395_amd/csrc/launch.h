@@ -88,6 +88,8 @@ struct AttnLaunch {
   int32_t key_halves;       // 1 or 2 wave groups per item, each on half of its key range
   bool uniform;             // items of near-equal cost
   bool group_by_xcd;        // items of near-equal cost: consecutive items onto one XCD
+  bool binned;              // the plan's items are binned by XCD
+  int32_t longest_keys;     // of an item, at most
   const void* knew = nullptr;   // fused append (bf16, page-aligned prefixes): the chunk's
   const void* vnew = nullptr;   //   new K/V rows [T][Hkv][128], else null
   bool q8 = false;              // e4m3 pages: Q quantised per column, S on the fp8 MFMA
