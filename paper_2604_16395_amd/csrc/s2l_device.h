@@ -113,17 +113,19 @@ __device__ inline QueryTerms split_queries(const u32x4& a, const u32x4& b, const
   // the exponent of (largest x factor), each taken as a number in [1, 2) and a power of two: no overflow on the way
   const uint32_t f = f2u(factor);
   const float top = u2f((m << 16 & 0x7FFFFFu) | 0x3F800000u) * u2f((f & 0x7FFFFFu) | 0x3F800000u);
-  const int e = (int)(m >> 7) + (int)(f >> 23) - 127 + (top >= 2.f) - 2;
-  const int s = e < 9 ? 9 : e > 254 ? 254 : e;   // below: all of it leaves scores of 2^-100 and less
-  const float scale = u2f((f & 0x7FFFFFu) | 0x3F800000u);
-  const int shift = (int)(f >> 23) - s;          // factor q 2^(127 - s) = scale (q 2^shift)
+  const int fe = (int)(f >> 23), e = (int)(m >> 7) + fe - 127 + (top >= 2.f) - 2;
+  // at least 9, for the third value's byte, and what keeps the multiplier finite: queries that this makes
+  // smaller than [4, 8) are below 2^-120
+  const int least = fe - 126 > 9 ? fe - 126 : 9;
+  const int s = e < least ? least : e > 254 ? 254 : e;
+  const float times = __builtin_ldexpf(u2f((f & 0x7FFFFFu) | 0x3F800000u), fe - s);   // factor 2^(127 - s)
   float y[32];
   f16x32 left;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const uint32_t w = i < 4 ? a[i & 3] : i < 8 ? b[i & 3] : i < 12 ? c[i & 3] : d[i & 3];
-    y[2 * i] = __builtin_ldexpf(bf16lo(w), shift) * scale;
-    y[2 * i + 1] = __builtin_ldexpf(bf16hi(w), shift) * scale;
+    y[2 * i] = bf16lo(w) * times;
+    y[2 * i + 1] = bf16hi(w) * times;
   }
 #pragma unroll
   for (int i = 0; i < 32; ++i) left[i] = (_Float16)y[i];
