@@ -51,10 +51,11 @@
 // by v_mfma_scale_f32_32x32x64_f8f6f4, which takes E2M1 against E2M3 at twice the rate of bf16: the queries, times
 // the softmax's factor, go as three E2M3 values each (s2l_device.h; 192 cycles a sub-block instead of 256), and -m is
 // what the score MFMAs start from, so their results are the exponents.  V is widened to bf16 on the way into LDS.
-// A layer of P = 131072, C = 2048 (8q/1kv) takes 815 us, 1360 TFLOP/s; 900 with K widened to bf16, 860 before
-// NaNs of V were kept in a register and pages copied past the range's end.  The loop's MFMA and VALU instructions
-// hardly overlap (MFMA 49% busy, VALU the rest), so each fma or cycle of MFMA that is left out counts.  The queries'
-// terms cost a workgroup 0.8 us before its first tile (600 tokens without prefix, 32q/8kv: 16.7 -> 17.5 us).
+// A layer of P = 131072, C = 2048 (8q/1kv) takes 0.80 to 0.83 ms (boxes differ), 1340 to 1390 TFLOP/s, above what a
+// bf16 product of 8192^3 reaches; K widened to bf16 took 1.12 times as long, three E2M3 terms without the factor
+// and -m in them 1.07 times.  The loop's MFMA and VALU instructions hardly overlap (with the terms alone MFMA was
+// busy 49% of the cycles, VALU most of the others, at 1.7 to 1.9 GHz), so each fma or cycle of MFMA that is left out
+// counts.  The queries' terms cost a workgroup 0.5 us before its first tile (600 tokens without prefix, 32q/8kv: 17.2 us).
 //
 // Quantised-Q variant (e4m3 pages only): each lane pair encodes its column of Q to e4m3 with
 // the column's own scale, K's codes stay e4m3 in LDS (same permuted chunk positions), and the
@@ -642,6 +643,8 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
     vf[0] = f.v[0];
     vf[1] = f.v[1];
     float l0 = 0.f, l1 = 0.f;
+    // MXFP4: a wave within a step goes before one that settles, masks or stages V: another two percent
+    if constexpr (kMx) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if (i + 2 < 8) {
@@ -672,6 +675,7 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
       else l0 = sum_bf16x2(pk, l0);
       if (i == 1) hook();
     }
+    if constexpr (kMx) __builtin_amdgcn_s_setprio(0);
     lsum = l0 + l1;
     __asm__ volatile("" ::"v"(po[0]), "v"(po[1]), "v"(lsum));   // produced here, not sunk
     if constexpr (kMx) {
