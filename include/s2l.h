@@ -358,7 +358,7 @@ s2l_status s2l_kv_gather(const s2l_kv_cache* cache, const s2l_batch* batch, int3
  * bf16 and MXFP4 values are exact (MXFP4 scale bytes 253 and 254 excepted); e4m3 ones are
  * decode(code) * scale in fp32, rounded to bf16 (attention keeps the scale apart and rounds nothing).
  * Errors: EINVAL (nulls, negative lengths, part, alignment), ERANGE (P_r + C_r > max_pages_per_req * 16),
- * ENOTSUP (head_dim/page_size, more than 65535 requests), EHIP.
+ * ENOTSUP (head_dim/page_size, more than 65535 requests or kv heads, or 2^28 positions of a request), EHIP.
  */
 #define S2L_READ_PREFIX 0
 #define S2L_READ_ALL 1
@@ -456,7 +456,8 @@ s2l_status s2l_attn_plan(const s2l_batch* batch, int32_t num_q_heads, int32_t nu
  * within about 2^-7 sum_j w_j |V_j - out| + 2^-8 |out| of the exact result; lse is the
  * log of the sum of those bf16 weights (within about 2^-8 of the exact value).  Over an MXFP4 cache tiles of 128
  * and 256 columns take each q within 2^-13 of the largest magnitude among its 32 dims (32 b .. 32 b + 31 of a
- * row), which moves s_j by at most 2^-13 softmax_scale sum |that magnitude K|; softmax_scale |q| < 2^100.
+ * row; of 2^-110 / softmax_scale where that is more), which moves s_j by at most 2^-13 softmax_scale
+ * sum |that magnitude K|; there softmax_scale |q| has to stay below 2^100.
  *   q   : device bf16 [T][Hq][128] (post-RoPE).     out : device bf16 [T][Hq][128].
  *   lse : device fp32 [T][Hq] or NULL.               softmax_scale > 0 (e.g. 1/sqrt(128)).
  *   plan: the s2l_plan_info returned by s2l_attn_plan for this batch and head counts.

@@ -559,8 +559,8 @@ s2l_status attn_launch(const s2l_kv_cache* cache, const s2l_batch* batch, const 
   a.key_halves = plan->key_halves;
   a.uniform = (plan->flags & S2L_PLAN_UNIFORM) != 0;
   a.binned = (plan->flags & S2L_PLAN_BINNED) != 0;
-  a.longest_keys = 0;
-  for (int32_t r = 0; r < batch->num_reqs; ++r)
+  a.longest_keys = 0;   // for decode tiles over MXFP4 pages alone
+  for (int32_t r = 0; r < batch->num_reqs && plan->tile_cols == s2l::kDecodeTileCols && a.kv.kind == s2l::kMxfp4Pages; ++r)
     a.longest_keys = std::max(a.longest_keys, batch->prefix_lens_host[r] + batch->chunk_lens_host[r]);
   if (plan->split_keys > 0) a.longest_keys = std::min(a.longest_keys, plan->split_keys);
   a.group_by_xcd = (plan->flags & (S2L_PLAN_UNIFORM | S2L_PLAN_BINNED)) != 0;
@@ -992,7 +992,8 @@ s2l_status s2l_kv_read(const s2l_kv_cache* cache, const s2l_batch* batch, int32_
   if ((st = check_batch(batch, true, &T)) != S2L_OK) return st;
   if (part != S2L_READ_PREFIX && part != S2L_READ_ALL && part != S2L_READ_CHUNK)
     return fail(S2L_EINVAL, "unknown part %d", part);
-  if (batch->num_reqs > 65535) return fail(S2L_ENOTSUP, "kv_read supports at most 65535 requests");
+  if (batch->num_reqs > 65535 || cache->num_kv_heads > 65535)
+    return fail(S2L_ENOTSUP, "kv_read supports at most 65535 requests and kv heads");
   if (out_rows < 0) return fail(S2L_EINVAL, "out_rows %lld < 0", (long long)out_rows);
   const bool skip_prefix = part == S2L_READ_CHUNK, with_chunk = part != S2L_READ_PREFIX;
   int32_t max_read = 0;
@@ -1000,6 +1001,7 @@ s2l_status s2l_kv_read(const s2l_kv_cache* cache, const s2l_batch* batch, int32_
     const int32_t p = batch->prefix_lens_host[r], n = p + (with_chunk ? batch->chunk_lens_host[r] : 0), b = skip_prefix ? p : 0;
     if (n > b) max_read = std::max(max_read, (n - 1) / s2l::kPageSize - b / s2l::kPageSize + 1);
   }
+  if (max_read >= 1 << 24) return fail(S2L_ENOTSUP, "kv_read supports at most 2^28 positions of a request");
   if (max_read > 0 && out_rows > 0 && (!cu_out || !k_out || !v_out)) return fail(S2L_EINVAL, "cu_out/k_out/v_out is NULL");
   if (reinterpret_cast<uintptr_t>(k_out) % 16 != 0 || reinterpret_cast<uintptr_t>(v_out) % 16 != 0)
     return fail(S2L_EINVAL, "k_out and v_out must be aligned to 16 bytes");

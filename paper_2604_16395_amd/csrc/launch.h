@@ -89,7 +89,7 @@ struct AttnLaunch {
   bool uniform;             // items of near-equal cost
   bool group_by_xcd;        // items of near-equal cost: consecutive items onto one XCD
   bool binned;              // the plan's items are binned by XCD
-  int32_t longest_keys;     // of an item, at most
+  int32_t longest_keys;     // of an item, at most (16-column tiles over MXFP4 pages)
   const void* knew = nullptr;   // fused append (bf16, page-aligned prefixes): the chunk's
   const void* vnew = nullptr;   //   new K/V rows [T][Hkv][128], else null
   bool q8 = false;              // e4m3 pages: Q quantised per column, S on the fp8 MFMA

@@ -188,6 +188,39 @@ def test_what_lies_behind_the_sequence_has_no_effect(layout):
     assert torch.equal(out.view(torch.int16), ref.view(torch.int16)) and torch.equal(lse, ref_lse)
 
 
+@pytest.mark.parametrize("offset", [1, 4])
+@pytest.mark.parametrize("layout", LAYOUTS)
+def test_q_and_out_of_a_view_between_16_byte_boundaries(layout, offset):
+    for hq, hkv in ((2, 2), (7, 1)):
+        tq = layout[0] // (hq // hkv)
+        case = mx_case("views", [100, 0], [tq + 1, tq], hq, hkv, seed=73)
+        s = MxSetup(case)
+        s.append()
+        T = case.total_tokens
+        ref, ref_lse = s.attention(opts_of(layout))
+        n = T * hq * 128
+        q = torch.empty(n + offset, dtype=torch.bfloat16, device=DEV)[offset:].view(T, hq, 128).copy_(s.q)
+        out = torch.full((n + offset,), float("nan"), dtype=torch.bfloat16, device=DEV)[offset:].view(T, hq, 128)
+        lse = torch.empty_like(ref_lse)
+        s2l.s2l_chunk_prefill_attn(s.cache, s.batch, q, hq, SCALE, out, lse, s.plan, s._ws)
+        torch.cuda.synchronize()
+        assert torch.equal(out.view(torch.int16), ref.view(torch.int16)) and torch.equal(lse, ref_lse)
+
+
+@pytest.mark.parametrize("R,hi", [(70, 4096), (100, 900), (300, 64)])
+def test_decode_batches_of_every_residency(R, hi):
+    """Binned, sorted and equal items, long and short, so that one workgroup a CU and two are run; a sample of rows."""
+    rng = np.random.default_rng(R)
+    P = rng.integers(1, hi, R)
+    case = mx_case("rounds", P, [1] * R, 32, 8, seed=R)
+    s = MxSetup(case)
+    s.append()
+    out, lse = s.attention()
+    rows = {r: [0] for r in rng.choice(R, 24, replace=False).tolist() + [int(P.argmax()), int(P.argmin())]}
+    assert s.plan.tile_cols == 16
+    assert_attention_close(case, out, lse, s.oracle(sample_rows=rows), rows, what=f"{R} rows")
+
+
 def nan_block(pool, tables, r, key, head, block):
     page, slot = slots(tables, r, [key])
     pool[page[0], head, 1024 + 4 * slot[0] + block] = 255

@@ -108,7 +108,10 @@ def test_reads_of_bad_batches():
     for P, C, status in (([-1], [4], EINVAL), ([0], [-1], EINVAL), ([1000], [25], ERANGE), ([0] * 65536, [0] * 65536, ENOTSUP)):
         b, keep = _batch(P, C)
         assert _read(_cache(dtype=2), b)[0] == status
+    b, keep = _batch([1 << 28], [1], max_pages=1 << 25)
+    assert _read(_cache(dtype=2), b)[0] == ENOTSUP
     b, keep = _batch([3], [4])
+    assert _read(_cache(dtype=2, hkv=65536), b)[0] == ENOTSUP
     assert _read(None, b)[0] == EINVAL and _read(_cache(), None)[0] == EINVAL
     b.block_tables = None
     assert _read(_cache(), b)[0] == EINVAL
