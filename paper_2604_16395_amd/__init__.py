@@ -91,15 +91,19 @@ class PagedKVCache:
         if fp8:
             _check(k_scale, torch.float32, "k_scale")
             _check(v_scale, torch.float32, "v_scale")
-        if mxfp4:
-            if k_pages.shape[2] != MXFP4_RUN_BYTES or v_pages.shape != k_pages.shape:
-                raise ValueError(f"MXFP4 pools must be [num_pages][Hkv][{MXFP4_RUN_BYTES}] of one shape (got "
-                                 f"{tuple(k_pages.shape)} and {tuple(v_pages.shape)})")
-            if k_scale is not None or v_scale is not None:
-                raise ValueError("MXFP4 pools hold their scales: k_scale and v_scale must be None")
+        if mxfp4 and (k_scale is not None or v_scale is not None):
+            raise ValueError("MXFP4 pools hold their scales: k_scale and v_scale must be None")
         self.k_pages, self.v_pages = k_pages, v_pages
         self.k_scale, self.v_scale = k_scale, v_scale
         self.fp8, self.mxfp4 = fp8, mxfp4
+        if mxfp4:
+            self._check_runs()
+
+    def _check_runs(self):
+        k, v = self.k_pages, self.v_pages
+        if k.dim() != 3 or k.shape[2] != MXFP4_RUN_BYTES or v.shape != k.shape or k.dtype != torch.uint8 or v.dtype != torch.uint8:
+            raise ValueError(f"MXFP4 pools must be uint8 [num_pages][Hkv][{MXFP4_RUN_BYTES}] of one shape (got "
+                             f"{k.dtype} {tuple(k.shape)} and {v.dtype} {tuple(v.shape)})")
 
     @property
     def num_pages(self):
@@ -110,6 +114,8 @@ class PagedKVCache:
         return self.k_pages.shape[1]
 
     def c(self):
+        if self.mxfp4:
+            self._check_runs()     # the attributes may be others by now
         return _lib.s2l_kv_cache(
             k_pages=self.k_pages.data_ptr(), v_pages=self.v_pages.data_ptr(),
             k_scale=self.k_scale.data_ptr() if self.fp8 else None,

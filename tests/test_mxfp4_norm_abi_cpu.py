@@ -128,6 +128,12 @@ def test_the_package_s_pools():
                      (torch.zeros((3, 2, 2 * s2l.MXFP4_RUN_BYTES), dtype=torch.uint8)[..., ::2], pool, {})):
         with pytest.raises(ValueError):
             s2l.PagedKVCache(k, v, **kw)
+    cache.v_pages = pool[:2]          # set later: found by the next call
+    with pytest.raises(ValueError):
+        cache.c()
+    cache.k_pages = cache.v_pages = torch.zeros((3, 2, 16, 128), dtype=torch.uint8)
+    with pytest.raises(ValueError):
+        cache.c()
 
 
 def test_the_package_s_norms():
