@@ -163,11 +163,12 @@ __global__ __launch_bounds__(256) void kv_gather_mxfp4_kernel(
   }
 }
 
-// Values: row cu_out[r] + i receives position begin + i of request r as bf16.  Workgroup (page of the part, request);
-// a thread's unit is eight dims of a row of a head, 16 bytes out, in the order of the output rows; it loads
-// kReadUnits of them, K and V, before it stores the first, and stores past the caches: the output is four times what
-// is read.  Bound by the memory, mostly written: 88219 MXFP4 rows of 8 heads, 457 MB, 103 us (a copy that moves as
-// much takes 84); 110 with one unit at a time, 107 with a page's units in turns by one workgroup.
+// Values: row cu_out[r] + i receives position begin + i of request r as bf16.  Workgroup (page of the part, request, kv
+// head), heads last: it reads a run whole, so that no cache line is read by two, and goes with the next page's.  A
+// thread's unit is eight dims of a slot, 16 bytes out, for K and for V; stores go past the caches, as the output of
+// MXFP4 pages is four times what is read.  Bound by the memory: 88219 MXFP4 rows of 8 heads, 457 MB, 81 us (a copy that
+// moves as much takes 84); 92 with ordinary stores, 86 and 88 with two and four heads a workgroup, 85 with heads first,
+// 88 with two pages, 103 with the units of a page in the order of its rows over the workgroups, 104 with K and V apart.
 template <PageKind kKind>
 struct ReadUnit {   // as loaded: widened when it is stored
   uint32_t x[kKind == kBf16Pages ? 4 : kKind == kE4m3Pages ? 2 : 1];
@@ -210,7 +211,6 @@ __device__ inline u32x4 unit_values(const ReadUnit<kKind>& u) {
   }
 }
 
-constexpr int kReadUnits = 2;
 template <PageKind kKind>
 __global__ __launch_bounds__(256) void kv_read_kernel(
     const void* __restrict__ kpool, const void* __restrict__ vpool, const float* __restrict__ kscale,
@@ -230,30 +230,13 @@ __global__ __launch_bounds__(256) void kv_read_kernel(
   auto clamp = [](int64_t x) { return (int)(x < 0 ? 0 : x > 16 ? 16 : x); };
   const int first = max(clamp(begin - lp * 16), clamp(-base));
   const int past = min(clamp(end - lp * 16), clamp(out_rows - base));
-  const int units = (past - first) * hkv * 16;
-  const int64_t dst = (base + first) * hkv * 128;
-  // gridDim.z workgroups take the page's units in one turn each
-  for (int u0 = threadIdx.x + (int)blockIdx.z * (256 * kReadUnits); u0 < units; u0 += 256 * kReadUnits * (int)gridDim.z) {
-    ReadUnit<kKind> k[kReadUnits], v[kReadUnits];
-#pragma unroll
-    for (int j = 0; j < kReadUnits; ++j) {
-      const int u = u0 + 256 * j;
-      if (u < units) {
-        const int c = u & 15, h = (u >> 4) % hkv, slot = first + (u >> 4) / hkv;
-        const int64_t run = page * hkv + h;
-        k[j] = read_unit<kKind>(kpool, kscale, run, h, slot, c);
-        v[j] = read_unit<kKind>(vpool, vscale, run, h, slot, c);
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < kReadUnits; ++j) {
-      const int u = u0 + 256 * j;
-      if (u < units) {
-        __builtin_nontemporal_store(unit_values<kKind>(k[j]), reinterpret_cast<u32x4*>(kout + dst + (int64_t)u * 8));
-        __builtin_nontemporal_store(unit_values<kKind>(v[j]), reinterpret_cast<u32x4*>(vout + dst + (int64_t)u * 8));
-      }
-    }
-  }
+  const int slot = threadIdx.x >> 4, c = threadIdx.x & 15, h = blockIdx.z;
+  if (slot < first || slot >= past) return;
+  const int64_t run = page * hkv + h, dst = ((base + slot) * hkv + h) * 128 + 8 * c;
+  const ReadUnit<kKind> k = read_unit<kKind>(kpool, kscale, run, h, slot, c);
+  const ReadUnit<kKind> v = read_unit<kKind>(vpool, vscale, run, h, slot, c);
+  __builtin_nontemporal_store(unit_values<kKind>(k), reinterpret_cast<u32x4*>(kout + dst));
+  __builtin_nontemporal_store(unit_values<kKind>(v), reinterpret_cast<u32x4*>(vout + dst));
 }
 
 // Page copy between two pools of the same layout (swap-out: device pool -> pinned host
@@ -361,7 +344,7 @@ hipError_t launch_kv_gather(const KvLaunch& a, int32_t include_chunk, const int3
 hipError_t launch_kv_read(const KvLaunch& a, bool skip_prefix, bool with_chunk, const int32_t* cu_out, void* kout, void* vout,
                           int64_t out_rows, int32_t max_pages_read, hipStream_t stream) {
   if (a.num_reqs == 0 || max_pages_read == 0 || out_rows == 0) return hipSuccess;
-  dim3 grid(max_pages_read, a.num_reqs, (a.hkv + kReadUnits - 1) / kReadUnits);
+  dim3 grid(max_pages_read, a.num_reqs, a.hkv);
   auto launch = [&](auto kind) {
     constexpr PageKind kKind = decltype(kind)::value;
     kv_read_kernel<kKind><<<grid, 256, 0, stream>>>(a.kpool, a.vpool, a.kscale, a.vscale, static_cast<uint16_t*>(kout),
