@@ -59,7 +59,8 @@ __global__ __launch_bounds__(256) void kv_append_kernel(
 
 // MXFP4: the same for kMxHeads heads of a page, whose rows a thread loads before it encodes the first.  Four lanes
 // hold a block of 32 dims (a row's 16 lanes are all there or none): its largest magnitude sets the scale.  One row 2.4 us
-// (2.6 with a workgroup a head, 3.0 with four heads a workgroup), 35107 rows of 8 heads, 182 MB, 37 us (40 and 40).
+// (2.6 with a workgroup a head, 3.0 with four heads a workgroup), 35107 rows of 8 heads, 182 MB, 33 us, their loads past
+// the caches (37 with ordinary ones, and 40 and 40; 42 with the codes stored past them too).
 constexpr int kMxHeads = 2;
 __global__ __launch_bounds__(256) void kv_append_mxfp4_kernel(
     const int32_t* __restrict__ prefix_lens, const int32_t* __restrict__ chunk_lens,
@@ -82,8 +83,8 @@ __global__ __launch_bounds__(256) void kv_append_mxfp4_kernel(
 #pragma unroll
   for (int j = 0; j < kMxHeads; ++j)
     if (j < heads) {
-      kx[j] = *reinterpret_cast<const u32x4*>(knew + src + j * 128);
-      vx[j] = *reinterpret_cast<const u32x4*>(vnew + src + j * 128);
+      kx[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(knew + src + j * 128));
+      vx[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vnew + src + j * 128));
     }
   const int64_t run = (page * hkv + h0) * kMxRunBytes;
   const int codes = slot * kMxCodeBytes + 4 * c, scale = kMxScalesAt + slot * kMxScaleBytes + (c >> 2);
