@@ -997,9 +997,12 @@ s2l_status s2l_kv_read(const s2l_kv_cache* cache, const s2l_batch* batch, int32_
   if (out_rows < 0) return fail(S2L_EINVAL, "out_rows %lld < 0", (long long)out_rows);
   const bool skip_prefix = part == S2L_READ_CHUNK, with_chunk = part != S2L_READ_PREFIX;
   int32_t max_read = 0;
+  int64_t rows = 0;
   for (int32_t r = 0; r < batch->num_reqs; ++r) {
     const int32_t p = batch->prefix_lens_host[r], n = p + (with_chunk ? batch->chunk_lens_host[r] : 0), b = skip_prefix ? p : 0;
-    if (n > b) max_read = std::max(max_read, (n - 1) / s2l::kPageSize - b / s2l::kPageSize + 1);
+    if (n <= b) continue;
+    max_read = std::max(max_read, (n - 1) / s2l::kPageSize - b / s2l::kPageSize + 1);
+    rows += n - b;
   }
   if (max_read >= 1 << 24) return fail(S2L_ENOTSUP, "kv_read supports at most 2^28 positions of a request");
   if (max_read > 0 && out_rows > 0 && (!cu_out || !k_out || !v_out)) return fail(S2L_EINVAL, "cu_out/k_out/v_out is NULL");
@@ -1007,7 +1010,7 @@ s2l_status s2l_kv_read(const s2l_kv_cache* cache, const s2l_batch* batch, int32_
     return fail(S2L_EINVAL, "k_out and v_out must be aligned to 16 bytes");
   (void)hipGetLastError();
   hipError_t e = s2l::launch_kv_read(kv_launch(cache, batch), skip_prefix, with_chunk, cu_out, k_out, v_out, out_rows,
-                                     max_read, static_cast<hipStream_t>(stream));
+                                     std::min(rows, out_rows), max_read, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail("kv_read launch", e);
   return ok();
 }

@@ -166,10 +166,14 @@ __global__ __launch_bounds__(256) void kv_gather_mxfp4_kernel(
 
 // Values: row cu_out[r] + i receives position begin + i of request r as bf16.  Workgroup (page of the part, request, kv
 // head), heads last: it reads a run whole, so that no cache line is read by two, and goes with the next page's.  A
-// thread's unit is eight dims of a slot, 16 bytes out, for K and for V; stores go past the caches, as the output of
-// MXFP4 pages is four times what is read.  Bound by the memory: 88219 MXFP4 rows of 8 heads, 457 MB, 81 us (a copy that
-// moves as much takes 84); 92 with ordinary stores, 86 and 88 with two and four heads a workgroup, 85 with heads first,
-// 88 with two pages, 103 with the units of a page in the order of its rows over the workgroups, 104 with K and V apart.
+// thread's unit is eight dims of a slot, 16 bytes out, for K and for V.  Bound by the memory: 88219 MXFP4 rows of 8
+// heads, 457 MB, 81 us (a copy that moves as much takes 84); 86 and 88 with two and four heads a workgroup, 85 with heads
+// first, 88 with two pages, 103 with the units of a page in the order of its rows over the workgroups, 104 with K and V
+// apart.
+// Stores go past the caches where the output is too large for whoever reads it next to find it there.  Past them and
+// ordinary, us alone and with a copy of the output after: 34 MB 7.8, 23.1 and 8.5, 19.7; 84 MB 16.8, 59 and 23.0, 46;
+// 101 MB 19.7, 69 and 28.4, 66; 117 MB 22.8, 79 and 33.1, 81; 201 MB 38.7, 132 and 53.6, 133; 361 MB 78.8, 232 and 93.9, 227.
+constexpr int64_t kCachedBytes = 105 << 20;
 template <PageKind kKind>
 struct ReadUnit {   // as loaded: widened when it is stored
   uint32_t x[kKind == kBf16Pages ? 4 : kKind == kE4m3Pages ? 2 : 1];
@@ -212,7 +216,7 @@ __device__ inline u32x4 unit_values(const ReadUnit<kKind>& u) {
   }
 }
 
-template <PageKind kKind>
+template <PageKind kKind, bool kPastCaches>
 __global__ __launch_bounds__(256) void kv_read_kernel(
     const void* __restrict__ kpool, const void* __restrict__ vpool, const float* __restrict__ kscale,
     const float* __restrict__ vscale, uint16_t* __restrict__ kout, uint16_t* __restrict__ vout,
@@ -236,8 +240,14 @@ __global__ __launch_bounds__(256) void kv_read_kernel(
   const int64_t run = page * hkv + h, dst = ((base + slot) * hkv + h) * 128 + 8 * c;
   const ReadUnit<kKind> k = read_unit<kKind>(kpool, kscale, run, h, slot, c);
   const ReadUnit<kKind> v = read_unit<kKind>(vpool, vscale, run, h, slot, c);
-  __builtin_nontemporal_store(unit_values<kKind>(k), reinterpret_cast<u32x4*>(kout + dst));
-  __builtin_nontemporal_store(unit_values<kKind>(v), reinterpret_cast<u32x4*>(vout + dst));
+  const u32x4 ky = unit_values<kKind>(k), vy = unit_values<kKind>(v);
+  if constexpr (kPastCaches) {
+    __builtin_nontemporal_store(ky, reinterpret_cast<u32x4*>(kout + dst));
+    __builtin_nontemporal_store(vy, reinterpret_cast<u32x4*>(vout + dst));
+  } else {
+    *reinterpret_cast<u32x4*>(kout + dst) = ky;
+    *reinterpret_cast<u32x4*>(vout + dst) = vy;
+  }
 }
 
 // Page copy between two pools of the same layout (swap-out: device pool -> pinned host
@@ -343,14 +353,16 @@ hipError_t launch_kv_gather(const KvLaunch& a, int32_t include_chunk, const int3
 }
 
 hipError_t launch_kv_read(const KvLaunch& a, bool skip_prefix, bool with_chunk, const int32_t* cu_out, void* kout, void* vout,
-                          int64_t out_rows, int32_t max_pages_read, hipStream_t stream) {
+                          int64_t out_rows, int64_t written_rows, int32_t max_pages_read, hipStream_t stream) {
   if (a.num_reqs == 0 || max_pages_read == 0 || out_rows == 0) return hipSuccess;
   dim3 grid(max_pages_read, a.num_reqs, a.hkv);
+  const bool past_caches = written_rows > kCachedBytes / (2 * kHeadDim * 2) / a.hkv;
   auto launch = [&](auto kind) {
     constexpr PageKind kKind = decltype(kind)::value;
-    kv_read_kernel<kKind><<<grid, 256, 0, stream>>>(a.kpool, a.vpool, a.kscale, a.vscale, static_cast<uint16_t*>(kout),
-                                                    static_cast<uint16_t*>(vout), a.prefix_lens, a.chunk_lens, cu_out,
-                                                    a.block_tables, a.max_pages, a.hkv, skip_prefix, with_chunk, out_rows);
+    const auto kernel = past_caches ? kv_read_kernel<kKind, true> : kv_read_kernel<kKind, false>;
+    kernel<<<grid, 256, 0, stream>>>(a.kpool, a.vpool, a.kscale, a.vscale, static_cast<uint16_t*>(kout),
+                                     static_cast<uint16_t*>(vout), a.prefix_lens, a.chunk_lens, cu_out, a.block_tables,
+                                     a.max_pages, a.hkv, skip_prefix, with_chunk, out_rows);
   };
   with_kind(a.kind, launch);
   return hipGetLastError();

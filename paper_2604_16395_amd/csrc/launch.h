@@ -40,7 +40,7 @@ hipError_t launch_kv_gather(const KvLaunch& a, int32_t include_chunk, const int3
                             void* vout, int32_t max_pages_read, hipStream_t stream);
 // Values of positions [P if skip_prefix, P + C if with_chunk else P) as bf16 rows, out_rows of them.
 hipError_t launch_kv_read(const KvLaunch& a, bool skip_prefix, bool with_chunk, const int32_t* cu_out, void* kout, void* vout,
-                          int64_t out_rows, int32_t max_pages_read, hipStream_t stream);
+                          int64_t out_rows, int64_t written_rows, int32_t max_pages_read, hipStream_t stream);
 // Counts used block-table entries outside [0, num_pages) into counts[0] and the largest
 // offending request + 1 into counts[1] (both cleared first).
 hipError_t launch_check_tables(const KvLaunch& a, int32_t max_pages_used, int32_t* counts, hipStream_t stream);

@@ -141,6 +141,28 @@ def test_read_gives_the_values(P, C, hkv, kind):
             assert torch.equal(got.nan_to_num(0), w.nan_to_num(0)), (part, kind)
 
 
+@pytest.mark.parametrize("P", [3201, 6655])
+def test_read_of_more_than_caches_hold(P):
+    """Outputs of 105 and 218 MB, where values are stored past the caches, from pages that requests share, and of a request alone."""
+    rng = np.random.default_rng(P)
+    host, cache = pools(40, 8, rng)
+    for h, dev in zip(host, (cache.k_pages, cache.v_pages)):
+        h[..., 1024:] = rng.integers(100, 140, h[..., 1024:].shape)
+        dev.copy_(torch.from_numpy(h))
+    tables = rng.integers(0, 40, (8, -(-P // 16))).astype(np.int32)
+    whole = [mxfp4.load(h, np.repeat(np.arange(40), 16), np.tile(np.arange(16), 40))[1] for h in host]    # of every page
+    whole = [torch.from_numpy(w).to(torch.float32).to(torch.bfloat16).to(DEV).view(40, 16, 8, 128) for w in whole]
+    for R in (8, 1):
+        batch = s2l.Batch([P] * R, [0] * R, tables[:R])
+        k, v = (torch.full((R * P, 8, 128), 7.0, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        s2l.s2l_kv_read(cache, batch, s2l.S2L_READ_PREFIX, torch.arange(R, device=DEV).int() * P, k, v)
+        torch.cuda.synchronize()
+        for got, w in zip((k, v), whole):
+            for r in range(R):
+                want = w[torch.from_numpy(tables[r].astype(np.int64)).to(DEV)].reshape(-1, 8, 128)[:P]
+                assert torch.equal(got[r * P:(r + 1) * P], want), (R, r)
+
+
 def test_read_of_nothing():
     cache = pools(2, 2, np.random.default_rng(0))[1]
     k = torch.zeros((0, 2, 128), dtype=torch.bfloat16, device=DEV)
