@@ -6,17 +6,17 @@
 // fp32 (2^-26 of a turn), for the hardware's sine and cosine, which take turns.
 //
 // Norms (kNorm): a head's squares are summed over its eight lanes before the rotation, fp32 until the one rounding at
-// the end.  One row 3.2 us, 35107 rows of 32 + 8 + 8 heads 163 us, as fast as a copy moves their 863 MB; 2342 rows of
-// 32 + 32 without pages 18.4 us (77 MB, which the last-level cache holds), bound by the arithmetic and, as all waves
+// the end.  One row 2.95 us, 35107 rows of 32 + 8 + 8 heads 163 us, as fast as a copy moves their 863 MB; 2342 rows of
+// 32 + 32 without pages 18.2 us (77 MB, which the last-level cache holds), bound by the arithmetic and, as all waves
 // are resident at once, by loading, computing and storing one after another.
 //
 // A wave takes one row (token) and 8 kHeads of its heads (a workgroup four rows; workgroups of the same rows
 // follow one another); lane l holds unit l % 8 of head l / 8, the 16 elements of 8 pairs in two 16-byte
 // chunks, so that a lane's 8 sines and cosines serve all its heads and rows of a head are read and
-// written whole.  Units past the rotated dims, and V's, are copied.  Nothing is shared between waves: no LDS, no barrier.
+// written whole.  Units past the rotated dims, and V's, are copied.  Nothing is shared between waves: no barrier.
 // Bound by the memory for many rows: 35107 rows of 32 + 8 + 8 heads, 863 MB, 160 us, 5.4 TB/s (171 with one head a
 // lane; 217 with one head a lane and the groups of a row far apart); by the chain of loads for few: one row 2.9 us, 512
-// rows 4.6 us (4.8 with two heads a lane), in a graph, one call after another.
+// rows 4.3 us, in a graph, one call after another.
 #include "launch.h"
 #include "s2l.h"
 #include "s2l_device.h"
@@ -154,24 +154,26 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a) {
     if (first <= last) weights_of(head0);
   }
 
+  // lane i takes pair i's sine and cosine, and hands them to the lanes that turn by it through the wave's part of LDS.
+  // Against each lane's own 8 pairs, their sums in doubles eight times over, us: one row 2.95 and 3.18 (32 + 8 + 8 heads, normed),
+  // 512 rows 4.3 and 5.3, 1024 normed 8.2 and 9.2, 4096 23.7 and 24.6; 35107 the same.
+  __shared__ __attribute__((aligned(16))) float turn_by[4][2][64];
   float cs[8], sn[8];
-  if (turns) {
-    double pos[S2L_ROPE_MAX_AXES];
-    const bool one_axis = kNorm && a.num_axes == 1;   // no choice among them for each pair
+  if (!kAppend || first < a.hq + a.hkv) {
+    const int pair = lane < half ? lane : 0;
+    const uint32_t axis = (uint32_t)(a.pair_axes[pair >> 5] >> (2 * (pair & 31))) & 3;   // two bits a pair
+    const double p = (double)(a.positions == nullptr ? at.pos : a.positions[axis * a.pos_stride + row]);
+    const double f = (double)a.inv_freq[pair] * 0.15915494309189535;
+    const float angle = (float)__builtin_fma(p, f, -__builtin_rint(p * f));
+    float* by = turn_by[threadIdx.x >> 6][0];
+    by[lane] = a.scale * __builtin_amdgcn_cosf(angle);
+    by[64 + lane] = a.scale * __builtin_amdgcn_sinf(angle);
+    __builtin_amdgcn_wave_barrier();   // a wave's accesses to LDS keep their order
 #pragma unroll
-    for (int i = 0; i < S2L_ROPE_MAX_AXES; ++i)
-      pos[i] = (double)(a.positions == nullptr ? at.pos : a.positions[(i < a.num_axes ? i : 0) * a.pos_stride + row]);
-    const f32x4 f0 = *reinterpret_cast<const f32x4_any*>(a.inv_freq + 8 * unit);
-    const f32x4 f1 = *reinterpret_cast<const f32x4_any*>(a.inv_freq + 8 * unit + 4);
-    const uint32_t axes = (uint32_t)(a.pair_axes[unit >> 2] >> (16 * (unit & 3)));   // two bits a pair
+    for (int i = 0; i < 8; i += 4) {
+      const f32x4 c4 = *reinterpret_cast<const f32x4*>(by + 8 * unit + i), s4 = *reinterpret_cast<const f32x4*>(by + 64 + 8 * unit + i);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t axis = axes >> (2 * i) & 3;
-      const double p = one_axis ? pos[0] : axis & 2 ? (axis & 1 ? pos[3] : pos[2]) : (axis & 1 ? pos[1] : pos[0]);
-      const double f = (double)(i < 4 ? f0[i & 3] : f1[i & 3]) * 0.15915494309189535;
-      const float angle = (float)__builtin_fma(p, f, -__builtin_rint(p * f));
-      cs[i] = a.scale * __builtin_amdgcn_cosf(angle);
-      sn[i] = a.scale * __builtin_amdgcn_sinf(angle);
+      for (int k = 0; k < 4; ++k) cs[i + k] = c4[k], sn[i + k] = s4[k];
     }
   }
 
@@ -255,13 +257,13 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a) {
   }
 }
 
-// Two heads a lane share its sines and cosines and halve the waves; as long as waves are few (6 a SIMD), more of them
-// hide more.  One head a lane and two, us in a graph: 32 + 8 + 8 heads, 512 rows 4.6 and 4.8, 1024 (6144 waves) 7.9 and
-// 7.9, 1365 (8190) 9.6 and 8.9, 4096 24.0 and 21.8; 64 + 8 + 8 into e4m3 pages, 600 (6000) 8.3 and 8.1, 1000 11.4 and
-// 10.1; 32 + 32 without pages, 768 (6144) 8.4 and 8.4, 1024 10.1 and 10.1.
-// With norms a head costs more beside what its lane shares (sines, weights), and many rows take up to four heads a
-// lane, evenly over the waves of a row: two, three and four, us in a graph: 35107 rows of 32 + 8 + 8 heads 167.9, 162.7,
-// 174.1 (two waves a row take three), 2342 rows of 32 + 32 without pages 20.0, 20.8, 18.4 (two waves, four).
+// Two heads a lane halve the waves and what each does beside its heads; as long as waves are few (6 a SIMD), more of them
+// hide more.  One head a lane and two, us in a graph, 32 + 8 + 8 heads: 512 rows 4.3 and 4.6, 1024 (6144 waves) 7.3 and 7.7,
+// 1365 (8190) 8.8 and 8.7, 2048 10.9 and 10.5, 4096 21.8 and 22.8, 8192 40.5 and 41.0.
+// With norms a head costs more beside what its lane shares (sines, weights), and rows whose heads fill waves of 32 take four
+// heads a lane.  Two, three and four, us in a graph: 2342 rows of 32 + 32 heads without pages 18.1, 18.8, 15.5, 20000 rows
+// 129, 123, 127; 1500 rows of 64 + 8 + 8 14.7, 16.7, 13.7; 5000 of 24 + 4 + 4 18.3, 19.4, 17.4, 20000 66.8, 74.9, 71.0.  Others two:
+// 35107 rows of 32 + 8 + 8 163.0, 164.2, 173.6, 4096 23.4, 24.3, 24.2, 20000 into e4m3 pages 90.7, 95.1, 105.8.
 template <bool kAdjacent, bool kAppend, PageKind kKind, bool kNorm>
 void launch(const RopeLaunch& a, hipStream_t stream) {
   constexpr int64_t kFewWaves = 6144;
@@ -272,12 +274,9 @@ void launch(const RopeLaunch& a, hipStream_t stream) {
     rope_kernel<kAdjacent, kAppend, kKind, kNorm, kHeads>
         <<<dim3((uint32_t)(four_rows * ((groups + kHeads - 1) / kHeads))), 256, 0, stream>>>(a);
   };
-  const int64_t waves = (groups + 3) / 4;   // of a row, at four heads a lane
-  const int64_t even = (groups + waves - 1) / waves;
-  if (a.total_rows * groups <= kFewWaves) run(std::integral_constant<int, 1>{});
-  else if (kNorm && even == 4) run(std::integral_constant<int, kNorm ? 4 : 2>{});
-  else if (kNorm && even == 3) run(std::integral_constant<int, kNorm ? 3 : 2>{});
-  else if (kNorm && even == 1) run(std::integral_constant<int, 1>{});
+  const int64_t waves = (groups + 3) / 4, a_lane = (groups + waves - 1) / waves;   // of a row: at most four heads a lane, evenly
+  if (a.total_rows * groups <= kFewWaves || (kNorm && a_lane == 1)) run(std::integral_constant<int, 1>{});
+  else if (kNorm && a_lane == 4) run(std::integral_constant<int, kNorm ? 4 : 2>{});
   else run(std::integral_constant<int, 2>{});
 }
 
