@@ -53,9 +53,9 @@
 // what the score MFMAs start from, so their results are the exponents.  V is widened to bf16 on the way into LDS.
 // A layer of P = 131072, C = 2048 (8q/1kv) takes 0.80 to 0.83 ms (boxes differ), 1340 to 1390 TFLOP/s, above what a
 // bf16 product of 8192^3 reaches; K widened to bf16 took 1.12 times as long, three E2M3 terms without the factor
-// and -m in them 1.07 times.  The loop's MFMA and VALU instructions hardly overlap (with the terms alone MFMA was
-// busy 49% of the cycles, VALU most of the others, at 1.7 to 1.9 GHz), so each fma or cycle of MFMA that is left out
-// counts.  The queries' terms cost a workgroup 0.5 us before its first tile (600 tokens without prefix, 32q/8kv: 17.2 us).
+// and -m in them 1.07 times.  The loop's MFMA and VALU instructions hardly overlap (MFMA busy 58% of the cycles,
+// VALU 45%, at the 1.7 to 1.9 GHz that the power limit allows), so each fma or cycle of MFMA that is left out counts.
+// The queries' terms cost a workgroup 0.5 us before its first tile (600 tokens without prefix, 32q/8kv: 17.2 us).
 //
 // Quantised-Q variant (e4m3 pages only): each lane pair encodes its column of Q to e4m3 with
 // the column's own scale, K's codes stay e4m3 in LDS (same permuted chunk positions), and the

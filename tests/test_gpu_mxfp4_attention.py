@@ -142,7 +142,7 @@ def test_a_query_that_is_not_finite(layout, bad):
     assert torch.equal(out.view(torch.int16), ref.view(torch.int16)) and torch.equal(lse, ref_lse)
 
 
-@pytest.mark.parametrize("scale", [1e-30, 1e-4, 0.7, 1.9, 1.0e3])
+@pytest.mark.parametrize("scale", [2.0 ** -120, 1e-30, 1e-4, 0.7, 1.9, 1.0e3])
 @pytest.mark.parametrize("layout", [(128, 1), (256, 1)])
 def test_other_softmax_scales(layout, scale):
     """Factors of every mantissa and size, with queries of sizes from 2^-100 to 2 (scores up to thousands)."""

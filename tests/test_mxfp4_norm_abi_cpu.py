@@ -88,6 +88,15 @@ def test_bad_mxfp4_caches(call):
         assert call(c, b)[0] == ENOTSUP
 
 
+@pytest.mark.parametrize("scale", [2.0 ** -121, 1e-45, 2.0 ** 121])
+def test_softmax_scales_past_the_queries_terms(scale):
+    b, keep = _batch([3], [4])
+    for cols in (128, 256):
+        c, info = _cache(dtype=2), _lib.s2l_plan_info(tile_cols=cols)
+        st, msg = _status("s2l_chunk_prefill_attn", byref(c), byref(b), FAKE, 4, scale, FAKE, None, byref(info), FAKE, 1 << 20, None)
+        assert st == ENOTSUP and "softmax_scale" in msg
+
+
 def test_quantised_queries_need_e4m3_pages():
     b, keep = _batch([3], [4])
     c, info = _cache(dtype=2), _lib.s2l_plan_info(tile_cols=128)
