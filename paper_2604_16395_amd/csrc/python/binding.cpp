@@ -37,7 +37,7 @@ PyObject *tensor_type, *cache_type, *batch_type, *opts_type, *info_type, *stream
 PyObject *s_dtype, *s_data_ptr, *s_is_contiguous, *s_shape, *s_numel, *s_k_pages, *s_v_pages, *s_k_scale, *s_v_scale,
     *s_fp8, *s_prefix_host, *s_chunk_host, *s_tables_host, *s_prefix_lens, *s_chunk_lens, *s_cu_chunk, *s_block_tables,
     *s_cuda_stream, *s_stride, *s_get_device, *s_inv_freq, *s_positions, *s_pair_axis, *s_adjacent, *s_scale, *s_states, *s_log_decay,
-    *s_slot_in, *s_slot_out, *s_mxfp4, *s_q_weight, *s_k_weight, *s_eps, *s_offset;
+    *s_slot_in, *s_slot_out, *s_mxfp4, *s_q_weight, *s_k_weight, *s_eps, *s_offset, *s_dim;
 
 // Owned reference, released at the end of the scope.
 struct Ref {
@@ -151,8 +151,13 @@ bool cache_arg(PyObject* o, s2l_kv_cache* c) {
   return true;
 }
 
-// None: the current stream of the current device; a number; or a torch.cuda.Stream.
-bool stream_arg(PyObject* s, void** p) {
+// None: the current stream of the current device (number `dev`, where the caller has it); a number; or a torch.cuda.Stream.
+bool stream_arg(PyObject* s, void** p, long dev = -1) {
+  if (s == Py_None && dev >= 0) {
+    const Ref number(PyLong_FromLong(dev));
+    const Ref raw(number ? PyObject_CallOneArg(get_stream, number.o) : nullptr);
+    return raw && to_ptr(raw.o, p);
+  }
   if (s == Py_None) {
     const Ref ready(PyObject_CallNoArgs(is_initialized));
     if (!ready || ready.o != Py_True) return false;
@@ -217,6 +222,18 @@ bool layout(PyObject* t, int ndim, int64_t* shape, int64_t* stride) {
     stride[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(st.o, i));
   }
   return !PyErr_Occurred();
+}
+
+// Shape of a tensor of three dimensions.
+bool shape3(PyObject* t, int64_t* shape) {
+  const Ref sh(PyObject_GetAttr(t, s_shape));
+  if (!sh || !PyTuple_Check(sh.o) || PyTuple_GET_SIZE(sh.o) != 3) return false;
+  for (int i = 0; i < 3; ++i) shape[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(sh.o, i));
+  return !PyErr_Occurred();
+}
+bool is_vector(PyObject* t) {
+  const Ref d(PyObject_CallMethodNoArgs(t, s_dim));
+  return d && PyLong_AsLong(d.o) == 1 && !PyErr_Occurred();
 }
 
 // A device tensor of rows [>= tokens][heads][128], each row's heads contiguous.
@@ -304,10 +321,14 @@ bool weight_arg(PyObject* o, PyObject* name, long dev, int32_t* dtype, const voi
   const Ref t(PyObject_GetAttr(o, name));
   *w = nullptr;
   if (!t || t.o == Py_None) return t.o == Py_None;
+  if ((PyObject*)Py_TYPE(t.o) != tensor_type) return false;
+  const Ref d(PyObject_GetAttr(t.o, s_dtype)), c(PyObject_CallMethodNoArgs(t.o, s_is_contiguous));
+  const int32_t type = d.o == f32 ? S2L_NORM_FP32 : d.o == bf16 ? S2L_NORM_BF16 : -1;
   void* p;
-  int64_t n, s;
-  const int32_t type = tensor(t.o, f32, &p) ? S2L_NORM_FP32 : tensor(t.o, bf16, &p) ? S2L_NORM_BF16 : -1;
-  if (type < 0 || (*dtype >= 0 && type != *dtype) || !layout(t.o, 1, &n, &s) || n != S2L_HEAD_DIM || !on_device(t.o, dev)) return false;
+  size_t n;
+  if (type < 0 || (*dtype >= 0 && type != *dtype) || c.o != Py_True || !numel(t.o, &n) || n != S2L_HEAD_DIM || !is_vector(t.o) ||
+      !on_device(t.o, dev) || !data_ptr(t.o, &p))
+    return false;
   *dtype = type;
   *w = p;
   return true;
@@ -431,7 +452,7 @@ PyObject* rotate(PyObject* const* a, Py_ssize_t n, bool normed) {
   if (n != 7 + normed || !batch_on_device(a[0], &batch, &tokens, &dev) || (normed && !norm_arg(a[1], dev, &norm))) return general();
   a += normed;
   if (!rope_arg(a[1], tokens, dev, &rope) || !q.take(a[2], tokens, dev) || !q_out.take(a[3], tokens, dev) || q.heads != q_out.heads ||
-      !stream_arg(a[6], &stream))
+      !stream_arg(a[6], &stream, dev))
     return general();
   if (a[4] != Py_None && (!k.take(a[4], tokens, dev) || !k_out.take(a[5], tokens, dev) || k.heads != k_out.heads)) return general();
   return call([&] {
@@ -459,7 +480,7 @@ PyObject* rotate_append(PyObject* const* a, Py_ssize_t n, bool normed) {
     return general();
   a += normed;
   if (!rope_arg(a[2], tokens, dev, &rope) || !k.take(a[5], tokens, dev) || !v.take(a[6], tokens, dev) ||
-      k.heads != cache.num_kv_heads || v.heads != k.heads || !stream_arg(a[7], &stream))
+      k.heads != cache.num_kv_heads || v.heads != k.heads || !stream_arg(a[7], &stream, dev))
     return general();
   if (a[3] != Py_None && (!q.take(a[3], tokens, dev) || !q_out.take(a[4], tokens, dev) || q.heads != q_out.heads)) return general();
   return call([&] {
@@ -477,15 +498,15 @@ PyObject* read(PyObject*, PyObject* const* a, Py_ssize_t n) {
   s2l_kv_cache cache;
   BatchArg batch;
   int32_t part;
-  int64_t tokens, rows[3], more[3], s[3];
+  int64_t tokens, rows[3], more[3];
   long dev;
   void *cu, *k, *v, *stream;
   size_t offsets;
   if (n != 7 || !cache_arg(a[0], &cache) || !batch_on_device(a[1], &batch, &tokens, &dev) || !cache_on_device(a[0], cache, dev) ||
-      !int_arg(a[2], &part) || !tensor(a[3], i32, &cu) || !numel(a[3], &offsets) || !on_device(a[3], dev) || !layout(a[3], 1, rows, s) ||
-      offsets < (size_t)batch.c.num_reqs || !tensor(a[4], bf16, &k) || !on_device(a[4], dev) || !layout(a[4], 3, rows, s) ||
-      !tensor(a[5], bf16, &v) || !on_device(a[5], dev) || !layout(a[5], 3, more, s) || rows[0] != more[0] ||
-      rows[1] != cache.num_kv_heads || more[1] != rows[1] || rows[2] != S2L_HEAD_DIM || more[2] != S2L_HEAD_DIM || !stream_arg(a[6], &stream))
+      !int_arg(a[2], &part) || !tensor(a[3], i32, &cu) || !numel(a[3], &offsets) || !on_device(a[3], dev) || !is_vector(a[3]) ||
+      offsets < (size_t)batch.c.num_reqs || !tensor(a[4], bf16, &k) || !on_device(a[4], dev) || !shape3(a[4], rows) ||
+      !tensor(a[5], bf16, &v) || !on_device(a[5], dev) || !shape3(a[5], more) || rows[0] != more[0] ||
+      rows[1] != cache.num_kv_heads || more[1] != rows[1] || rows[2] != S2L_HEAD_DIM || more[2] != S2L_HEAD_DIM || !stream_arg(a[6], &stream, dev))
     return general();
   return call([&] { return lib.read(&cache, &batch.c, part, static_cast<const int32_t*>(cu), k, v, rows[0], stream); });
 }
@@ -500,7 +521,7 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void *in, *slots, *states, *decay, *ws = nullptr, *st;
   if (n != 9 || (PyObject*)Py_TYPE(a[0]) != state_type || !batch_on_device(a[1], &batch, &tokens, &dev) || !q.take(a[2], tokens, dev) ||
       !k.take(a[3], tokens, dev) || !v.take(a[4], tokens, dev) || !PyFloat_CheckExact(a[5]) || !out.take(a[6], tokens, dev) ||
-      k.heads != v.heads || q.heads != out.heads || !stream_arg(a[8], &st) ||
+      k.heads != v.heads || q.heads != out.heads || !stream_arg(a[8], &st, dev) ||
       !attr_tensor(a[0], s_slot_in, i32, dev, &in, &in_slots) || !attr_tensor(a[0], s_slot_out, i32, dev, &slots, &out_slots) ||
       !attr_tensor(a[0], s_log_decay, f32, dev, &decay, &decays) || !attr_tensor(a[0], s_states, f32, dev, &states, &elements))
     return general();
@@ -566,7 +587,7 @@ PyMODINIT_FUNC PyInit__binding(void) {
                {&s_stride, "stride"}, {&s_get_device, "get_device"}, {&s_inv_freq, "inv_freq"}, {&s_positions, "positions"},
                {&s_pair_axis, "pair_axis"}, {&s_adjacent, "adjacent"}, {&s_scale, "scale"}, {&s_states, "states"},
                {&s_log_decay, "log_decay"}, {&s_slot_in, "slot_in"}, {&s_slot_out, "slot_out"}, {&s_mxfp4, "mxfp4"},
-               {&s_q_weight, "q_weight"}, {&s_k_weight, "k_weight"}, {&s_eps, "eps"}, {&s_offset, "offset"}};
+               {&s_q_weight, "q_weight"}, {&s_k_weight, "k_weight"}, {&s_eps, "eps"}, {&s_offset, "offset"}, {&s_dim, "dim"}};
   for (const auto& n : names)
     if (!(*n.o = PyUnicode_InternFromString(n.s))) return nullptr;
   return PyModule_Create(&module);
