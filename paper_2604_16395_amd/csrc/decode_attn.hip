@@ -13,7 +13,7 @@
 // waves run independently over the item's tiles (wave w takes tiles w, w+4, ...),
 // each with its own online softmax, and merge their (O, m, l) through LDS at the end.
 //
-// A tile is 32 keys (bf16) or 64 keys (e4m3), so that two tiles of registers fit 256 a lane and
+// A tile is 32 keys (bf16) or 64 keys (e4m3, MXFP4), so that two tiles of registers fit 256 a lane and
 // two workgroups a CU, and a wave's share of a short range is whole tiles.  Bound by HBM for long
 // ranges and by the latency of the item, page, K and V loads for short ones.  Against 64-key
 // bf16 tiles in 361 registers, e4m3 codes widened where they were loaded (so waited for there), a
@@ -25,10 +25,10 @@
 //   * K goes from HBM straight into the A operand of S^T = K Q^T
 //     (v_mfma_f32_16x16x32_bf16): lane (j, q) loads key j of the tile's page b, dims
 //     32 ks + 8 q .. + 7, a 16-byte load (fp8: the 16 codes of dims 64 t + 16 q .. + 15 serve
-//     k-steps 2 t and 2 t + 1, widened to bf16 exactly where they are used);
+//     k-steps 2 t and 2 t + 1, MXFP4: the 32 codes of block q, one scale; widened to bf16 exactly where they are used);
 //   * S^T lands as keys 16 b + 4 q + v of column j in lane (j, q);
 //   * softmax in the exp2 domain against a per-column reference m (the exact max of the
-//     wave's first 64 keys, that is of one e4m3 tile or two bf16 tiles; raised, with O and l
+//     wave's first 64 keys, that is of one e4m3 or MXFP4 tile or two bf16 tiles; raised, with O and l
 //     rescaled, at the second of these, and later only if a probability would exceed 2^64: a
 //     reference from 32 keys leaves the largest probabilities further from 1, where they round
 //     exactly, and the result 1% further from the exact one), probabilities rounded to bf16, the row sum adding exactly those;
@@ -42,6 +42,11 @@
 // the compiler's own wait counts are exact; the loop is unrolled by two so that the two K
 // and V register sets alternate without copies.  No barrier inside the loop: every LDS
 // byte a wave reads it wrote itself.
+//
+// MXFP4 pages: 136 bytes a key and head are a quarter of bf16's, with the same work on them: 64 rows of 8192 keys (32q/8kv)
+// 99 us, 5.8 TB/s; one row of 2047 keys 5.6 us and its merge 2.8.  K as codes on the f8f6f4 MFMA, as the prefill kernel
+// multiplies it, took 8.4 us for 7.8 for the row and 138 for 115 over 922 short rows (the queries' terms come first) and
+// gained 1% on long ones; register sets three to five deep took 1.06 to 1.18 times the time.
 #include "launch.h"
 #include "plan_rules.h"
 #include "s2l_device.h"
@@ -58,6 +63,10 @@ constexpr int kVRow = kHeadDim * 2;             // bf16 key row in LDS
 template <PageKind kKind>
 constexpr int kTilePages = kKind == kBf16Pages ? 2 : 4;
 constexpr int kDNoNan = 0x7FFFFFFF;
+// MXFP4 codes are loaded as data that is read once (nt).  Against ordinary loads, cold: 64 equal rows of 8192 keys 110 -> 99 us,
+// of 4096 57.3 -> 53.0, 64 rows of up to 16384 (64q/8kv) 118.7 -> 116.3, 4 of 120000 104.9 -> 102.2, 300 of up to 2000 79.4 -> 76.7;
+// the same rows again and again, which the last-level cache holds in part, 113 -> 109, but 50.2 -> 52.5 where it holds most.
+constexpr int kStreamed = 2;
 constexpr float kDLn2 = 0.6931471805599453f;
 constexpr float kDOverflow = 18446744073709551616.0f;   // 2^64
 constexpr int32_t kDRsrcWord3 = 0x00020000;
@@ -194,8 +203,8 @@ __global__ __launch_bounds__(kDecodeWaves * 64, 2) void attn_decode_kernel(
       const auto vr = page_rsrc(vpb + page * page_stride, bytes);
       if constexpr (kMx) {   // K: key j, block q.  V: key l / 4, block l % 4
         const int vo = lane >> 2;
-        t.k[b][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kr, j * kMxCodeBytes + 16 * qg, 0, 0));
-        t.v[b][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vr, vo * kMxCodeBytes + 16 * (lane & 3), 0, 0));
+        t.k[b][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kr, j * kMxCodeBytes + 16 * qg, 0, kStreamed));
+        t.v[b][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vr, vo * kMxCodeBytes + 16 * (lane & 3), 0, kStreamed));
         t.ks[b] = __builtin_amdgcn_raw_buffer_load_b8(kr, kMxScalesAt + j * kMxScaleBytes + qg, 0, 0);
         t.vs[b] = __builtin_amdgcn_raw_buffer_load_b8(vr, kMxScalesAt + vo * kMxScaleBytes + (lane & 3), 0, 0);
         continue;
