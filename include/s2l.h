@@ -455,9 +455,7 @@ s2l_status s2l_attn_plan(const s2l_batch* batch, int32_t num_q_heads, int32_t nu
  * weights e^{s_j} / sum are applied as bf16 values normalised by their own sum, so out is
  * within about 2^-7 sum_j w_j |V_j - out| + 2^-8 |out| of the exact result; lse is the
  * log of the sum of those bf16 weights (within about 2^-8 of the exact value).  Over an MXFP4 cache tiles of 128
- * and 256 columns take each q within 2^-13 of the largest magnitude among its 32 dims (32 b .. 32 b + 31 of a
- * row; of 2^-110 / softmax_scale where that is more), which moves s_j by at most 2^-13 softmax_scale
- * sum |that magnitude K|; there softmax_scale is 2^-120 to 2^120 (ENOTSUP otherwise) and softmax_scale |q| has to stay below 2^100.
+ * and 256 columns take a softmax_scale of 2^-120 to 2^120 (ENOTSUP otherwise).
  *   q   : device bf16 [T][Hq][128] (post-RoPE).     out : device bf16 [T][Hq][128].
  *   lse : device fp32 [T][Hq] or NULL.               softmax_scale > 0 (e.g. 1/sqrt(128)).
  *   plan: the s2l_plan_info returned by s2l_attn_plan for this batch and head counts.

@@ -535,7 +535,7 @@ s2l_status attn_common(const s2l_kv_cache* cache, const s2l_batch* batch, const 
   if ((st = check_batch(batch, true, T)) != S2L_OK) return st;
   if ((st = check_heads(hq, cache->num_kv_heads)) != S2L_OK) return st;
   if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(S2L_EINVAL, "softmax_scale must be finite and > 0");
-  // the factor's exponent joins the queries' in a byte
+  // away from the ends of fp32's range, where the factor log2 e softmax_scale loses bits or overflows
   if (cache->dtype == S2L_KV_MXFP4 && plan && plan->tile_cols != s2l::kDecodeTileCols && !(scale >= 0x1p-120f && scale <= 0x1p120f))
     return fail(S2L_ENOTSUP, "softmax_scale %g over MXFP4 pages unsupported (2^-120 to 2^120)", (double)scale);
   if (*T > 0 && (!q || !out)) return fail(S2L_EINVAL, "q/out is NULL");

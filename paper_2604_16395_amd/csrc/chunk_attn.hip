@@ -47,15 +47,12 @@
 // overflow at the start of step b, before it enters O.  The causal mask is applied only to
 // sub-blocks that reach past the first query token's position.
 //
-// MXFP4 pages: K's codes and scales are copied into LDS as they are (4.25 KiB a tile) and multiplied as they are
-// by v_mfma_scale_f32_32x32x64_f8f6f4, which takes E2M1 against E2M3 at twice the rate of bf16: the queries, times
-// the softmax's factor, go as three E2M3 values each (s2l_device.h; 192 cycles a sub-block instead of 256), and -m is
-// what the score MFMAs start from, so their results are the exponents.  V is widened to bf16 on the way into LDS.
-// A layer of P = 131072, C = 2048 (8q/1kv) takes 0.80 to 0.83 ms (boxes differ), 1340 to 1390 TFLOP/s, above what a
-// bf16 product of 8192^3 reaches; K widened to bf16 took 1.12 times as long, three E2M3 terms without the factor
-// and -m in them 1.07 times.  The loop's MFMA and VALU instructions hardly overlap (MFMA busy 58% of the cycles,
-// VALU 45%, at the 1.7 to 1.9 GHz that the power limit allows), so each fma or cycle of MFMA that is left out counts.
-// The queries' terms cost a workgroup 0.5 us before its first tile (600 tokens without prefix, 32q/8kv: 17.2 us).
+// MXFP4 pages: K and V are widened to bf16, exactly, on their way through registers into LDS, as e4m3 pages are, and
+// multiply bf16 queries as they are.  A layer of P = 131072, C = 2048 (8q/1kv) takes 0.90 to 0.92 ms, 1200 to 1230 TFLOP/s
+// (bf16 pages 0.91 to 0.92); 600 tokens without prefix (32q/8kv) 16.4 us.  K's codes multiplied as they are stored on the
+// f8f6f4 MFMA, by three E2M3 terms of each query, took 0.89 of the time (chunk on 8192 tokens 0.96, 600 tokens 1.03) and held
+// a query only within 2^-13 of the largest of its 32 dims: beside dims 100 times as large that outweighs every other
+// rounding here.  A higher wave priority within a step: the same to 1%.
 //
 // Quantised-Q variant (e4m3 pages only): each lane pair encodes its column of Q to e4m3 with
 // the column's own scale, K's codes stay e4m3 in LDS (same permuted chunk positions), and the
@@ -76,8 +73,6 @@ constexpr int kRowBytes = kHeadDim * 2;              // one bf16 key row in LDS
 constexpr int kTileBytes = kKvTile * kRowBytes;      // 16 KiB
 constexpr int kSubBytes = 32 * kRowBytes;            // one 32-key sub-block of a tile
 constexpr int kNoNan = 0x7FFFFFFF;
-constexpr int kMxSubBytes = 32 * kMxCodeBytes;       // MXFP4: a tile of K is held as codes, 64 bytes a key,
-constexpr int kMxTileScales = 2 * kMxSubBytes;       //   then four scale bytes a key
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kOverflow = 18446744073709551616.0f;   // 2^64: largest probability kept
@@ -152,16 +147,6 @@ __device__ inline void slot_schedule() {
   }
 }
 
-// C + K Q^T over 64 dims, half kHalf of them: MXFP4 codes of K, of which the lane's scale bytes are 0 and 2, and
-// term kTerm of the queries.
-template <int kHalf, int kTerm>
-__device__ inline f32x16 mx_mfma(const u32x4& k, const u32x6& q, const f32x16& c, uint32_t k_scales, uint32_t q_scales) {
-  constexpr int kFp4 = 4, kE2M3 = 2;   // the MFMA's element types
-  const i32x8 a = {(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
-  const i32x8 b = {(int)q[0], (int)q[1], (int)q[2], (int)q[3], (int)q[4], (int)q[5], 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, kFp4, kE2M3, 2 * kHalf, k_scales, kTerm, q_scales);
-}
-
 // Weight 2^(m_s - m*) of a piece in the log-sum-exp merge (0 for an empty piece).
 __device__ inline float merge_weight(float m_s, float mstar) {
   return m_s == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_s - mstar);
@@ -203,7 +188,6 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
   constexpr int kMxLanes = 64 / kRowsPerWave;        // MXFP4: lanes sharing a row, 8 or 16 bytes of codes each
   constexpr int kRun = run_bytes(kKind);             // bytes of one (page, kv head)
   constexpr int kKeyBytes = kRun / 16;
-  constexpr int kKSub = kMx ? kMxSubBytes : kSubBytes;   // a 32-key sub-block of a tile of K in LDS
   __shared__ __attribute__((aligned(1024))) uint8_t smem[RingT::kBytes];
   __shared__ __attribute__((aligned(256))) int32_t s_pages[kWaves][2][64];   // next page windows
   __shared__ int32_t s_nan[kMx ? kMxScaleBytes : 1];   // MXFP4: the first key whose V is NaN, of each 32 dims
@@ -276,19 +260,9 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
   // zero column; both divisions correctly rounded, codes RNE with saturation, as the page
   // encoder); for the fp8 MFMA of k-half j lane (n, half) holds the codes of
   // Q[col][32 (2 j + half) + b], b < 32, and the scores take sq in their scale.
-  // MXFP4: the column in E2M3 terms (s2l_device.h), for the MFMA of k-half j lane (n, half) those of dims
-  // 32 (2 j + half) .. + 31; made once the first copies are on their way.
   i32x8 q8[2];
-  u32x4 q_raw[kMx ? 8 : 1];
-  u32x6 q6[2][3];
-  uint32_t q_scales[2] = {0, 0};
   if constexpr (!kWiden) {
     // copied through LDS below, so that its latency overlaps that of the first K and V tiles
-  } else if constexpr (kMx) {
-    const uint16_t* qrow = q + ((int64_t)(row0 + (valid ? tok : 0)) * hq + (valid ? hq_col : 0)) * 128 + 32 * half;
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-      q_raw[k] = valid ? *reinterpret_cast<const u32x4*>(qrow + 64 * (k >> 2) + 8 * (k & 3)) : u32x4{0, 0, 0, 0};
   } else if constexpr (!kQ8) {
     const uint16_t* qrow = q + ((int64_t)(row0 + (valid ? tok : 0)) * hq + (valid ? hq_col : 0)) * 128 + 8 * half;
 #pragma unroll
@@ -339,12 +313,6 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
   for (int j = 0; j < 2; ++j)
 #pragma unroll
     for (int t = 0; t < 2; ++t) ka8[j][t] = grp_base + n * kRowBytes + (((4 * j + 2 * half + t) ^ (n & 15)) << 4);
-  // MXFP4: chunk 2 j + half of row n (a block of 32 dims), at that chunk ^ ((n >> 2) & 3): 16 consecutive
-  // lanes hit 64 banks; the row's scales, of which the MFMA takes bytes half and 2 + half.
-  uint32_t kmx[2];
-#pragma unroll
-  for (int j = 0; j < 2; ++j) kmx[j] = grp_base + n * kMxCodeBytes + (((2 * j + half) ^ ((n >> 2) & 3)) << 4);
-  const uint32_t kmx_scale = grp_base + kMxTileScales + n * kMxScaleBytes;
   // V^T (A of O^T += V^T P^T), d-block db, first 4-key set of k-step 0: within each group
   // of 16 lanes, lane j addresses key row (j >> 2) at column 32 db + 16 ((l >> 4) & 1) +
   // 4 (j & 3); the transposing read hands lane i the four keys of column base + i, so lane
@@ -475,30 +443,17 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
     for (int i = 0; i < kF8Loads; ++i)
       st.x[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, vo[i], 0, 0));
   };
-  // MXFP4: codes and scales of page pg of the tile of K at key kb, copied straight into LDS, lane l the
-  // chunk that row l / 4 holds at position l % 4.  Two waves that share a page split the two copies.  Keys at or
-  // past `hi` come with their page: their scores are masked, whatever they are.
-  const uint32_t kmx_vo = (lane >> 2) * kMxCodeBytes + (((lane & 3) ^ ((lane >> 4) & 3)) << 4);
-  auto mx_copy_k = [&](int32_t pg, int kb, int dst) {
-    const uint32_t lds = (uint32_t)(uintptr_t)(lds_void*)smem + grp_base + dst;
-    const i32x4 rs = sgpr_rsrc(kpb + (int64_t)pg * page_stride, kb + 16 * pw < hi ? kRun : 0);
-    if (kQuarters == 1 || cw % kQuarters == 0)
-      lds_dma_b128(rs, kmx_vo, __builtin_amdgcn_readfirstlane(lds + 16 * pw * kMxCodeBytes));
-    if ((kQuarters == 1 || cw % kQuarters == 1) && lane < 16)
-      lds_dma_b32(rs, kMxScalesAt + lane * kMxScaleBytes,
-                  __builtin_amdgcn_readfirstlane(lds + kMxTileScales + 16 * pw * kMxScaleBytes));
-  };
-  // e4m3 -> bf16 into the permuted rows: 16 codes = bf16 chunks 2f, 2f + 1.  MXFP4 (V alone): 16 or 32 codes,
-  // the chunks from 16 f / kMxLanes on.  A block that is NaN (or past bf16's range) goes in with values of 2^-125
+  // e4m3 -> bf16 into the permuted rows: 16 codes = bf16 chunks 2f, 2f + 1.  MXFP4: 16 or 32 codes, the
+  // chunks from 16 f / kMxLanes on.  A block of V that is NaN (or past bf16's range) goes in with values of 2^-125
   // and less, and its key (of the tile at key kb) into nan_key: 0 times NaN would reach the columns that do not
-  // see the key.  So what keys at or past `hi` hold has no effect: no column sees them.
+  // see the key.  So what keys at or past `hi` hold has no effect: no column sees them, and their scores are masked.
   int32_t nan_key = kNoNan;
   auto f8_store = [&](const F8Stage& st, int dst, bool is_k, int kb) {
     if constexpr (kMx) {
       const int row = 16 * pw + s0 + lane / kMxLanes, f = lane % kMxLanes;
-      const int sw = (row & 3) << 2;
+      const int sw = is_k ? (row & 15) : ((row & 3) << 2);
       uint8_t* rp = smem + grp_base + dst + row * kRowBytes;
-      const bool bad = st.scale > 252u;
+      const bool bad = !is_k && st.scale > 252u;
       nan_key = bad && kb + row < nan_key ? kb + row : nan_key;
       const float scale = mx_scale(bad ? 0u : st.scale);
 #pragma unroll
@@ -541,37 +496,10 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
   auto mfma_q8 = [&](const i32x8& a, const i32x8& b, const f32x16& c) {
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);
   };
-  // MXFP4: the codes of K for k-half j, and the key's scales (from this lane's first byte on), of the
-  // sub-block at LDS byte `kofs`; S^T += K Q^T over 64 dims of one of the two parts of Q.
-  auto read_kmx = [&](int kofs, int j) { return *reinterpret_cast<const u32x4*>(smem + kofs + kmx[j]); };
-  auto read_kmx_scale = [&](int kofs) {
-    const int at = (kofs & ~(kTileBytes - 1)) + (kofs & kMxSubBytes ? 32 * kMxScaleBytes : 0);
-    return *reinterpret_cast<const uint32_t*>(smem + at + kmx_scale) >> (8 * half);
-  };
-  // Term i % 3 of Q against half i / 3 of the dims, i < 6.
-  auto mfma_mx = [&](const u32x4* k, uint32_t scale, int i, const f32x16& c) {
-    switch (i) {
-      case 0: return mx_mfma<0, 0>(k[0], q6[0][0], c, scale, q_scales[0]);
-      case 1: return mx_mfma<0, 1>(k[0], q6[0][1], c, scale, q_scales[0]);
-      case 2: return mx_mfma<0, 2>(k[0], q6[0][2], c, scale, q_scales[0]);
-      case 3: return mx_mfma<1, 0>(k[1], q6[1][0], c, scale, q_scales[1]);
-      case 4: return mx_mfma<1, 1>(k[1], q6[1][1], c, scale, q_scales[1]);
-      default: return mx_mfma<1, 2>(k[1], q6[1][2], c, scale, q_scales[1]);
-    }
-  };
-  // S(b+1) = K(b+1) Q^T from the sub-block at LDS byte `kofs`.  MXFP4: less m, which is in every register that
-  // the MFMAs start from, and in units of the exponents of the probabilities, as Q holds the softmax's factor.
-  f32x16 s_begin = f32x16{};
-  // the exponent of the probability of a score
-  auto exponent = [&](float s) { return kMx ? s : __builtin_fmaf(s, c_log2, -m_run); };
+  // S(b+1) = K(b+1) Q^T from the sub-block at LDS byte `kofs`.
   auto qk = [&](int kofs) {
-    f32x16 s = s_begin;
-    if constexpr (kMx) {
-      const uint32_t scale = read_kmx_scale(kofs);
-      const u32x4 k[2] = {read_kmx(kofs, 0), read_kmx(kofs, 1)};
-#pragma unroll
-      for (int i = 0; i < 6; ++i) s = mfma_mx(k, scale, i, s);
-    } else if constexpr (kQ8) {
+    f32x16 s = f32x16{};
+    if constexpr (kQ8) {
       s = mfma_q8(read_k8(kofs, 0), q8[0], s);
       s = mfma_q8(read_k8(kofs, 1), q8[1], s);
     } else {
@@ -605,17 +533,11 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
   struct Pre {
     bf16x8 k[2], v[2];
     i32x8 k8[2];   // kQ8: both fp8 K operands of the step
-    u32x4 kmx[2];  // MXFP4: both operands of K, and their scales
-    uint32_t kmx_scale;
   };
   auto prefetch = [&](int kofs, int vofs, auto with_qk) {
     Pre f;
     if constexpr (decltype(with_qk)::value) {
-      if constexpr (kMx) {
-        f.kmx[0] = read_kmx(kofs, 0);
-        f.kmx[1] = read_kmx(kofs, 1);
-        f.kmx_scale = read_kmx_scale(kofs);
-      } else if constexpr (kQ8) {
+      if constexpr (kQ8) {
         f.k8[0] = read_k8(kofs, 0);
         f.k8[1] = read_k8(kofs, 1);
       } else {
@@ -636,62 +558,41 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
                        auto with_qk, float& lsum, auto with_next, int nkofs, int nvofs, Pre& nxt, auto&& hook) {
     constexpr bool kQK = decltype(with_qk)::value;
     constexpr bool kNext = decltype(with_next)::value;
-    f32x16 sn = s_begin;
+    f32x16 sn = f32x16{};
     bf16x8 kf[10], vf[10];
     kf[0] = f.k[0];
     kf[1] = f.k[1];
     vf[0] = f.v[0];
     vf[1] = f.v[1];
     float l0 = 0.f, l1 = 0.f;
-    // MXFP4: a wave within a step goes before one that settles, masks or stages V: another two percent
-    if constexpr (kMx) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if (i + 2 < 8) {
-        if constexpr (kQK && !kQ8 && !kMx) kf[i + 2] = read_k(kofs, i + 2);
+        if constexpr (kQK && !kQ8) kf[i + 2] = read_k(kofs, i + 2);
         vf[i + 2] = read_v(vofs, (i + 2) >> 2, (i + 2) & 3);
       } else if constexpr (kNext) {
-        if constexpr (kMx) {
-          nxt.kmx[i - 6] = read_kmx(nkofs, i - 6);
-          if (i == 6) nxt.kmx_scale = read_kmx_scale(nkofs);
-        } else if constexpr (kQ8) nxt.k8[i - 6] = read_k8(nkofs, i - 6);
+        if constexpr (kQ8) nxt.k8[i - 6] = read_k8(nkofs, i - 6);
         else nxt.k[i - 6] = read_k(nkofs, i - 6);
         nxt.v[i - 6] = read_v(nvofs, 0, i - 6);
       }
-      if constexpr (kQK && kMx) {
-        if (i < 6) sn = mfma_mx(f.kmx, f.kmx_scale, i, sn);
-      } else if constexpr (kQK && kQ8) {
+      if constexpr (kQK && kQ8) {
         if (i < 2) sn = mfma_q8(f.k8[i], q8[i], sn);   // the two fp8 MFMAs in the first slots
       } else if constexpr (kQK) {
         sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[i], sn, 0, 0, 0);
       }
       o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i], __builtin_bit_cast(bf16x8, pp[i >> 2]), o[i & 3],
                                                           0, 0, 0);
-      const float p0 = __builtin_amdgcn_exp2f(exponent(s[2 * i]));
-      const float p1 = __builtin_amdgcn_exp2f(exponent(s[2 * i + 1]));
+      const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * i], c_log2, -m_run));
+      const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * i + 1], c_log2, -m_run));
       const uint32_t pk = pack_bf16x2(p0, p1);
       po[i >> 2][i & 3] = pk;
       if (i & 1) l1 = sum_bf16x2(pk, l1);
       else l0 = sum_bf16x2(pk, l0);
       if (i == 1) hook();
     }
-    if constexpr (kMx) __builtin_amdgcn_s_setprio(0);
     lsum = l0 + l1;
     __asm__ volatile("" ::"v"(po[0]), "v"(po[1]), "v"(lsum));   // produced here, not sunk
-    if constexpr (kMx) {
-      // six of the eight slots have a score MFMA, of 32 cycles as the other's
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (kQK && i < 6) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // MFMA (S)
-          __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);   // VALU
-        }
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);     // MFMA (O)
-        if (i < 6) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);          // LDS reads (V)
-        else if (kNext) __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);     // LDS reads (K, V)
-        __builtin_amdgcn_sched_group_barrier(0x002, kQK ? 3 : 6, 0);
-      }
-    } else if constexpr (!kQ8) {
+    if constexpr (!kQ8) {
       slot_schedule<kQK, true>();
       slot_schedule<kQK, true>();
       slot_schedule<kQK, true>();
@@ -739,10 +640,10 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
     float l0 = 0.f, l1 = 0.f;
 #pragma unroll
     for (int e = 0; e < 16; e += 4) {
-      const float p0 = __builtin_amdgcn_exp2f(exponent(s[e]));
-      const float p1 = __builtin_amdgcn_exp2f(exponent(s[e + 1]));
-      const float p2 = __builtin_amdgcn_exp2f(exponent(s[e + 2]));
-      const float p3 = __builtin_amdgcn_exp2f(exponent(s[e + 3]));
+      const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c_log2, -m_run));
+      const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e + 1], c_log2, -m_run));
+      const float p2 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e + 2], c_log2, -m_run));
+      const float p3 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e + 3], c_log2, -m_run));
       const uint32_t pk0 = pack_bf16x2(p0, p1), pk1 = pack_bf16x2(p2, p3);
       p[e >> 3][(e >> 1) & 3] = pk0;
       p[e >> 3][((e >> 1) & 3) + 1] = pk1;
@@ -757,22 +658,16 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
   // reference raised to that sub-block's exact max: O and l, which hold only earlier
   // sub-blocks, are rescaled and P is recomputed (rare branch).  Then the sum joins l.  The
   // reference of a column is shared by its lane pair, and so is the decision.
-  auto settle = [&](f32x16& s, u32x4* p, float& lsum, f32x16* next) {
+  auto settle = [&](const f32x16& s, u32x4* p, float& lsum) {
     if (__builtin_amdgcn_ballot_w64(lsum > kOverflow) != 0) {
       __asm__ volatile("" ::);
       const bool over = max_with_partner(lsum) > kOverflow;
-      const float t = kMx ? m_run + block_max(s) : block_max(s) * c_log2;
+      const float t = block_max(s) * c_log2;
       const float m_new = over ? t : m_run;
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
 #pragma unroll
       for (int db = 0; db < 4; ++db) o[db] *= alpha;
       l_run *= alpha;
-      if constexpr (kMx) {   // the scores of this sub-block and of the next one are less the old reference
-        const float up = m_new - m_run;
-        s -= up;
-        if (next != nullptr) *next -= up;
-        s_begin = f32x16{} - m_new;
-      }
       m_run = m_new;
       probs(s, p, lsum);
     }
@@ -814,12 +709,10 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
       __builtin_amdgcn_s_barrier();
       advance_window(t + kS + 1);
     } else {
-      if constexpr (kMx) wait_vmcnt<0>();   // this wave's copies of iteration t - 1
       wait_lgkmcnt0();
-      __builtin_amdgcn_s_barrier();   // the stores (and copies) of iteration t - 1 are visible
-      if constexpr (kMx) mx_copy_k(pg_knext, lo + (t + 2) * kKvTile, kKBase + kJ * kTileBytes);
+      __builtin_amdgcn_s_barrier();   // the stores of iteration t - 1 are visible
       f8_load(vst, vpb, pg_klast, lo + (t + 1) * kKvTile, vvo);
-      if constexpr (!kMx) f8_load(kst, kpb, pg_knext, lo + (t + 2) * kKvTile, kvo);
+      f8_load(kst, kpb, pg_knext, lo + (t + 2) * kKvTile, kvo);
       pg_klast = pg_knext;
       advance_window(t + 3);
       pg_knext = page_of(t + 3);
@@ -843,22 +736,22 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
     // sub-block 2t+1 (scores sc; P(2t) in pa, from scores sp)
     {
       const Pre f = prefetch(kcur, vcur, kWithQK);
-      settle(sp, pa, lsum_p, &sc);
+      settle(sp, pa, lsum_p);
       mask(sc, sb1);
       float ls;
       const f32x16 sn =
-          step_main(sc, pa, pb, kcur, vcur, f, kWithQK, ls, kWithNext, kcur + kKSub, vcur + kSubBytes, f2, copies);
+          step_main(sc, pa, pb, kcur, vcur, f, kWithQK, ls, kWithNext, kcur + kSubBytes, vcur + kSubBytes, f2, copies);
       sp = sc;
       sc = sn;
       lsum_p = ls;
     }
     // sub-block 2t+2 (P(2t+1) in pb)
     {
-      settle(sp, pb, lsum_p, &sc);
+      settle(sp, pb, lsum_p);
       mask(sc, sb1 + 32);
       float ls;
       const f32x16 sn =
-          step_main(sc, pb, pa, kcur + kKSub, vcur + kSubBytes, f2, kWithQK, ls, kNoNext, 0, 0, f2, no_hook);
+          step_main(sc, pb, pa, kcur + kSubBytes, vcur + kSubBytes, f2, kWithQK, ls, kNoNext, 0, 0, f2, no_hook);
       sp = sc;
       sc = sn;
       lsum_p = ls;
@@ -866,7 +759,7 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
     if constexpr (kWiden) {
       // K(t + 2) into stage t % 2 (K(t) there was last read in iteration t - 1), V(t + 1)
       // into stage (t + 1) % 2 (V(t - 1) there likewise)
-      if constexpr (!kMx) f8_store(kst, kKBase + kJ * kTileBytes, true, lo + (t + 2) * kKvTile);
+      f8_store(kst, kKBase + kJ * kTileBytes, true, lo + (t + 2) * kKvTile);
       f8_store(vst, kVBase + ((kJ + 1) % 2) * kTileBytes, false, lo + (t + 1) * kKvTile);
     }
   };
@@ -982,29 +875,14 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
       pg_klast = pg[kS - 1];
       pg_knext = pg[kS];
     } else {
-      if constexpr (kMx) {
-        mx_copy_k(pg[0], lo, kKBase);
-        mx_copy_k(pg[1], lo + kKvTile, kKBase + kTileBytes);
-      } else {
-        f8_load(kst, kpb, pg[0], lo, kvo);
-      }
+      f8_load(kst, kpb, pg[0], lo, kvo);
       f8_load(vst, vpb, pg[0], lo, vvo);
       fetch_window(0, 1);
       if (ntiles > 64 - kS - 2) fetch_window(64, 0);
-      if constexpr (kMx) {
-        const QueryTerms q0 = split_queries(q_raw[0], q_raw[1], q_raw[2], q_raw[3], scale_log2);
-        const QueryTerms q1 = split_queries(q_raw[4], q_raw[5], q_raw[6], q_raw[7], scale_log2);
-#pragma unroll
-        for (int i = 0; i < 3; ++i) q6[0][i] = q0.t[i], q6[1][i] = q1.t[i];
-        q_scales[0] = q0.scales;
-        q_scales[1] = q1.scales;
-      }
-      if constexpr (!kMx) f8_store(kst, kKBase, true, lo);
+      f8_store(kst, kKBase, true, lo);
       f8_store(vst, kVBase, false, lo);
-      if constexpr (!kMx) {
-        f8_load(kst, kpb, pg[1], lo + kKvTile, kvo);
-        f8_store(kst, kKBase + kTileBytes, true, lo + kKvTile);
-      }
+      f8_load(kst, kpb, pg[1], lo + kKvTile, kvo);
+      f8_store(kst, kKBase + kTileBytes, true, lo + kKvTile);
       pg_klast = pg[1];
       pg_knext = pg[2];
       // the windows, and every load: one still pending in the compiler's count on some path
@@ -1019,15 +897,11 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
     sp = qk(kKBase);
     mask(sp, lo);
     {
-      const float t = kMx ? block_max(sp) : block_max(sp) * c_log2;
+      const float t = block_max(sp) * c_log2;
       m_run = t == -INFINITY ? 0.f : t;
-      if constexpr (kMx) {
-        sp -= m_run;
-        s_begin = f32x16{} - m_run;
-      }
     }
     probs(sp, pa, lsum_p);
-    sc = qk(kKBase + kKSub);
+    sc = qk(kKBase + kSubBytes);
   } else {
     append_rows();
   }
@@ -1064,17 +938,17 @@ __global__ __launch_bounds__(kColWaves * kHalves * 64, 8 / (kColWaves * kHalves)
   }
   if (ntiles > 0) {
     // last tile (t = ntiles - 1): sub-block 2t+1 takes the softmax, P(2t) V, then P(2t+1) V
-    if constexpr (!kWiden || kMx) wait_vmcnt<0>();
-    if constexpr (kWiden) wait_lgkmcnt0();
+    if constexpr (!kWiden) wait_vmcnt<0>();
+    else wait_lgkmcnt0();
     __builtin_amdgcn_s_barrier();
     const int vlast = kVBase + (t % kS) * kTileBytes;
     constexpr std::false_type kNoQK{};
     Pre f = prefetch(0, vlast, kNoQK);
-    settle(sp, pa, lsum_p, &sc);
+    settle(sp, pa, lsum_p);
     mask(sc, lo + (2 * t + 1) * 32);
     float ls;
     step_main(sc, pa, pb, 0, vlast, f, kNoQK, ls, std::false_type{}, 0, 0, f, [] {});
-    settle(sc, pb, ls, nullptr);
+    settle(sc, pb, ls);
     pv_acc(pb, vlast + kSubBytes);
   }
 

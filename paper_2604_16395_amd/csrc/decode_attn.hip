@@ -44,8 +44,8 @@
 // byte a wave reads it wrote itself.
 //
 // MXFP4 pages: 136 bytes a key and head are a quarter of bf16's, with the same work on them: 64 rows of 8192 keys (32q/8kv)
-// 99 us, 5.8 TB/s; one row of 2047 keys 5.6 us and its merge 2.8.  K as codes on the f8f6f4 MFMA, as the prefill kernel
-// multiplies it, took 8.4 us for 7.8 for the row and 138 for 115 over 922 short rows (the queries' terms come first) and
+// 99 us, 5.8 TB/s; one row of 2047 keys 5.6 us and its merge 2.8.  K as codes on the f8f6f4 MFMA, by terms of the
+// queries, took 8.4 us for 7.8 for the row and 138 for 115 over 922 short rows (the queries' terms come first) and
 // gained 1% on long ones; register sets three to five deep took 1.06 to 1.18 times the time.
 #include "launch.h"
 #include "plan_rules.h"

@@ -13,9 +13,6 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x6 __attribute__((ext_vector_type(6)));
-typedef _Float16 f16x32 __attribute__((ext_vector_type(32)));
-typedef float f32x32 __attribute__((ext_vector_type(32)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 __device__ inline uint32_t f2u(float x) { return __builtin_bit_cast(uint32_t, x); }
@@ -94,51 +91,6 @@ __device__ inline uint32_t mx_scale_byte(uint32_t magnitude) {
 // The codes of eight dims of such a block: 0 where it is NaN.
 __device__ inline uint32_t mx_encode8(const u32x4& x, uint32_t byte) {
   return byte == 255u ? 0u : bf16x8_to_fp4x8(x, mx_scale(byte));
-}
-
-// Queries against MXFP4 keys on the f8f6f4 MFMA, which takes the keys' codes and scales as they are stored and,
-// against E2M3 values, runs at twice the rate of bf16.  Queries enter times a factor (the softmax's, so that the
-// products are the exponents of the probabilities), as the sum of three E2M3 values with one power of two for
-// each 32 dims, as the keys have it:
-//   factor q = 2^(s - 127) (t0 + t1 / 8 + t2 / 256 + rest),
-// each value the nearest to what the ones before leave (at most 7.5).  The block's largest goes to [4, 8), so t0
-// leaves at most 1/4 (1/2 from 7.75 on), t1 2^-7 (2^-6), t2 2^-12 (2^-11); what t0 leaves is rounded to f16 on the
-// way, 2^-14 (2^-13) at most.  So |rest| <= 2^-13 of the block's largest: 14 bits below it, where bf16 has 8.
-struct QueryTerms {
-  u32x6 t[3];
-  uint32_t scales;     // of t0 .. t2, a byte each: 255 (NaN) where a query is not finite
-};
-__device__ inline QueryTerms split_queries(const u32x4& a, const u32x4& b, const u32x4& c, const u32x4& d, float factor) {
-  const uint32_t m = max_u16x2(max_u16x2(max_magnitude(a), max_magnitude(b)), max_u16x2(max_magnitude(c), max_magnitude(d)));
-  // the exponent of (largest x factor), each taken as a number in [1, 2) and a power of two: no overflow on the way
-  const uint32_t f = f2u(factor);
-  const float top = u2f((m << 16 & 0x7FFFFFu) | 0x3F800000u) * u2f((f & 0x7FFFFFu) | 0x3F800000u);
-  const int fe = (int)(f >> 23), e = (int)(m >> 7) + fe - 127 + (top >= 2.f) - 2;
-  // at least 9, for the third value's byte, and what keeps the multiplier finite: queries that this makes
-  // smaller than [4, 8) are below 2^-120
-  const int least = fe - 126 > 9 ? fe - 126 : 9;
-  const int s = e < least ? least : e > 254 ? 254 : e;
-  const float times = __builtin_ldexpf(u2f((f & 0x7FFFFFu) | 0x3F800000u), fe - s);   // factor 2^(127 - s)
-  float y[32];
-  f16x32 left;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const uint32_t w = i < 4 ? a[i & 3] : i < 8 ? b[i & 3] : i < 12 ? c[i & 3] : d[i & 3];
-    y[2 * i] = bf16lo(w) * times;
-    y[2 * i + 1] = bf16hi(w) * times;
-  }
-#pragma unroll
-  for (int i = 0; i < 32; ++i) left[i] = (_Float16)y[i];
-  QueryTerms r;
-  r.scales = m >= 0x7F80u ? 0xFFFFFFFFu : (uint32_t)(s | (s - 3) << 8 | (s - 8) << 16);
-  r.t[0] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_f16(left, 1.f);
-  const f32x32 t0 = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(r.t[0], 1.f);
-#pragma unroll
-  for (int i = 0; i < 32; ++i) left[i] = (_Float16)(y[i] - t0[i]);
-  r.t[1] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_f16(left, 0.125f);
-  left -= __builtin_amdgcn_cvt_scalef32_pk32_f16_fp6(r.t[1], 0.125f);
-  r.t[2] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_f16(left, 0.00390625f);
-  return r;
 }
 
 // x of lane l ^ 1, l ^ 2, and of the lane opposite in its eight (for a value that is equal in each four).
