@@ -159,7 +159,7 @@ typedef struct s2l_plan_info {
   int32_t num_tiles;       /* query tiles (a split tile has one item per key-range piece)   */
   int64_t part_floats;     /* fp32 words of split partials in the workspace                 */
   int32_t key_halves;      /* wave groups per work item (1 or 2)                            */
-  int32_t flags;           /* S2L_PLAN_UNIFORM: the items' key ranges are within 25% of     */
+  int16_t flags;           /* S2L_PLAN_UNIFORM: the items' key ranges are within 25% of     */
                            /* their mean, so consecutive items (one kv head's pages) are    */
                            /* grouped onto one XCD's L2.  S2L_PLAN_BINNED: items of unequal */
                            /* cost, each (request, kv head) group placed whole on the XCD   */
@@ -168,6 +168,8 @@ typedef struct s2l_plan_info {
                            /* them).  Otherwise (the bins would not balance to within 4%)   */
                            /* items run longest request first, spread over the XCDs, so the */
                            /* dispatcher balances them                                      */
+  uint16_t lengths;        /* a digest of the batch's lengths: attention refuses a plan for */
+                           /* another batch (EINVAL)                                        */
 } s2l_plan_info;
 #define S2L_PLAN_UNIFORM 1
 #define S2L_PLAN_BINNED 2

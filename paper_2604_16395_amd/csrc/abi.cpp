@@ -420,6 +420,19 @@ bool bin_groups(int32_t R, const int32_t* P, const int32_t* C, int32_t hkv, int3
   return s2l::bins_balanced(bins);
 }
 
+// A digest of the lengths of a batch, by which attention knows a plan that was made for another: one product a
+// request (no time beside the checks of the lengths), and a plan of other lengths passes once in 2^16.
+uint16_t lengths_digest(int32_t R, const int32_t* P, const int32_t* C) {
+  uint64_t sum = 0;
+  uint32_t a = 0, b = 0;
+  for (int32_t r = 0; r < R; ++r) {
+    a += 0x9E3779B9u;   // odd: every request's pair is its own
+    b += 0x85157AF5u;
+    sum += (uint64_t)((uint32_t)P[r] + a) * ((uint32_t)C[r] + b);
+  }
+  return (uint16_t)((sum * 0x9E3779B97F4A7C15ull) >> 48);
+}
+
 // Host plan: the partition the device plan kernel stores (same rules, same order).
 void host_plan(int32_t R, const int32_t* P, const int32_t* C, int32_t hq, int32_t hkv, const Resolved& o,
                s2l_plan_info* info, int32_t* items, int64_t cap) {
@@ -463,6 +476,7 @@ void host_plan(int32_t R, const int32_t* P, const int32_t* C, int32_t hq, int32_
   info->num_tiles = (int32_t)n_tiles;
   info->part_floats = part;
   info->key_halves = o.key_halves;
+  info->lengths = lengths_digest(R, P, C);
   // item key ranges: tile t of request r covers keys [0, P + i1), cut into ns pieces
   int64_t keys_sum = 0, keys_max = 0;
   for (int32_t r = 0; r < R; ++r) {
@@ -539,6 +553,9 @@ s2l_status attn_common(const s2l_kv_cache* cache, const s2l_batch* batch, const 
   if (cache->dtype == S2L_KV_MXFP4 && plan && plan->tile_cols != s2l::kDecodeTileCols && !(scale >= 0x1p-120f && scale <= 0x1p120f))
     return fail(S2L_ENOTSUP, "softmax_scale %g over MXFP4 pages unsupported (2^-120 to 2^120)", (double)scale);
   if (*T > 0 && (!q || !out)) return fail(S2L_EINVAL, "q/out is NULL");
+  if (plan && plan->num_reqs == batch->num_reqs &&
+      plan->lengths != lengths_digest(batch->num_reqs, batch->prefix_lens_host, batch->chunk_lens_host))
+    return fail(S2L_EINVAL, "plan was made for another batch (its lengths differ)");
   return check_plan(plan, batch, hq, cache->num_kv_heads, *T, ws, ws_bytes);
 }
 
