@@ -101,9 +101,10 @@ class PagedKVCache:
 
     def _check_runs(self):
         k, v = self.k_pages, self.v_pages
-        if k.dim() != 3 or k.shape[2] != MXFP4_RUN_BYTES or v.shape != k.shape or k.dtype != torch.uint8 or v.dtype != torch.uint8:
-            raise ValueError(f"MXFP4 pools must be uint8 [num_pages][Hkv][{MXFP4_RUN_BYTES}] of one shape (got "
-                             f"{k.dtype} {tuple(k.shape)} and {v.dtype} {tuple(v.shape)})")
+        if (k.dim() != 3 or k.shape[2] != MXFP4_RUN_BYTES or v.shape != k.shape or k.dtype != torch.uint8 or v.dtype != torch.uint8
+                or not k.is_contiguous() or not v.is_contiguous()):
+            raise ValueError(f"MXFP4 pools must be contiguous uint8 [num_pages][Hkv][{MXFP4_RUN_BYTES}] of one shape (got "
+                             f"{k.dtype} {tuple(k.shape)}, strides {k.stride()}, and {v.dtype} {tuple(v.shape)}, strides {v.stride()})")
 
     @property
     def num_pages(self):

@@ -133,13 +133,17 @@ bool cache_arg(PyObject* o, s2l_kv_cache* c) {
     if (PyErr_Occurred() || x < 0 || x > INT32_MAX) return false;
     n[i] = (int32_t)x;
   }
-  if (mx.o == Py_True) {
-    if (n[2] != S2L_MXFP4_RUN_BYTES || fp8.o == Py_True) return false;
+  void *ks = nullptr, *vs = nullptr;
+  if (mx.o == Py_True) {   // both pools in full, as they may be others than those that the cache was made of
+    const Ref v(PyObject_GetAttr(o, s_v_pages));
+    if (n[2] != S2L_MXFP4_RUN_BYTES || fp8.o == Py_True || !v || !tensor(k.o, u8, &c->k_pages) || !tensor(v.o, u8, &c->v_pages)) return false;
+    const Ref v_shape(PyObject_GetAttr(v.o, s_shape));
+    if (!v_shape || PyObject_RichCompareBool(shape.o, v_shape.o, Py_EQ) != 1) return false;
     n[2] = S2L_PAGE_SIZE;
     n[3] = S2L_HEAD_DIM;
+  } else if (!data_ptr(k.o, &c->k_pages) || !attr_data_ptr(o, s_v_pages, &c->v_pages)) {
+    return false;
   }
-  void *ks = nullptr, *vs = nullptr;
-  if (!data_ptr(k.o, &c->k_pages) || !attr_data_ptr(o, s_v_pages, &c->v_pages)) return false;
   if (fp8.o == Py_True && (!attr_data_ptr(o, s_k_scale, &ks) || !attr_data_ptr(o, s_v_scale, &vs))) return false;
   c->k_scale = static_cast<const float*>(ks);
   c->v_scale = static_cast<const float*>(vs);
