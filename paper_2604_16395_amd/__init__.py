@@ -458,13 +458,15 @@ def s2l_linear_attn(state, batch, q, k, v, scale, out, workspace=None, stream=No
 
 
 def _swap(name, cache, pairs, host_k, host_v, stream):
-    _check(pairs, torch.int32, "pairs")
-    if pairs.dim() != 2 or pairs.shape[1] != 2 or not pairs.is_cuda:
-        raise ValueError("pairs must be a device int32 tensor [n][2]")
     if host_k.is_cuda or host_v.is_cuda or host_k.dtype != cache.k_pages.dtype or host_v.dtype != host_k.dtype:
         raise ValueError("host pools must be host tensors of the cache's element type")
     if not (host_k.is_contiguous() and host_v.is_contiguous()) or host_k.shape != host_v.shape:
         raise ValueError("host pools must be contiguous and of one shape")
+    if host_k.dim() < 1 or host_k.numel() * cache.num_pages != cache.k_pages.numel() * host_k.shape[0]:
+        raise ValueError(f"host pools must hold pages of the cache's size ({tuple(cache.k_pages.shape[1:])}, got {tuple(host_k.shape)})")
+    _check(pairs, torch.int32, "pairs")
+    if pairs.dim() != 2 or pairs.shape[1] != 2 or not pairs.is_cuda:
+        raise ValueError("pairs must be a device int32 tensor [n][2]")
     cc = cache.c()
     _lib.call(name, ctypes.byref(cc), _ptr(pairs), pairs.shape[0], _ptr(host_k), _ptr(host_v),
               host_k.shape[0], _stream(stream))
