@@ -255,7 +255,7 @@ s2l_status s2l_rope_kv_append(const s2l_kv_cache* cache, const s2l_batch* batch,
 typedef struct s2l_qk_norm {
   const void* q_weight;     /* device [128] for all query heads; NULL: factors of 1, without offset */
   const void* k_weight;     /* device [128] for all key heads, likewise                              */
-  float eps;                /* finite, > 0                                                           */
+  float eps;                /* finite, at least 2^-126                                               */
   float offset;             /* finite; 1 where weights are kept as their distance from one, else 0   */
   int32_t weight_dtype;     /* S2L_NORM_BF16 or S2L_NORM_FP32                                        */
   int32_t reserved;

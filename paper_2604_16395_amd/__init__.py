@@ -220,7 +220,7 @@ class QKNorm:
     """The norms of queries and keys for each head: x / sqrt(mean x^2 + eps) * (weight + offset).
 
     q_weight, k_weight: device [128], both bf16 or both fp32; None: no weight (nor offset).  offset: 1 where
-    weights are kept as their distance from one."""
+    weights are kept as their distance from one.  eps: at least 2^-126 (what is less is zero to the hardware's root)."""
 
     def __init__(self, q_weight=None, k_weight=None, eps=1e-6, offset=0.0):
         self.q_weight, self.k_weight, self.eps, self.offset = q_weight, k_weight, float(eps), float(offset)

@@ -636,7 +636,8 @@ s2l_status check_norm(const s2l_qk_norm* norm) {
   if (!norm) return fail(S2L_EINVAL, "norm is NULL");
   if (norm->weight_dtype != S2L_NORM_BF16 && norm->weight_dtype != S2L_NORM_FP32)
     return fail(S2L_EINVAL, "unknown norm weight dtype %d", norm->weight_dtype);
-  if (!(norm->eps > 0.0f) || !std::isfinite(norm->eps)) return fail(S2L_EINVAL, "norm eps must be finite and > 0");
+  // the kernel's root takes denormal numbers for zero
+  if (!(norm->eps >= 0x1p-126f) || !std::isfinite(norm->eps)) return fail(S2L_EINVAL, "norm eps must be finite and at least 2^-126");
   if (!std::isfinite(norm->offset)) return fail(S2L_EINVAL, "norm offset must be finite");
   const uintptr_t size = norm->weight_dtype == S2L_NORM_FP32 ? 4 : 2;
   for (const void* w : {norm->q_weight, norm->k_weight})
