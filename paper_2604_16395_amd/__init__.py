@@ -304,7 +304,7 @@ def _load_native():
         device, raw_stream = (getattr(torch._C, n, None) for n in ("_cuda_getDevice", "_cuda_getCurrentRawStream"))
         _native = _lib.binding((torch.Tensor, PagedKVCache, Batch, s2l_plan_opts, s2l_plan_info, torch.cuda.Stream,
                                 torch.bfloat16, torch.float32, torch.uint8, torch.cuda.is_initialized, device, raw_stream,
-                                Rope, LinearState, torch.int32, QKNorm))
+                                Rope, LinearState, torch.int32, QKNorm, torch.nn.Parameter))
     return _native
 
 

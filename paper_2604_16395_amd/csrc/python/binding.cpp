@@ -33,7 +33,7 @@ struct Entry {
 } lib;
 
 PyObject *tensor_type, *cache_type, *batch_type, *opts_type, *info_type, *stream_type, *bf16, *f32, *u8, *is_initialized, *get_device, *get_stream,
-    *rope_type, *state_type, *i32, *norm_type;
+    *rope_type, *state_type, *i32, *norm_type, *parameter_type;
 PyObject *s_dtype, *s_data_ptr, *s_is_contiguous, *s_shape, *s_numel, *s_k_pages, *s_v_pages, *s_k_scale, *s_v_scale,
     *s_fp8, *s_prefix_host, *s_chunk_host, *s_tables_host, *s_prefix_lens, *s_chunk_lens, *s_cu_chunk, *s_block_tables,
     *s_cuda_stream, *s_stride, *s_get_device, *s_inv_freq, *s_positions, *s_pair_axis, *s_adjacent, *s_scale, *s_states, *s_log_decay,
@@ -319,13 +319,13 @@ bool rope_arg(PyObject* o, int64_t tokens, long dev, s2l_rope* r) {
   return true;
 }
 
-// A QKNorm's weight: None, or a contiguous device vector of 128 of the type that `dtype` names, which the
-// first weight sets.
+// A QKNorm's weight: None, or a contiguous device vector of 128 (a tensor, or a module's parameter) of the type that
+// `dtype` names, which the first weight sets.
 bool weight_arg(PyObject* o, PyObject* name, long dev, int32_t* dtype, const void** w) {
   const Ref t(PyObject_GetAttr(o, name));
   *w = nullptr;
   if (!t || t.o == Py_None) return t.o == Py_None;
-  if ((PyObject*)Py_TYPE(t.o) != tensor_type) return false;
+  if ((PyObject*)Py_TYPE(t.o) != tensor_type && (PyObject*)Py_TYPE(t.o) != parameter_type) return false;
   const Ref d(PyObject_GetAttr(t.o, s_dtype)), c(PyObject_CallMethodNoArgs(t.o, s_is_contiguous));
   const int32_t type = d.o == f32 ? S2L_NORM_FP32 : d.o == bf16 ? S2L_NORM_BF16 : -1;
   void* p;
@@ -546,14 +546,14 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void* f[13];
   PyObject** o[] = {&tensor_type, &cache_type, &batch_type, &opts_type, &info_type, &stream_type,
-                    &bf16, &f32, &u8, &is_initialized, &get_device, &get_stream, &rope_type, &state_type, &i32, &norm_type};
-  if (n != 2 || !PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) != 16 || !PyTuple_Check(a[1]) || PyTuple_GET_SIZE(a[1]) != 13) {
+                    &bf16, &f32, &u8, &is_initialized, &get_device, &get_stream, &rope_type, &state_type, &i32, &norm_type, &parameter_type};
+  if (n != 2 || !PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) != 17 || !PyTuple_Check(a[1]) || PyTuple_GET_SIZE(a[1]) != 13) {
     PyErr_SetString(PyExc_TypeError, "setup(objects, addresses)");
     return nullptr;
   }
   for (int i = 0; i < 13; ++i)
     if (!to_ptr(PyTuple_GET_ITEM(a[1], i), &f[i])) return nullptr;
-  for (int i = 0; i < 16; ++i) {
+  for (int i = 0; i < 17; ++i) {
     Py_INCREF(PyTuple_GET_ITEM(a[0], i));
     Py_XSETREF(*o[i], PyTuple_GET_ITEM(a[0], i));
   }
