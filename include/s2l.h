@@ -343,7 +343,7 @@ s2l_status s2l_linear_attn(const s2l_linear_state* state, const s2l_batch* batch
  * Used by the tests and as the dense form of a swap-out.
  *   cu_out : device int32 [R+1] row offsets chosen by the caller (need not be dense).
  *   k_out, v_out: device, caller-owned, at least max_r(cu_out[r] + n_r) rows.
- * Errors: EINVAL (nulls, negative lengths), ERANGE (P_r + C_r > max_pages_per_req * 16),
+ * Errors: EINVAL (nulls, negative lengths, MXFP4 outputs off 4 bytes), ERANGE (P_r + C_r > max_pages_per_req * 16),
  * ENOTSUP (head_dim/page_size), EHIP.
  */
 s2l_status s2l_kv_gather(const s2l_kv_cache* cache, const s2l_batch* batch, int32_t include_chunk,

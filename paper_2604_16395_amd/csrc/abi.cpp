@@ -998,6 +998,8 @@ s2l_status s2l_kv_gather(const s2l_kv_cache* cache, const s2l_batch* batch, int3
     if (pages > max_read) max_read = pages;
   }
   if (max_read > 0 && (!cu_out || !k_out || !v_out)) return fail(S2L_EINVAL, "cu_out/k_out/v_out is NULL");
+  if (cache->dtype == S2L_KV_MXFP4 && (reinterpret_cast<uintptr_t>(k_out) % 4 != 0 || reinterpret_cast<uintptr_t>(v_out) % 4 != 0))
+    return fail(S2L_EINVAL, "k_out and v_out of MXFP4 rows must be aligned to 4 bytes");
   (void)hipGetLastError();
   hipError_t e = s2l::launch_kv_gather(kv_launch(cache, batch), include_chunk, cu_out, k_out, v_out, max_read,
                                        static_cast<hipStream_t>(stream));
