@@ -16,7 +16,7 @@ BATCHES = [  # long rows of a length, short rows of up to a length, the plan's o
     ("binned, short", 8, 700, 60, 300, BINNED, False, False),
     ("binned, many", 8, 2500, 92, 60, BINNED, True, True),
     ("binned, long, few", 8, 2500, 60, 60, BINNED, False, True),
-    ("binned, long pieces, few", 3, 9000, 24, 60, BINNED, False, False),
+    ("binned, pieces, few", 3, 9000, 24, 60, BINNED, False, True),
 ]
 
 
