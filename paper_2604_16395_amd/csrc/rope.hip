@@ -260,10 +260,11 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch a) {
 // Two heads a lane halve the waves and what each does beside its heads; as long as waves are few (6 a SIMD), more of them
 // hide more.  One head a lane and two, us in a graph, 32 + 8 + 8 heads: 512 rows 4.3 and 4.6, 1024 (6144 waves) 7.3 and 7.7,
 // 1365 (8190) 8.8 and 8.7, 2048 10.9 and 10.5, 4096 21.8 and 22.8, 8192 40.5 and 41.0.
-// With norms a head costs more beside what its lane shares (sines, weights), and rows whose heads fill waves of 32 take four
-// heads a lane.  Two, three and four, us in a graph: 2342 rows of 32 + 32 heads without pages 18.1, 18.8, 15.5, 20000 rows
-// 129, 123, 127; 1500 rows of 64 + 8 + 8 14.7, 16.7, 13.7; 5000 of 24 + 4 + 4 18.3, 19.4, 17.4, 20000 66.8, 74.9, 71.0.  Others two:
-// 35107 rows of 32 + 8 + 8 163.0, 164.2, 173.6, 4096 23.4, 24.3, 24.2, 20000 into e4m3 pages 90.7, 95.1, 105.8.
+// With norms, four heads a lane for rows of more than 32 heads without pages, and for rows appended whose heads are 7, 11 or
+// 15 groups of eight.  Time of four over that of two, mean of 1000 to 20000 rows: without pages 4 groups 1.04, 7 0.95, 8 0.96 and 1.00, 10 and 11 0.98, 12 to 16 0.99 to 1.01 (2342 rows of 32 + 32 heads 15.1 us
+// and 17.1); into bf16, e4m3 and MXFP4 pages 4 groups 1.09, 1.08, 1.08, 7 0.98, 0.91, 0.92, 8 1.03, 1.01, 1.01, 10 1.01, 1.00, 1.00,
+// 11 1.00, 0.96, 0.96, 12 1.02, 1.00, 1.00, 13 1.16, 1.21, 1.20, 14 1.03, 1.01, 1.01, 15 1.00, 0.91, 0.93, 16 1.02, 1.02, 1.02.
+// 35107 rows of 32 + 8 + 8 into bf16 pages with two, three and four: 163.0, 164.2, 173.6 us.
 template <bool kAdjacent, bool kAppend, PageKind kKind, bool kNorm>
 void launch(const RopeLaunch& a, hipStream_t stream) {
   constexpr int64_t kFewWaves = 6144;
@@ -275,8 +276,9 @@ void launch(const RopeLaunch& a, hipStream_t stream) {
         <<<dim3((uint32_t)(four_rows * ((groups + kHeads - 1) / kHeads))), 256, 0, stream>>>(a);
   };
   const int64_t waves = (groups + 3) / 4, a_lane = (groups + waves - 1) / waves;   // of a row: at most four heads a lane, evenly
+  const bool four = kNorm && groups > 4 && (kAppend ? groups % 4 == 3 : a_lane == 4);
   if (a.total_rows * groups <= kFewWaves || (kNorm && a_lane == 1)) run(std::integral_constant<int, 1>{});
-  else if (kNorm && a_lane == 4) run(std::integral_constant<int, kNorm ? 4 : 2>{});
+  else if (four) run(std::integral_constant<int, kNorm ? 4 : 2>{});
   else run(std::integral_constant<int, 2>{});
 }
 
