@@ -44,7 +44,7 @@
 // byte a wave reads it wrote itself.
 //
 // MXFP4 pages: 136 bytes a key and head are a quarter of bf16's, with the same work on them: 64 rows of 8192 keys (32q/8kv)
-// 99 us, 5.8 TB/s; one row of 2047 keys 5.6 us and its merge 2.8.  K as codes on the f8f6f4 MFMA, by terms of the
+// 109 us, 5.2 TB/s; one row of 2047 keys 5.6 us and its merge 2.8.  K as codes on the f8f6f4 MFMA, by terms of the
 // queries, took 8.4 us for 7.8 for the row and 138 for 115 over 922 short rows (the queries' terms come first) and
 // gained 1% on long ones; register sets three to five deep took 1.06 to 1.18 times the time.
 #include "launch.h"
@@ -63,10 +63,6 @@ constexpr int kVRow = kHeadDim * 2;             // bf16 key row in LDS
 template <PageKind kKind>
 constexpr int kTilePages = kKind == kBf16Pages ? 2 : 4;
 constexpr int kDNoNan = 0x7FFFFFFF;
-// MXFP4 codes are loaded as data that is read once (nt).  Against ordinary loads, cold: 64 equal rows of 8192 keys 110 -> 99 us,
-// of 4096 57.3 -> 53.0, 64 rows of up to 16384 (64q/8kv) 118.7 -> 116.3, 4 of 120000 104.9 -> 102.2, 300 of up to 2000 79.4 -> 76.7;
-// the same rows again and again, which the last-level cache holds in part, 113 -> 109, but 50.2 -> 52.5 where it holds most.
-constexpr int kStreamed = 2;
 constexpr float kDLn2 = 0.6931471805599453f;
 constexpr float kDOverflow = 18446744073709551616.0f;   // 2^64
 constexpr int32_t kDRsrcWord3 = 0x00020000;
@@ -201,10 +197,14 @@ __global__ __launch_bounds__(kDecodeWaves * 64, 2) void attn_decode_kernel(
       const int bytes = __builtin_amdgcn_readfirstlane(kMx ? (keys > 0 ? kRun : 0) : keys * kKeyBytes);
       const auto kr = page_rsrc(kpb + page * page_stride, bytes);
       const auto vr = page_rsrc(vpb + page * page_stride, bytes);
-      if constexpr (kMx) {   // K: key j, block q.  V: key l / 4, block l % 4
+      // MXFP4, K: key j, block q.  V: key l / 4, block l % 4.  Ordinary loads, as requests may share pages.  Against loads of
+      // data that is read once (nt), us: 64 requests that share 8192 keys (32q/8kv) 72 and 95, 16384 keys (64q/8kv) 122 and 177;
+      // cold and unshared 64 rows of 8192 keys 109 and 99, of up to 16384 (64q/8kv) 119.5 and 115.5, 4 of 120000 109 and 104;
+      // 285 MB again and again 50 and 53.  V alone read once lies between them in each.
+      if constexpr (kMx) {
         const int vo = lane >> 2;
-        t.k[b][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kr, j * kMxCodeBytes + 16 * qg, 0, kStreamed));
-        t.v[b][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vr, vo * kMxCodeBytes + 16 * (lane & 3), 0, kStreamed));
+        t.k[b][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kr, j * kMxCodeBytes + 16 * qg, 0, 0));
+        t.v[b][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vr, vo * kMxCodeBytes + 16 * (lane & 3), 0, 0));
         t.ks[b] = __builtin_amdgcn_raw_buffer_load_b8(kr, kMxScalesAt + j * kMxScaleBytes + qg, 0, 0);
         t.vs[b] = __builtin_amdgcn_raw_buffer_load_b8(vr, kMxScalesAt + vo * kMxScaleBytes + (lane & 3), 0, 0);
         continue;
