@@ -541,6 +541,14 @@ s2l_status check_plan(const s2l_plan_info* plan, const s2l_batch* b, int32_t hq,
   return S2L_OK;
 }
 
+// Over MXFP4 pages tiles of 128 and 256 columns take scales away from the ends of fp32's range, where the factor
+// log2 e softmax_scale loses bits or overflows.
+s2l_status check_scale(const s2l_kv_cache* cache, float scale, int32_t tile_cols) {
+  if (cache->dtype == S2L_KV_MXFP4 && tile_cols != s2l::kDecodeTileCols && !(scale >= 0x1p-120f && scale <= 0x1p120f))
+    return fail(S2L_ENOTSUP, "softmax_scale %g over MXFP4 pages unsupported (2^-120 to 2^120)", (double)scale);
+  return S2L_OK;
+}
+
 s2l_status attn_common(const s2l_kv_cache* cache, const s2l_batch* batch, const void* q, int32_t hq,
                        float scale, void* out, const s2l_plan_info* plan, const void* ws, size_t ws_bytes,
                        int64_t* T) {
@@ -549,9 +557,7 @@ s2l_status attn_common(const s2l_kv_cache* cache, const s2l_batch* batch, const 
   if ((st = check_batch(batch, true, T)) != S2L_OK) return st;
   if ((st = check_heads(hq, cache->num_kv_heads)) != S2L_OK) return st;
   if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(S2L_EINVAL, "softmax_scale must be finite and > 0");
-  // away from the ends of fp32's range, where the factor log2 e softmax_scale loses bits or overflows
-  if (cache->dtype == S2L_KV_MXFP4 && plan && plan->tile_cols != s2l::kDecodeTileCols && !(scale >= 0x1p-120f && scale <= 0x1p120f))
-    return fail(S2L_ENOTSUP, "softmax_scale %g over MXFP4 pages unsupported (2^-120 to 2^120)", (double)scale);
+  if (plan && (st = check_scale(cache, scale, plan->tile_cols)) != S2L_OK) return st;
   if (*T > 0 && (!q || !out)) return fail(S2L_EINVAL, "q/out is NULL");
   if (plan && plan->num_reqs == batch->num_reqs &&
       plan->lengths != lengths_digest(batch->num_reqs, batch->prefix_lens_host, batch->chunk_lens_host))
@@ -1176,6 +1182,7 @@ s2l_status s2l_chunk_prefill_attn_noalloc(const s2l_kv_cache* cache, const s2l_b
                 "this batch needs %lld bytes of workspace, more than the %zu bytes of scratch the allocation-free "
                 "call holds; use s2l_chunk_prefill_attn with a caller workspace",
                 (long long)pi.workspace_bytes, s2l::kNoAllocScratchBytes);
+  if ((st = check_scale(cache, softmax_scale, o.tile_cols)) != S2L_OK) return st;
   void* ws = nullptr;
   hipError_t e = s2l::noalloc_scratch(&ws);
   if (e != hipSuccess) return hip_fail("taking the scratch array's device address", e);
