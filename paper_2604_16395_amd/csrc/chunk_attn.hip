@@ -48,8 +48,8 @@
 // sub-blocks that reach past the first query token's position.
 //
 // MXFP4 pages: K and V are widened to bf16, exactly, on their way through registers into LDS, as e4m3 pages are, and
-// multiply bf16 queries as they are.  A layer of P = 131072, C = 2048 (8q/1kv) takes 0.90 to 0.92 ms, 1200 to 1230 TFLOP/s
-// (bf16 pages 0.91 to 0.92); 600 tokens without prefix (32q/8kv) 16.4 us.  K's codes multiplied as they are stored on the
+// multiply bf16 queries as they are.  A layer of P = 131072, C = 2048 (8q/1kv) takes 0.90 to 0.97 ms, 1140 to 1230 TFLOP/s
+// (boxes differ); 600 tokens without prefix (32q/8kv) 16.3 us.  K's codes multiplied as they are stored on the
 // f8f6f4 MFMA, by three E2M3 terms of each query, took 0.89 of the time (chunk on 8192 tokens 0.96, 600 tokens 1.03) and held
 // a query only within 2^-13 of the largest of its 32 dims: beside dims 100 times as large that outweighs every other
 // rounding here.  A higher wave priority within a step: the same to 1%.

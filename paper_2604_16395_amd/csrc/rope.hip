@@ -7,8 +7,9 @@
 //
 // Norms (kNorm): a head's squares are summed over its eight lanes before the rotation, fp32 until the one rounding at
 // the end.  One row 2.95 us, 35107 rows of 32 + 8 + 8 heads 163 us, as fast as a copy moves their 863 MB; 2342 rows of
-// 32 + 32 without pages 18.2 us (77 MB, which the last-level cache holds), bound by the arithmetic and, as all waves
-// are resident at once, by loading, computing and storing one after another.
+// 32 + 32 without pages 18 us (77 MB, which the last-level cache holds), bound by the arithmetic and, as all waves
+// are resident at once, by loading, computing and storing one after another.  Into MXFP4 pages one row 3.05 us, 35107 rows
+// 148 us (757 MB), without norms 2.5 and 138; into e4m3 pages 3.1 and 149, 2.6 and 144.
 //
 // A wave takes one row (token) and 8 kHeads of its heads (a workgroup four rows; workgroups of the same rows
 // follow one another); lane l holds unit l % 8 of head l / 8, the 16 elements of 8 pairs in two 16-byte
